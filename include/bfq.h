@@ -52,7 +52,8 @@ typedef enum {
     BFQ_ERR_WORKSPACE = -7,      /* angles not set yet, or plan workspace too small */
     BFQ_ERR_CUDA = -8,           /* a CUDA runtime call failed; see bfq_last_cuda_error */
     BFQ_ERR_DEVICE_TIMEOUT = -9, /* a bounded device-side wait gave up (reported by bfq_device_status) */
-    BFQ_ERR_TOO_LARGE = -10      /* bfq_backward_noalloc: n exceeds BFQ_NOALLOC_MAX_N */
+    BFQ_ERR_TOO_LARGE = -10,     /* bfq_backward_noalloc: n exceeds BFQ_NOALLOC_MAX_N; bfq_kv_attend: more row tiles than it numbers */
+    BFQ_ERR_INDEX = -11          /* a slot, position, page or length on the device outside its range (reported by bfq_device_status) */
 } bfq_status;
 
 #define BFQ_MIN_N 16
@@ -216,7 +217,8 @@ int bfq_backward_noalloc(int n, const float* theta, const void* x, bfq_dtype xt,
                          int64_t rows, int64_t ld, void* dx, bfq_dtype dxt, float* dtheta, void* stream);
 
 /* Synchronises the device and returns BFQ_OK, or BFQ_ERR_DEVICE_TIMEOUT if a kernel of this plan
- * reported a bounded wait that ran out, or BFQ_ERR_CUDA.  (No counterpart in the paper.) */
+ * reported a bounded wait that ran out, or BFQ_ERR_INDEX if one met an index outside its range (bfq_kv_*), or BFQ_ERR_CUDA.  What is
+ * reported is forgotten.  (No counterpart in the paper.) */
 int bfq_device_status(bfq_plan* plan);
 
 /* Last cudaError_t seen by this plan (0 = cudaSuccess).  (No counterpart in the paper.) */
@@ -345,6 +347,100 @@ int bfq_measure_fma_rates(float* cycles_per_instruction);
  * memory.  Returns BFQ_OK, BFQ_ERR_NULL, BFQ_ERR_CUDA or BFQ_ERR_DEVICE_TIMEOUT (a bounded wait ran out).
  */
 int bfq_measure_mma_rates(float* cycles_per_mma);
+
+/*
+ * Paged low-bit cache of rotated keys and values, and attention over it.  (No counterpart in the paper: its invariance (Sec. 3.1) for
+ * the third thing that a low-bit model holds in memory.  With Q on the elements of a head, (Q q) . (Q k) = q . k, and a row of Q k is
+ * quantized as activations are.)  The plan's n is the head dimension, 64 or 128, else BFQ_ERR_UNSUPPORTED_N.
+ *
+ * A cache is four arrays of the caller's on the device: for keys and for values codes [pages][heads][page_size][n * bits / 8] bytes and
+ * scales [pages][heads][page_size] fp16 bits, in the formats of bfq_forward_quant, a scale for each row.  Within a page everything is
+ * contiguous; *_page is the distance from page to page (codes: bytes, scales: elements; multiples of 16 bytes).  bits is 4 or 8,
+ * page_size a power of two from 16 to 256; all pointers are 16-byte aligned.  Slot s is place s % page_size of page s / page_size.
+ */
+typedef struct {
+    uint8_t* k_codes;
+    uint16_t* k_scales;
+    uint8_t* v_codes;
+    uint16_t* v_scales;
+    int64_t k_codes_page, k_scales_page, v_codes_page, v_scales_page;
+    int64_t pages;
+    int heads, page_size, bits;
+} bfq_kv_cache;
+
+/* Rows [tokens][heads][n]: elements of a row contiguous, strides of tokens and heads in elements (multiples of 16 bytes), 16-byte aligned. */
+typedef struct {
+    const void* data;
+    int64_t token, head;
+    int heads;
+} bfq_heads;
+
+/*
+ * What bfq_kv_append does to queries and keys before Q; every part may be left out (NULL).  Norms: x <- w x / sqrt(mean x^2 + eps) over a
+ * head, w fp32 [n].  Position rotation of the first `dims` elements (a multiple of 16, at most n): element pair i, (i, i + dims / 2) or,
+ * interleaved, (2 i, 2 i + 1), by the angle whose cosine is table[position][i] and sine table[position][dims / 2 + i];
+ * table fp32 [rows][dims], 16-byte aligned; positions int32 [tokens].
+ */
+typedef struct {
+    const int32_t* positions;
+    const float* table;
+    int64_t rows;
+    int dims, interleaved;
+    const float* q_norm;
+    const float* k_norm;
+    float eps;
+} bfq_kv_positions;
+
+/*
+ * One pass over a step's new tokens: norms, position rotation (`at`, may be NULL: neither) and Q on queries and keys, Q on values; keys
+ * and values quantized (bfq_forward_quant's quantizer, a row is a head) into the cache at slots[token], queries to q_out in bf16.
+ * slots: int64 [tokens]; a negative slot: the token's keys and values go nowhere (padding).  The other slots must differ from one another:
+ * of two tokens with one slot, parts of either may stay.  q and q_out may both be NULL, and q_out may be q in place where q is bf16.
+ * k, v and q are of type xt.  A slot or position outside its range is reported by bfq_device_status (BFQ_ERR_INDEX): that slot is not
+ * written, that position counts as 0.  Allocates nothing.
+ */
+int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots, int64_t tokens, bfq_dtype xt, const bfq_heads* k, const bfq_heads* v,
+                  const bfq_heads* q, const bfq_heads* q_out, const bfq_kv_positions* at, void* stream);
+/* The rows at any slots, dequantized and turned back (Q^T) into the model's basis: k, v [tokens][heads][n] of type t, 16-byte aligned.  Rows of
+ * negative slots are zero, and of slots outside the cache (which are reported). */
+int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots, int64_t tokens, bfq_dtype t, void* k, void* v, void* stream);
+
+/*
+ * Attention of the last tokens of each sequence over what is cached of it:
+ *     out = Q^T softmax(scale q K^T) V     (K, V: the cache's rows, dequantized; q as bfq_kv_append gives it),
+ * in the model's basis.  Query head h reads key head h / (q.heads / cache heads); at most 128 query heads to a key head.
+ *   q, out      bf16 [tokens][q heads][n]
+ *   lse         fp32 [tokens][q heads], or NULL: log sum exp(scale q k), -infinity for a row without keys
+ *   block_table int32 [batch][table_width], rows table_ld apart: a sequence's pages in order; lengths int32 [batch]: its cached keys, those
+ *               of its own tokens in this call included (pages behind them are not looked at)
+ *   q_starts    int32 [batch + 1], not decreasing: sequence b has tokens q_starts[b] .. q_starts[b + 1] - 1 of q, at most max_new of them, the
+ *               last of which is key lengths[b] - 1; each sees the keys up to its own.  NULL: token b is sequence b's only one.
+ *   prefix      pages of a prefix that all sequences share, int32 [prefix_pages], of which prefix_length keys are read, once for the
+ *               whole batch; every token sees all of them.  lengths and block_table do not count them.  prefix_length 0: none.
+ * A row without keys (no length, or a token in front of its sequence's first key) is zero.  Rows of out and lse of tokens that no
+ * sequence has stay as they were.  A page, length or number of tokens outside its range is reported by bfq_device_status
+ * (BFQ_ERR_INDEX) and the outputs of that call mean nothing; memory outside the arrays is not touched.  workspace: device,
+ * 256-byte aligned, the caller's until the call's work on `stream` is done, at least bfq_kv_attend_workspace bytes (0 on
+ * bad arguments; does not look at the data pointers' contents), BFQ_ERR_WORKSPACE otherwise.  Allocates nothing.
+ */
+typedef struct {
+    bfq_heads q, out;
+    float* lse;
+    int64_t tokens;
+    int batch;
+    const int32_t* block_table;
+    int64_t table_ld;
+    int table_width;
+    const int32_t* lengths;
+    const int32_t* q_starts;
+    int max_new;
+    const int32_t* prefix;
+    int prefix_pages;
+    int64_t prefix_length;
+    float scale;
+} bfq_kv_queries;
+size_t bfq_kv_attend_workspace(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_queries* in);
+int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_queries* in, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Number of CTAs the backward pass uses (= number of d-theta partial sums); informational. */
 int bfq_backward_partials(const bfq_plan* plan);

@@ -10,6 +10,8 @@ import os
 
 import torch
 
+from .kv_cache import KVCache
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbfq.so")
 
@@ -18,7 +20,7 @@ BFQ_OK = 0
 STATUS_NAMES = {
     0: "BFQ_OK", -1: "BFQ_ERR_NULL", -2: "BFQ_ERR_UNSUPPORTED_N", -3: "BFQ_ERR_BITS", -4: "BFQ_ERR_ALIGN",
     -5: "BFQ_ERR_STRIDE", -6: "BFQ_ERR_DTYPE", -7: "BFQ_ERR_WORKSPACE", -8: "BFQ_ERR_CUDA",
-    -9: "BFQ_ERR_DEVICE_TIMEOUT", -10: "BFQ_ERR_TOO_LARGE",
+    -9: "BFQ_ERR_DEVICE_TIMEOUT", -10: "BFQ_ERR_TOO_LARGE", -11: "BFQ_ERR_INDEX",
 }
 
 # name -> (restype, argtypes); must list every symbol include/bfq.h declares
@@ -56,7 +58,29 @@ SIGNATURES = {
     "bfq_composite_forward": (_i, [_p, _p, _i, _p, _i, _i64, _i64, _p, _i, _i64, _p]),
     "bfq_composite_forward_quant": (_i, [_p, _p, _i, _p, _i, _i64, _i64, _i, _p, _p, _p]),
     "bfq_composite_inverse": (_i, [_p, _p, _i, _p, _i, _i64, _i64, _p, _i, _i64, _p]),
+    "bfq_kv_append": (_i, [_p, _p, _p, _i64, _i, _p, _p, _p, _p, _p, _p]),
+    "bfq_kv_read": (_i, [_p, _p, _p, _i64, _i, _p, _p, _p]),
+    "bfq_kv_attend_workspace": (ctypes.c_size_t, [_p, _p, _p]),
+    "bfq_kv_attend": (_i, [_p, _p, _p, _p, ctypes.c_size_t, _p]),
 }
+
+
+class _CKVCache(ctypes.Structure):
+    _fields_ = [("k_codes", _p), ("k_scales", _p), ("v_codes", _p), ("v_scales", _p), ("k_codes_page", _i64), ("k_scales_page", _i64),
+                ("v_codes_page", _i64), ("v_scales_page", _i64), ("pages", _i64), ("heads", _i), ("page_size", _i), ("bits", _i)]
+
+
+class _CHeads(ctypes.Structure):
+    _fields_ = [("data", _p), ("token", _i64), ("head", _i64), ("heads", _i)]
+
+
+class _CPositions(ctypes.Structure):
+    _fields_ = [("positions", _p), ("table", _p), ("rows", _i64), ("dims", _i), ("interleaved", _i), ("q_norm", _p), ("k_norm", _p), ("eps", ctypes.c_float)]
+
+
+class _CQueries(ctypes.Structure):
+    _fields_ = [("q", _CHeads), ("out", _CHeads), ("lse", _p), ("tokens", _i64), ("batch", _i), ("block_table", _p), ("table_ld", _i64), ("table_width", _i),
+                ("lengths", _p), ("q_starts", _p), ("max_new", _i), ("prefix", _p), ("prefix_pages", _i), ("prefix_length", _i64), ("scale", ctypes.c_float)]
 
 _lib = None
 
@@ -452,6 +476,148 @@ class Plan:
                 return c
         _check(self._c.bfq_dequant_gemm(*args, _stream(c)), "bfq_dequant_gemm")
         return c
+
+    # -- paged low-bit cache of keys and values (kv_cache.py); this plan's n is the head dimension -------------------
+    def _cache(self, cache: KVCache):
+        if not isinstance(cache, KVCache) or cache.head_dim != self.n or cache.device != self.device:
+            got = (cache.head_dim, str(cache.device)) if isinstance(cache, KVCache) else type(cache)
+            raise ValueError(f"cache: expected a KVCache of heads of {self.n} elements on {self.device}, got {got}")
+        pages = [t.stride(0) if cache.pages > 1 else t.shape[1:].numel() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+        return ctypes.byref(_CKVCache(cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), *pages,
+                                      cache.pages, cache.heads, cache.page_size, cache.bits))
+
+    def _head_rows(self, t, tokens, heads, dtype, what: str):
+        """Checks rows [tokens][heads][n] (unit inner stride, on the plan's device; tokens, heads, dtype where given) and describes them."""
+        if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[2] != self.n or t.stride(2) != 1:
+            raise ValueError(f"{what}: expected [tokens][heads][{self.n}] with unit inner stride, got {tuple(t.shape) if isinstance(t, torch.Tensor) else type(t)}")
+        _on(t, self.device, what)
+        shape, stride = t.shape, t.stride()
+        if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or shape[1] < 1:
+            raise ValueError(f"{what}: expected [{tokens}][{heads}][{self.n}], got {tuple(shape)}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+        head = stride[1] if shape[1] > 1 else self.n
+        return _CHeads(t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * self.n, head, shape[1])
+
+    def _apart(self, t, what: str):
+        """Rows that are written: no two of them may share memory."""
+        shape, stride = t.shape, t.stride()
+        (few, near), (many, far) = sorted(zip(shape[:2], stride[:2]), key=lambda d: d[1])
+        if t.numel() and ((few > 1 and near < self.n) or (many > 1 and far < (few - 1) * near + self.n)):
+            raise ValueError(f"{what}: rows overlap (strides {stride})")
+
+    def append_kv(self, cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, q: torch.Tensor | None = None,
+                  positions: torch.Tensor | None = None, rope: torch.Tensor | None = None, interleaved: bool = False,
+                  q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6, q_out: torch.Tensor | None = None):
+        """A step's new tokens into the cache: k, v [tokens][heads][n] (bf16 or fp32), quantized at slots int64 [tokens] (negative: nowhere); before
+        that queries and keys are normed per head (q_norm, k_norm fp32 [n]) and rotated by position (positions int32 [tokens], rope fp32
+        [rows][dims]: cosines of dims / 2 frequencies, then sines; pairs (i, i + dims / 2), or (2 i, 2 i + 1) if interleaved), and all are rotated
+        by Q.  Returns the queries as attend_kv takes them, bf16 (q_out, or a new tensor), or None without q."""
+        c = self._cache(cache)
+        ck = self._head_rows(k, None, cache.heads, None, "k")
+        tokens, xt = k.shape[0], _dt(k)
+        cv = self._head_rows(v, tokens, cache.heads, k.dtype, "v")
+        _exact(slots, torch.int64, (tokens,), self.device, "slots")
+        cq = co = None
+        if q is not None:
+            cq = self._head_rows(q, tokens, None, k.dtype, "q")
+            given = q_out is not None
+            if not given:
+                q_out = torch.empty((tokens, q.shape[1], self.n), dtype=torch.bfloat16, device=self.device)
+            co = self._head_rows(q_out, tokens, q.shape[1], torch.bfloat16, "q_out")
+            if given:
+                self._apart(q_out, "q_out")
+        elif q_out is not None or q_norm is not None:
+            raise ValueError("q_out and q_norm are for calls with q")
+        if (positions is None) != (rope is None):
+            raise ValueError("positions and rope come together")
+        at = _CPositions()
+        if positions is not None:
+            _exact(positions, torch.int32, (tokens,), self.device, "positions")
+            if rope.dim() != 2 or not 16 <= rope.shape[1] <= self.n or rope.shape[1] % 16 or not rope.shape[0]:
+                raise ValueError(f"rope: expected [positions][dims], dims a multiple of 16 up to {self.n}, got {tuple(rope.shape)}")
+            _exact(rope, torch.float32, rope.shape, self.device, "rope")
+            at.positions, at.table, at.rows, at.dims, at.interleaved = positions.data_ptr(), rope.data_ptr(), rope.shape[0], rope.shape[1], bool(interleaved)
+        if q_norm is not None:
+            at.q_norm = _exact(q_norm, torch.float32, (self.n,), self.device, "q_norm").data_ptr()
+        if k_norm is not None:
+            at.k_norm = _exact(k_norm, torch.float32, (self.n,), self.device, "k_norm").data_ptr()
+        at.eps = eps
+        ref = ctypes.byref
+        _check(self._c.bfq_kv_append(self._h, c, slots.data_ptr(), tokens, xt, ref(ck), ref(cv), ref(cq) if cq is not None else None,
+                                     ref(co) if co is not None else None, ref(at), _stream(k)), "bfq_kv_append")
+        return q_out
+
+    def read_kv(self, cache: KVCache, slots: torch.Tensor, dtype=torch.bfloat16):
+        """-> (k, v) [tokens][heads][n] of `dtype` (bf16 or fp32): the rows at slots int64 [tokens], dequantized and in the model's basis;
+        zeros for a negative slot."""
+        c = self._cache(cache)
+        kind = _DTYPES.get(dtype)
+        if kind is None:
+            raise TypeError(f"unsupported dtype {dtype}")
+        if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+            raise ValueError("slots: expected int64 [tokens]")
+        tokens = slots.shape[0]
+        _exact(slots, torch.int64, (tokens,), self.device, "slots")
+        k, v = torch.empty((2, tokens, cache.heads, self.n), dtype=dtype, device=self.device).unbind(0)
+        _check(self._c.bfq_kv_read(self._h, c, slots.data_ptr(), tokens, kind, k.data_ptr(), v.data_ptr(), _stream(slots)), "bfq_kv_read")
+        return k, v
+
+    def attend_kv(self, cache: KVCache, q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, scale: float | None = None,
+                  q_starts: torch.Tensor | None = None, max_new: int | None = None, prefix: torch.Tensor | None = None, prefix_length: int = 0,
+                  want_lse: bool = False, out: torch.Tensor | None = None):
+        """Attention of q, bf16 [tokens][heads][n] as append_kv gives it, over the cached keys and values of each sequence; out in the model's
+        basis, bf16.  block_table int32 [batch][width]: a sequence's pages; lengths int32 [batch]: its cached keys, this call's tokens
+        included.  q_starts int32 [batch + 1] with max_new, the most tokens that a sequence has in q: each sees the keys up to its own;
+        without them token b is sequence b's only one.  prefix int32 [pages], prefix_length: keys in front of every sequence, read once for
+        all.  scale: 1 / sqrt(n) by default.  want_lse: (out, fp32 [tokens][heads] log sum exp of the scaled scores).  Rows of tokens behind
+        the last sequence are not written."""
+        c = self._cache(cache)
+        cq = self._head_rows(q, None, None, torch.bfloat16, "q")
+        tokens, heads = q.shape[0], q.shape[1]
+        if heads % cache.heads or heads // cache.heads > 128:
+            raise ValueError(f"q: {heads} heads are not 1 to 128 for each of the cache's {cache.heads}")
+        if not isinstance(lengths, torch.Tensor) or lengths.dim() != 1:
+            raise ValueError("lengths: expected int32 [batch]")
+        batch = lengths.shape[0]
+        _exact(lengths, torch.int32, (batch,), self.device, "lengths")
+        if not isinstance(block_table, torch.Tensor) or block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch or \
+                (block_table.shape[1] > 1 and block_table.stride(1) != 1) or (batch > 1 and block_table.stride(0) < block_table.shape[1]):
+            raise ValueError(f"block_table: expected int32 [{batch}][pages] with unit inner stride")
+        _on(block_table, self.device, "block_table")
+        if q_starts is not None:
+            _exact(q_starts, torch.int32, (batch + 1,), self.device, "q_starts")
+            if max_new is None or (tokens and not 1 <= max_new):
+                raise ValueError("q_starts: max_new, the most tokens of a sequence, is needed and at least 1")
+            max_new = min(int(max_new), max(tokens, 1))
+        elif tokens < batch:
+            raise ValueError(f"q: expected a token for each of {batch} sequences, got {tokens}")
+        if prefix is None:
+            if prefix_length:
+                raise ValueError("prefix_length without prefix")
+        else:
+            if not isinstance(prefix, torch.Tensor) or prefix.dim() != 1:
+                raise ValueError("prefix: expected int32 [pages]")
+            _exact(prefix, torch.int32, (prefix.shape[0],), self.device, "prefix")
+            if not 0 <= prefix_length <= prefix.shape[0] * cache.page_size:
+                raise ValueError(f"prefix_length: {prefix_length} keys are not in {prefix.shape[0]} pages of {cache.page_size}")
+        given = out is not None
+        if not given:
+            out = torch.empty((tokens, heads, self.n), dtype=torch.bfloat16, device=self.device)
+        co = self._head_rows(out, tokens, heads, torch.bfloat16, "out")
+        if given:
+            self._apart(out, "out")
+        lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device) if want_lse else None
+        if tokens and batch:
+            a = _CQueries(cq, co, lse.data_ptr() if want_lse else None, tokens, batch, block_table.data_ptr(),
+                          block_table.stride(0) if batch > 1 else block_table.shape[1], block_table.shape[1], lengths.data_ptr(),
+                          q_starts.data_ptr() if q_starts is not None else None, max_new or 1, prefix.data_ptr() if prefix is not None else None,
+                          prefix.shape[0] if prefix is not None else 0, int(prefix_length), float(scale) if scale is not None else self.n ** -0.5)
+            a = ctypes.byref(a)
+            size = self._c.bfq_kv_attend_workspace(self._h, c, a)
+            room = torch.empty(size + 256, dtype=torch.uint8, device=self.device)
+            _check(self._c.bfq_kv_attend(self._h, c, a, (room.data_ptr() + 255) // 256 * 256, size, _stream(q)), "bfq_kv_attend")
+        return (out, lse) if want_lse else out
 
     def device_status(self) -> int:
         return int(self._c.bfq_device_status(self._h))

@@ -835,7 +835,7 @@ int bfq_device_status(bfq_plan* plan) {
     if (e != cudaSuccess) return cuda_fail(plan, e);
     if (word != 0) {
         cudaMemset(plan->status_word, 0, sizeof(int));
-        return BFQ_ERR_DEVICE_TIMEOUT;
+        return word == kBadIndex ? BFQ_ERR_INDEX : BFQ_ERR_DEVICE_TIMEOUT;
     }
     return BFQ_OK;
 }
@@ -875,6 +875,7 @@ const char* bfq_status_string(int status) {
         case BFQ_ERR_CUDA: return "CUDA runtime error";
         case BFQ_ERR_DEVICE_TIMEOUT: return "bounded device-side wait gave up";
         case BFQ_ERR_TOO_LARGE: return "row length exceeds the fixed scratch of the no-allocation entry point";
+        case BFQ_ERR_INDEX: return "index on the device out of range";
         default: return "unknown status";
     }
 }

@@ -6,6 +6,7 @@
 namespace bfq {
 constexpr int kMaxDevices = 64;
 constexpr int kBackwardCtasPerSm = 2;  // upper bound on resident backward CTAs per SM (sizes the partial sums)
+constexpr int kBadIndex = 16;  // status word: an index on the device outside its range; other values: a wait that ran out
 }  // namespace bfq
 
 struct bfq_plan {

@@ -1,0 +1,565 @@
+"""The paged low-bit cache of rotated keys and values (Plan.append_kv, read_kv, attend_kv) against plain float64.
+
+Tolerances, from the arithmetic (a rounding to bf16 is off by at most 2^-8 of the value, to fp32 by 2^-24):
+  * appended rows: the quantizer's rule of tests/parity.py (codes exact but next to a boundary, scales within one fp16 step); queries and rows
+    read back: one rounding to the output's type plus fp32 arithmetic, 1e-5 of the row's norm (some thirty operations of 2^-24 each).
+  * attention: with P the probabilities and V the cached values, in the rotated basis each probability is rounded once to bf16 after its value's
+    scale, so |error| <= 2^-8 P |V|.  A score is an fp32 sum of D exact products, off by at most 2^-16 scale |q| |k| (128 additions of 2^-23), which
+    with the exponential's 2^-20 is the relative error of a probability, twice with the sum's; the sums over the keys add 2^-23 a key.  The
+    basis change takes that bound through |Q|, and the result is rounded once: 2^-8 |out|."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2509_09679_b200 import BfqError, KVCache, Plan, binding, synth
+from parity import Guarded, check_quant, to_f64
+
+DEV = "cuda:0"
+gpu = pytest.mark.gpu
+
+
+# ---- the cache and its calls in plain float64 ----------------------------------------------------------------------------
+def make_plan(n, kind="normal", seed=3):
+    theta = synth.angles(n, kind, seed)
+    p = Plan(n, DEV)
+    p.set_angles(theta.to(DEV))
+    return p, to_f64(theta)
+
+
+def make_cache(pages, heads, n, page, bits, seed):
+    """A cache full of rows of uneven sizes, some of them zero, and its values in float64 [pages][heads][page][n] (rotated basis)."""
+    rng = np.random.default_rng(seed)
+    parts, values = [], []
+    for _ in range(2):
+        y = rng.standard_normal((pages * heads * page, n)) * rng.uniform(0.2, 2.0, (pages * heads * page, 1))
+        y[rng.random(y.shape[0]) < 0.02] = 0.0
+        codes, scales = oracle.quantize(y, bits)
+        parts += [torch.from_numpy(oracle.pack(codes, bits)).view(pages, heads, page, -1), torch.from_numpy(scales.view(np.int16)).view(torch.float16).view(pages, heads, page)]
+        values.append(oracle.dequantize(codes, scales).reshape(pages, heads, page, n))
+    return KVCache(*(t.to(DEV) for t in parts), bits), values
+
+
+def dense(theta):
+    n = 2 * theta.shape[1]
+    return oracle.forward(theta, np.eye(n)).T.copy()  # rows of the identity: the columns of Q
+
+
+def positioned(x, w, eps, positions, table, interleaved):
+    """Norm and position rotation of [tokens][heads][n] in float64."""
+    if w is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * w
+    if positions is None:
+        return x
+    x, r = x.copy(), table.shape[1]
+    i, j = (np.arange(0, r, 2), np.arange(1, r, 2)) if interleaved else (np.arange(r // 2), np.arange(r // 2, r))
+    c, s = table[positions][:, None, : r // 2], table[positions][:, None, r // 2:]
+    a, b = x[..., i], x[..., j]
+    x[..., i], x[..., j] = a * c - b * s, b * c + a * s
+    return x
+
+
+def rows_at(cache, which, slots):
+    codes, scales = (cache.k_codes, cache.k_scales) if which == "k" else (cache.v_codes, cache.v_scales)
+    at, place = slots // cache.page_size, slots % cache.page_size
+    return codes[at, :, place], scales[at, :, place]
+
+
+def rope_table(rows, dims):
+    angle = np.arange(rows)[:, None] * 10000.0 ** (-np.arange(0, dims, 2) / dims)
+    return torch.from_numpy(np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32))
+
+
+def attention(q, theta, k, v, table, lengths, starts, page, scale, prefix=None, prefix_length=0):
+    """-> (out, lse, error bound of out, of lse) [tokens][heads][n]; k, v [pages][heads][page][n], q float64 in the rotated basis."""
+    tokens, heads, n = q.shape
+    group = heads // k.shape[1]
+    out, bound = np.zeros_like(q), np.zeros_like(q)
+    lse, lse_bound = np.full((tokens, heads), -np.inf), np.zeros((tokens, heads))
+    Q = dense(theta)
+    for b, length in enumerate(lengths):
+        first, last = starts[b], starts[b + 1]
+        for h in range(heads):
+            flat = lambda x, pages, count: x[pages, h // group].reshape(-1, n)[:count]
+            kk, vv = flat(k, table[b], length), flat(v, table[b], length)
+            for t in range(first, last):
+                own = max(0, length - (last - first) + (t - first) + 1)
+                ks, vs = kk[:own], vv[:own]
+                if prefix_length:
+                    ks, vs = np.concatenate([flat(k, prefix, prefix_length), ks]), np.concatenate([flat(v, prefix, prefix_length), vs])
+                if not len(ks):
+                    continue
+                s = ks @ q[t, h] * scale
+                e = np.exp(s - s.max())
+                p = e / e.sum()
+                out[t, h] = p @ vs @ Q
+                delta = 2.0 ** -16 * (np.abs(ks) @ np.abs(q[t, h])).max() * abs(scale) + 2.0 ** -20 + 2.0 ** -23 * np.abs(s).max()
+                bound[t, h] = (2.0 ** -8 + 2 * delta + len(ks) * 2.0 ** -23) * (p @ np.abs(vs)) @ np.abs(Q) + (2.0 ** -8 + 1e-6) * np.abs(out[t, h]) + 1e-30
+                lse[t, h] = s.max() + np.log(e.sum())
+                lse_bound[t, h] = delta + 2.0 ** -22 * abs(lse[t, h]) + len(ks) * 2.0 ** -23
+    return out, lse, bound, lse_bound
+
+
+def check_attention(got, lse, want):
+    ref, ref_lse, bound, lse_bound = want
+    o = to_f64(got)
+    assert np.isfinite(o).all()
+    err = np.abs(o - ref)
+    assert (err <= bound).all(), f"{(err > bound).sum()} elements, worst {(err / np.maximum(bound, 1e-300)).max():.3g} of the bound"
+    if lse is not None:
+        l = to_f64(lse)
+        assert ((l == -np.inf) == (ref_lse == -np.inf)).all()
+        fine = np.isfinite(ref_lse)
+        assert (np.abs(l[fine] - ref_lse[fine]) <= lse_bound[fine]).all()
+
+
+def tables(lengths, page, extra_pages, seed, prefix_pages=0):
+    """Pages of each sequence in a shuffled cache: (block table, prefix pages, pages in all)."""
+    width = max(1, -(-max(lengths) // page))
+    pages = len(lengths) * width + prefix_pages + extra_pages
+    order = np.random.default_rng(seed).permutation(pages)
+    return order[prefix_pages:prefix_pages + len(lengths) * width].reshape(len(lengths), width), order[:prefix_pages], pages
+
+
+def i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+# ---- appending -------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,bits,page,dtype,hq,hkv,tokens", [
+    (128, 4, 64, torch.bfloat16, 8, 2, 37), (128, 8, 16, torch.bfloat16, 5, 5, 1), (64, 4, 16, torch.float32, 7, 1, 130), (64, 8, 256, torch.bfloat16, 6, 3, 300),
+    (128, 4, 32, torch.float32, 2, 2, 75), (128, 8, 128, torch.float32, 16, 1, 33)])
+@pytest.mark.parametrize("norm,dims,interleaved", [(True, "all", False), (False, "half", False), (True, "all", True), (False, "half", True), (True, 0, False)])
+def test_append(n, bits, page, dtype, hq, hkv, tokens, norm, dims, interleaved):
+    p, theta = make_plan(n)
+    g = torch.Generator().manual_seed(5)
+    qkv = torch.randn((tokens, hq + 2 * hkv, n), generator=g)
+    qkv[:, :, 3] *= 20
+    qkv[tokens // 2, hq + hkv] = 0.0  # a row of zeros among the values
+    qkv = qkv.to(dtype)
+    dev = qkv.to(DEV)
+    cache, _ = make_cache(3 + 2 * tokens // page, hkv, n, page, bits, 7)
+    slots = torch.randperm(cache.pages * page, generator=g)[:tokens]
+    slots[1::7] = -1
+    dims = {"all": n, "half": n // 2}.get(dims, 0)
+    table = rope_table(500, dims) if dims else None
+    positions = torch.randint(0, 500, (tokens,), generator=g, dtype=torch.int32) if dims else None
+    w = 1 + 0.3 * torch.randn((2, n), generator=g) if norm else [None, None]
+    before = {name: getattr(cache, name).clone() for name in ("k_codes", "k_scales", "v_codes", "v_scales")}
+    put = lambda t: None if t is None else t.to(DEV)
+    q = p.append_kv(cache, dev[:, hq:hq + hkv], dev[:, hq + hkv:], slots.to(DEV), q=dev[:, :hq], positions=put(positions), rope=put(table), interleaved=interleaved,
+                    q_norm=put(w[0]), k_norm=put(w[1]), eps=1e-5)
+    assert p.device_status() == 0
+    x = to_f64(qkv)
+    turn = lambda t, weight: positioned(t, None if weight is None else to_f64(weight), 1e-5, None if positions is None else positions.numpy(),
+                                        None if table is None else to_f64(table), interleaved)
+    wq = oracle.forward(theta, turn(x[:, :hq], w[0]).reshape(-1, n)).reshape(tokens, hq, n)
+    err, norms = np.abs(to_f64(q) - wq), np.linalg.norm(wq, axis=-1, keepdims=True)
+    assert q.dtype == torch.bfloat16 and (err <= 2.0 ** -8 * np.abs(wq) + 1e-5 * norms).all()
+    keep = (slots >= 0).numpy()
+    at = slots[slots >= 0].to(DEV)
+    for which, ref in (("k", turn(x[:, hq:hq + hkv], w[1])), ("v", x[:, hq + hkv:])):
+        codes, scales = rows_at(cache, which, at)
+        check_quant(codes.reshape(-1, codes.shape[-1]), scales.reshape(-1), oracle.forward(theta, ref[keep].reshape(-1, n)), bits, which)
+    for name, old in before.items():  # every other place as it was
+        now = getattr(cache, name).clone()
+        now[at // page, :, at % page] = old[at // page, :, at % page]
+        assert torch.equal(now, old), name
+
+
+@gpu
+def test_append_without_queries_and_in_place():
+    p, theta = make_plan(128)
+    cache, _ = make_cache(4, 2, 128, 16, 4, 1)
+    other, _ = make_cache(4, 2, 128, 16, 4, 1)
+    x = torch.randn((9, 8, 128), device=DEV).to(torch.bfloat16)
+    slots = torch.arange(5, 14, device=DEV)
+    assert p.append_kv(cache, x[:, 4:6], x[:, 6:], slots) is None
+    q = p.append_kv(other, x[:, 4:6], x[:, 6:], slots, q=x[:, :4])
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        assert torch.equal(getattr(cache, name), getattr(other, name))
+    back = x[:, :4]
+    assert p.append_kv(other, x[:, 4:6], x[:, 6:], slots, q=back, q_out=back) is back and torch.equal(back, q)
+    assert p.append_kv(cache, x[:0, 4:6], x[:0, 6:], slots[:0], q=x[:0, :4]).shape == (0, 4, 128)
+
+
+@gpu
+def test_append_writes_nothing_outside():
+    n, page, heads = 64, 16, 3
+    p, _ = make_plan(n)
+    guards = [Guarded((5, heads, page, n // 2), torch.uint8, DEV), Guarded((5, heads, page), torch.float16, DEV),
+              Guarded((5, heads, page, n // 2), torch.uint8, DEV), Guarded((5, heads, page), torch.float16, DEV)]
+    cache = KVCache(*(g.view for g in guards), 4)
+    q_out = Guarded((80, 6, n), torch.bfloat16, DEV)
+    x = torch.randn((80, 12, n), device=DEV)
+    p.append_kv(cache, x[:, 6:9], x[:, 9:], torch.randperm(80, device=DEV), q=x[:, :6], q_out=q_out.view)
+    torch.cuda.synchronize()
+    assert all(g.intact() for g in guards + [q_out])
+
+
+@gpu
+@pytest.mark.parametrize("n", [64, 128])
+def test_append_reports_slots_and_positions_outside(n):
+    p, theta = make_plan(n)
+    cache, _ = make_cache(2, 1, n, 16, 8, 2)
+    before = cache.k_codes.clone()
+    x = torch.randn((3, 3, n), device=DEV)
+    p.append_kv(cache, x[:, 1:2], x[:, 2:], torch.tensor([3, 32, 1 << 40], device=DEV), q=x[:, :1])
+    assert p.device_status() == -11 and p.device_status() == 0
+    assert (cache.k_codes != before).nonzero()[:, [0, 2]].unique(dim=0).tolist() == [[0, 3]]
+    table, slots = rope_table(4, 16).to(DEV), torch.arange(3, device=DEV)
+    at_zero = p.append_kv(cache, x[:, 1:2], x[:, 2:], slots, q=x[:, :1], positions=i32([0, 0, 0]), rope=table)
+    assert p.device_status() == 0
+    assert torch.equal(p.append_kv(cache, x[:, 1:2], x[:, 2:], slots, q=x[:, :1], positions=i32([4, -1, 1 << 30]), rope=table), at_zero)
+    assert p.device_status() == -11
+
+
+# ---- reading back ------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,bits,page,heads,tokens", [(128, 4, 64, 3, 130), (64, 8, 16, 1, 1), (128, 8, 32, 2, 67), (64, 4, 128, 5, 1001)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_read(n, bits, page, heads, tokens, dtype):
+    p, theta = make_plan(n, "uniform")
+    cache, values = make_cache(7, heads, n, page, bits, 3)
+    slots = torch.randint(0, 7 * page, (tokens,), generator=torch.Generator().manual_seed(1))
+    slots[tokens // 2::5] = -1
+    got = p.read_kv(cache, slots.to(DEV), dtype)
+    s = slots.clamp(min=0).numpy()
+    for out, value in zip(got, values):
+        rows = value[s // page, :, s % page]
+        rows[slots.numpy() < 0] = 0.0
+        ref = oracle.inverse(theta, rows.reshape(-1, n)).reshape(rows.shape)
+        tol = (2.0 ** -8 if dtype == torch.bfloat16 else 0.0) * np.abs(ref) + 1e-5 * np.linalg.norm(rows, axis=-1, keepdims=True)
+        assert out.dtype == dtype and (np.abs(to_f64(out) - ref) <= tol).all()
+    assert p.device_status() == 0
+    p.read_kv(cache, torch.tensor([7 * page], device=DEV))
+    assert p.device_status() == -11
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+EDGES = [0, 1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300, 1000]
+
+
+@gpu
+@pytest.mark.parametrize("n,bits,page,hq,hkv", [(128, 4, 64, 8, 2), (128, 8, 16, 3, 3), (64, 4, 32, 16, 1), (64, 8, 256, 7, 1), (128, 4, 16, 34, 2), (64, 4, 128, 128, 1)])
+def test_attend_one_token(n, bits, page, hq, hkv):
+    p, theta = make_plan(n)
+    table, _, pages = tables(EDGES, page, 3, 11)
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 12)
+    q = (2 * torch.randn((len(EDGES), hq, n), generator=torch.Generator().manual_seed(13))).to(torch.bfloat16)
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(EDGES), want_lse=True)
+    assert p.device_status() == 0
+    check_attention(out, lse, attention(to_f64(q), theta, k, v, table, EDGES, range(len(EDGES) + 1), page, n ** -0.5))
+    assert torch.equal(out, p.attend_kv(cache, q.to(DEV), i32(table), i32(EDGES)))
+
+
+@gpu
+@pytest.mark.parametrize("length", [1, 77, 64 * 300 + 1])
+def test_attend_one_sequence(length):
+    n, page = 128, 64
+    p, theta = make_plan(n)
+    table, _, pages = tables([length], page, 1, 21)
+    cache, (k, v) = make_cache(pages, 1, n, page, 4, 22)
+    q = (3 * torch.randn((1, 4, n), generator=torch.Generator().manual_seed(23))).to(torch.bfloat16)
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32([length]), scale=0.2, want_lse=True)
+    check_attention(out, lse, attention(to_f64(q), theta, k, v, table, [length], [0, 1], page, 0.2))
+
+
+@gpu
+@pytest.mark.parametrize("n,bits,page,hq,hkv", [(128, 4, 64, 8, 2), (64, 8, 16, 5, 1), (128, 8, 32, 2, 2), (64, 4, 64, 14, 2)])
+@pytest.mark.parametrize("news,lengths", [([3, 1, 0, 5, 2], [3, 70, 9, 200, 1]), ([40, 7], [40, 129]), ([130, 1, 260], [500, 0, 260]), ([300], [310])])
+def test_attend_several_tokens(n, bits, page, hq, hkv, news, lengths):
+    """Causal in a sequence's own tokens; a sequence of more tokens than keys has rows without any."""
+    p, theta = make_plan(n)
+    table, _, pages = tables(lengths, page, 2, 31)
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 32)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = (2 * torch.randn((starts[-1], hq, n), generator=torch.Generator().manual_seed(33))).to(torch.bfloat16)
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True)
+    assert p.device_status() == 0
+    check_attention(out, lse, attention(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5))
+
+
+@gpu
+@pytest.mark.parametrize("n,bits,page,hq,hkv", [(128, 4, 64, 8, 2), (64, 8, 16, 7, 1), (128, 8, 32, 3, 3), (64, 4, 128, 40, 2)])
+@pytest.mark.parametrize("prefix_length,news,lengths", [(1, None, [1, 0, 33]), (64, None, [100] * 5), (1000, None, [5, 64, 0, 130, 1, 2, 3, 4, 5]), (129, [2, 0, 7], [2, 5, 90]),
+                                                        (700, [50, 3], [60, 3]), (320, None, [0, 0])])
+def test_attend_shared_prefix(n, bits, page, hq, hkv, prefix_length, news, lengths):
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 2, 41, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 42)
+    starts = np.concatenate([[0], np.cumsum(news)]) if news else np.arange(len(lengths) + 1)
+    q = (2 * torch.randn((starts[-1], hq, n), generator=torch.Generator().manual_seed(43))).to(torch.bfloat16)
+    some = dict(q_starts=i32(starts), max_new=max(news)) if news else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), prefix=i32(prefix), prefix_length=prefix_length, want_lse=True, **some)
+    assert p.device_status() == 0
+    check_attention(out, lse, attention(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
+
+
+@gpu
+def test_attend_a_prefix_alone():
+    """Sequences without pages of their own: a block table of width 0."""
+    p, theta = make_plan(128)
+    cache, (k, v) = make_cache(3, 1, 128, 64, 4, 1)
+    q = torch.randn((5, 2, 128), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    out = p.attend_kv(cache, q.to(DEV), i32(np.zeros((5, 0))), i32([0] * 5), prefix=i32([2, 0, 1]), prefix_length=150)
+    check_attention(out, None, attention(to_f64(q), theta, k, v, np.zeros((5, 0), int), [0] * 5, range(6), 64, 128 ** -0.5, [2, 0, 1], 150))
+
+
+@gpu
+@pytest.mark.parametrize("prefix_length", [0, 200])
+def test_attend_large_and_uneven_scores(prefix_length):
+    """Scores that rise and fall by hundreds along the keys: the reference moves often, most probabilities vanish."""
+    n, page, lengths = 128, 16, [600, 333]
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 0, 51, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, 1, n, page, 8, 52)
+    q = (torch.tensor([1.0, 20.0, 60.0, 0.0]).view(1, 4, 1) * torch.randn((2, 4, n), generator=torch.Generator().manual_seed(53))).to(torch.bfloat16)
+    some = dict(prefix=i32(prefix), prefix_length=prefix_length) if prefix_length else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), want_lse=True, **some)
+    check_attention(out, lse, attention(to_f64(q), theta, k, v, table, lengths, range(3), page, n ** -0.5, prefix, prefix_length))
+
+
+@gpu
+def test_attend_strides_and_rows_of_no_sequence():
+    n, page, hq, hkv, lengths, news = 128, 32, 4, 2, [50, 20], [3, 1]
+    p, theta = make_plan(n)
+    table, _, pages = tables(lengths, page, 0, 61)
+    made, (k, v) = make_cache(pages, hkv, n, page, 4, 62)
+    both = torch.zeros((pages, 2, hkv, page, n // 2), dtype=torch.uint8, device=DEV)  # keys and values of a page side by side
+    both[:, 0], both[:, 1] = made.k_codes, made.v_codes
+    scales = torch.zeros((pages, 2, hkv, page), dtype=torch.float16, device=DEV)
+    scales[:, 0], scales[:, 1] = made.k_scales, made.v_scales
+    cache = KVCache(both[:, 0], scales[:, 0], both[:, 1], scales[:, 1], 4)
+    wide = torch.zeros((2, table.shape[1] + 3), dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = i32(table)
+    q = torch.randn((hq, 7, n), generator=torch.Generator().manual_seed(63)).to(torch.bfloat16).transpose(0, 1)  # heads outermost
+    out = torch.full((7, hq + 1, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    p.attend_kv(cache, q.to(DEV), wide[:, :table.shape[1]], i32(lengths), q_starts=i32([1, 4, 5]), max_new=3, out=out[:, 1:])
+    want = attention(to_f64(q), theta, k, v, table, lengths, [1, 4, 5], page, n ** -0.5)
+    check_attention(out[1:5, 1:], None, tuple(w[1:5] for w in want))
+    assert (out[:, 0] == 7).all() and (out[:1] == 7).all() and (out[5:] == 7).all()
+
+
+@gpu
+def test_attend_reports_what_is_out_of_range():
+    p, _ = make_plan(64)
+    cache, _ = make_cache(4, 1, 64, 16, 4, 1)
+    q = torch.randn((2, 2, 64), device=DEV).to(torch.bfloat16)
+    table = i32([[0, 1], [2, 3]])
+    good = p.attend_kv(cache, q, table, i32([20, 32]))
+    assert p.device_status() == 0
+    p.attend_kv(cache, q, i32([[0, 4], [-1, 3]]), i32([20, 32]))
+    assert p.device_status() == -11
+    p.attend_kv(cache, q, table, i32([33, -1]))
+    assert p.device_status() == -11
+    p.attend_kv(cache, q, table, i32([20, 32]), prefix=i32([1 << 20]), prefix_length=3)
+    assert p.device_status() == -11
+    assert torch.equal(p.attend_kv(cache, q, i32([[0, 1], [2, 3]]), i32([20, 32])), good)
+    p.attend_kv(cache, q, table[:1], i32([20]), q_starts=i32([0, 2]), max_new=1)  # more tokens than it was told
+    assert p.device_status() == -11
+
+
+@gpu
+def test_calls_on_other_streams_and_in_graphs():
+    """A captured step replayed on new inputs, beside another captured step with a workspace of its own."""
+    n, page, lengths = 128, 64, [130, 64, 999]
+    p, theta = make_plan(n)
+    table, _, pages = tables([1000] * 3, page, 0, 71)
+    cache, _ = make_cache(pages, 2, n, page, 4, 72)
+    t, lens = i32(table), i32(lengths)
+    x = torch.randn((3, 12, n), device=DEV).to(torch.bfloat16)
+    slots = torch.tensor([table[b][(m - 1) // page] * page + (m - 1) % page for b, m in enumerate(lengths)], device=DEV)
+
+    def step():
+        q = p.append_kv(cache, x[:, 8:10], x[:, 10:], slots, q=x[:, :8])
+        return p.attend_kv(cache, q, t, lens)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = step()
+    side.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    outs = []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(step())
+    for g, o in zip(graphs, outs):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, first)
+    x.copy_(torch.randn_like(x))
+    lens.copy_(i32([1000, 1, 500]))
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    got = outs[0].clone()
+    assert torch.equal(got, step()) and not torch.equal(got, first) and p.device_status() == 0
+
+
+@gpu
+def test_a_cache_larger_than_four_gigabytes():
+    n, page, heads, pages = 128, 256, 8, 17000  # 4.46 GB of codes for keys, and for values
+    p, theta = make_plan(n)
+    at = [pages - 1, 3, pages - 2]
+    small, (k, v) = make_cache(3, heads, n, page, 8, 81)
+    cache = KVCache(*(torch.empty((pages, *t.shape[1:]), dtype=t.dtype, device=DEV) for t in (small.k_codes, small.k_scales, small.v_codes, small.v_scales)), 8)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        getattr(cache, name)[at] = getattr(small, name)
+    q = torch.randn((1, heads, n), generator=torch.Generator().manual_seed(82)).to(torch.bfloat16)
+    length = 3 * page - 5
+    out = p.attend_kv(cache, q.to(DEV), i32([at]), i32([length]))
+    check_attention(out, None, attention(to_f64(q), theta, k, v, np.array([[0, 1, 2]]), [length], [0, 1], page, n ** -0.5))
+    slots = torch.tensor([pages * page - 1, (pages - 2) * page], device=DEV)
+    x = torch.randn((2, 2 * heads, n), device=DEV)
+    p.append_kv(cache, x[:, :heads], x[:, heads:], slots)
+    got = p.read_kv(cache, slots, torch.float32)
+    for side, ref in zip(got, (x[:, :heads], x[:, heads:])):
+        assert ((side - ref).norm(dim=-1) < 0.02 * ref.norm(dim=-1)).all()  # 8 bits: a step of max / 127, half of it at most, in 128 places
+    assert p.device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("bits,page", [(8, 16), (4, 64)])
+def test_a_prompt_and_decoded_tokens_behind_a_shared_prefix(bits, page):
+    """The calls as a serving loop makes them, against attention in float64 over the rows as the cache gives them back."""
+    n, hq, hkv, shared = 128, 8, 2, 150
+    p, theta = make_plan(n)
+    g = torch.Generator().manual_seed(91)
+    table, prefix, pages = tables([200] * 3, page, 0, 92, -(-shared // page))
+    cache = KVCache.empty(pages, hkv, n, page, bits, DEV)
+    rope = rope_table(1000, n).to(DEV)
+    norm = (1 + 0.1 * torch.randn(n, generator=g)).to(DEV)
+    slot = lambda row, i: int(row[i // page]) * page + i % page
+    make = lambda t: torch.randn((t, hq + 2 * hkv, n), generator=g).to(torch.bfloat16).to(DEV)
+
+    def append(x, slots, positions):
+        return p.append_kv(cache, x[:, hq:hq + hkv], x[:, hq + hkv:], torch.tensor(slots, device=DEV), q=x[:, :hq], positions=i32(positions), rope=rope,
+                           q_norm=norm, k_norm=norm)
+
+    append(make(shared), [slot(prefix, i) for i in range(shared)], range(shared))
+    lengths = [0, 0, 0]
+    for news in ([60, 1, 33], [1, 1, 1], [1, 1, 1], [4, 0, 2]):
+        starts = np.concatenate([[0], np.cumsum(news)])
+        at = [(b, lengths[b] + i) for b in range(3) for i in range(news[b])]
+        q = append(make(int(starts[-1])), [slot(table[b], i) for b, i in at], [shared + i for _, i in at])
+        lengths = [a + b for a, b in zip(lengths, news)]
+        some = dict(q_starts=i32(starts), max_new=max(news)) if news != [1, 1, 1] else {}
+        out, lse = p.attend_kv(cache, q, i32(table), i32(lengths), prefix=i32(prefix), prefix_length=shared, want_lse=True, **some)
+        values = []
+        for which in ("k", "v"):
+            codes, scales = (cache.k_codes, cache.k_scales) if which == "k" else (cache.v_codes, cache.v_scales)
+            unpacked = oracle.unpack(codes.cpu().numpy().reshape(-1, codes.shape[-1]), bits).astype(np.float64)
+            values.append((unpacked * to_f64(scales).reshape(-1, 1)).reshape(pages, hkv, page, n))
+        check_attention(out, lse, attention(to_f64(q), theta, *values, table, lengths, starts, page, n ** -0.5, prefix, shared))
+    assert p.device_status() == 0
+
+
+# ---- refusals: no GPU is needed ------------------------------------------------------------------------------------------------
+def planless(n=128):
+    p = object.__new__(Plan)
+    p.n, p.L, p.device, p._h = n, n.bit_length() - 1, torch.device("cpu"), None
+    return p
+
+
+def host_cache(n=128, heads=2, page=16, bits=4, pages=3):
+    return KVCache.empty(pages, heads, n, page, bits, "cpu")
+
+
+def test_caches_that_are_refused():
+    c = host_cache()
+    parts = [c.k_codes, c.k_scales, c.v_codes, c.v_scales]
+    with pytest.raises(ValueError, match="bits"):
+        KVCache(*parts, 2)
+    for i in range(4):
+        bad = list(parts)
+        bad[i] = bad[i][:2]
+        with pytest.raises(ValueError, match="expected"):
+            KVCache(*bad, 4)
+        bad[i] = parts[i].transpose(1, 2).contiguous().transpose(1, 2)
+        with pytest.raises(ValueError, match="contiguous"):
+            KVCache(*bad, 4)
+        bad[i] = parts[i].to(torch.int16)
+        with pytest.raises(ValueError, match="expected"):
+            KVCache(*bad, 4)
+        bad[i] = parts[i][:1].expand(parts[i].shape)
+        with pytest.raises(ValueError, match="overlap"):
+            KVCache(*bad, 4)
+    for page in (8, 24, 512):
+        with pytest.raises(ValueError, match="page_size"):
+            host_cache(page=page)
+    assert host_cache(bits=8).head_dim == 128 and host_cache(pages=0).pages == 0
+
+
+def test_calls_that_are_refused(monkeypatch):
+    """Every bad argument raises before the library is reached (the cache lies on the host, which the plan takes for its device)."""
+    p, c = planless(), host_cache()
+    monkeypatch.setattr(binding, "_on", lambda *a: None)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    k, slots = bf(5, 2, 128), torch.zeros(5, dtype=torch.int64)
+    bad_append = [
+        dict(cache=host_cache(64)), dict(cache=None), dict(k=bf(5, 3, 128)), dict(k=bf(5, 2, 64)), dict(k=bf(5, 2, 256)[..., ::2]), dict(v=bf(4, 2, 128)), dict(v=k.float()),
+        dict(slots=slots[:4]), dict(slots=slots.int()), dict(q=bf(4, 4, 128)), dict(q=bf(5, 4, 128).float()), dict(q=bf(5, 4, 128), q_out=bf(5, 4, 128).float()),
+        dict(q=bf(5, 4, 128), q_out=bf(1, 4, 128).expand(5, 4, 128)), dict(q_norm=torch.ones(128)), dict(k_norm=torch.ones(64)), dict(k_norm=torch.ones(128).bfloat16()),
+        dict(positions=torch.zeros(5, dtype=torch.int32)), dict(rope=torch.zeros((4, 128))), dict(positions=torch.zeros(5), rope=torch.zeros((4, 128))),
+        dict(positions=torch.zeros(5, dtype=torch.int32), rope=torch.zeros((4, 24))), dict(positions=torch.zeros(5, dtype=torch.int32), rope=torch.zeros((4, 144))),
+        dict(positions=torch.zeros(5, dtype=torch.int32), rope=torch.zeros((0, 64)))]
+    for change in bad_append:
+        with pytest.raises((ValueError, TypeError)):
+            p.append_kv(**{**dict(cache=c, k=k, v=k, slots=slots), **change})
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        p.append_kv(c, k.half(), k.half(), slots)
+    for change in (dict(slots=slots.int()), dict(slots=slots.view(1, 5)), dict(dtype=torch.float16), dict(cache=host_cache(64))):
+        with pytest.raises((ValueError, TypeError)):
+            p.read_kv(**{**dict(cache=c, slots=slots), **change})
+    table, lengths = torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    bad_attend = [
+        dict(q=bf(2, 4, 128)), dict(q=bf(3, 3, 128)), dict(q=bf(3, 4, 64)), dict(q=bf(3, 4, 128).float()), dict(q=bf(3, 258, 128)), dict(lengths=lengths.long()),
+        dict(lengths=lengths[:2]), dict(block_table=table.long()), dict(block_table=table.t()), dict(block_table=table.view(-1)), dict(q_starts=torch.zeros(4, dtype=torch.int32)),
+        dict(q_starts=torch.zeros(3, dtype=torch.int32), max_new=1), dict(q_starts=torch.zeros(4, dtype=torch.int32), max_new=0), dict(prefix_length=3),
+        dict(prefix=table[0], prefix_length=65), dict(prefix=table[0], prefix_length=-1), dict(prefix=table[0].long(), prefix_length=1), dict(out=bf(3, 2, 128)),
+        dict(out=bf(3, 4, 128).float()), dict(out=bf(3, 1, 128).expand(3, 4, 128)), dict(cache=host_cache(64))]
+    for change in bad_attend:
+        with pytest.raises(ValueError):
+            p.attend_kv(**{**dict(cache=c, q=bf(3, 4, 128), block_table=table, lengths=lengths), **change})
+
+
+def test_tensors_on_another_device_are_refused():
+    p = planless()
+    p.device = torch.device("cuda", 0)
+    with pytest.raises(ValueError, match="cuda:0"):
+        p.attend_kv(host_cache(), torch.zeros((3, 4, 128), dtype=torch.bfloat16), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32))
+
+
+def test_the_c_entries_refuse_null_pointers():
+    L = binding.lib()
+    assert L.bfq_kv_append(None, None, None, 1, 0, None, None, None, None, None, None) == -1
+    assert L.bfq_kv_read(None, None, None, 1, 0, None, None, None) == -1
+    assert L.bfq_kv_attend(None, None, None, None, 0, None) == -1 and L.bfq_kv_attend_workspace(None, None, None) == 0
+
+
+@gpu
+def test_what_the_c_entries_refuse():
+    cache, _ = make_cache(2, 1, 64, 16, 4, 1)
+    q = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device=DEV)
+    fresh = Plan(64, DEV)
+    with pytest.raises(BfqError) as e:
+        fresh.attend_kv(cache, q, i32([[0]]), i32([1]))  # no angles yet
+    assert e.value.status == -7
+    p, _ = make_plan(64)
+    for scale in (float("nan"), float("inf")):
+        with pytest.raises(BfqError) as e:
+            p.attend_kv(cache, q, i32([[0]]), i32([1]), scale=scale)
+        assert e.value.status == -5
+    odd = torch.zeros(2 * 64 + 8, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(BfqError) as e:
+        p.attend_kv(cache, odd[1:65].view(1, 1, 64), i32([[0]]), i32([1]))
+    assert e.value.status == -4
+    with pytest.raises(BfqError) as e:
+        p.attend_kv(cache, odd.as_strided((2, 1, 64), (68, 64, 1)), i32([[0], [0]]), i32([1, 1]))
+    assert e.value.status == -5
+    small, _ = make_plan(256)
+    with pytest.raises(ValueError):
+        small.attend_kv(cache, q, i32([[0]]), i32([1]))
+    assert p.attend_kv(cache, q[:0], i32(np.zeros((0, 1))), i32([])).shape == (0, 1, 64)
