@@ -91,7 +91,7 @@ def _not_native(*args):
 
 class _Interpreted:
     """In the place of fast_calls: every call is done by the methods below."""
-    forward = forward_quant = inverse = staticmethod(_not_native)
+    forward = forward_quant = inverse = append_kv = read_kv = attend_kv = staticmethod(_not_native)
 
 
 _fast = _Interpreted  # set by lib()
@@ -513,6 +513,11 @@ class Plan:
         that queries and keys are normed per head (q_norm, k_norm fp32 [n]) and rotated by position (positions int32 [tokens], rope fp32
         [rows][dims]: cosines of dims / 2 frequencies, then sines; pairs (i, i + dims / 2), or (2 i, 2 i + 1) if interleaved), and all are rotated
         by Q.  Returns the queries as attend_kv takes them, bf16 (q_out, or a new tensor), or None without q."""
+        if q_out is None and type(cache) is KVCache:
+            done = _fast.append_kv(self._id, self.n, self._index, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, cache.bits, k, v, slots, q,
+                                   positions, rope, interleaved, q_norm, k_norm, eps)
+            if done is not None:
+                return None if done is True else (done if type(done) is not int else _check(done, "bfq_kv_append"))
         c = self._cache(cache)
         ck = self._head_rows(k, None, cache.heads, None, "k")
         tokens, xt = k.shape[0], _dt(k)
@@ -551,6 +556,10 @@ class Plan:
     def read_kv(self, cache: KVCache, slots: torch.Tensor, dtype=torch.bfloat16):
         """-> (k, v) [tokens][heads][n] of `dtype` (bf16 or fp32): the rows at slots int64 [tokens], dequantized and in the model's basis;
         zeros for a negative slot."""
+        if dtype is torch.bfloat16 and type(cache) is KVCache:
+            done = _fast.read_kv(self._id, self.n, self._index, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, cache.bits, slots)
+            if done is not None:
+                return done if type(done) is not int else _check(done, "bfq_kv_read")
         c = self._cache(cache)
         kind = _DTYPES.get(dtype)
         if kind is None:
@@ -572,6 +581,11 @@ class Plan:
         without them token b is sequence b's only one.  prefix int32 [pages], prefix_length: keys in front of every sequence, read once for
         all.  scale: 1 / sqrt(n) by default.  want_lse: (out, fp32 [tokens][heads] log sum exp of the scaled scores).  Rows of tokens behind
         the last sequence are not written."""
+        if out is None and not want_lse and type(cache) is KVCache:
+            done = _fast.attend_kv(self._id, self.n, self._index, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, cache.bits, q, block_table,
+                                   lengths, scale, q_starts, max_new, prefix, prefix_length)
+            if done is not None:
+                return done if type(done) is not int else _check(done, "bfq_kv_attend")
         c = self._cache(cache)
         cq = self._head_rows(q, None, None, torch.bfloat16, "q")
         tokens, heads = q.shape[0], q.shape[1]

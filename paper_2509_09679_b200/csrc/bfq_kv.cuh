@@ -32,84 +32,90 @@ struct Heads {
 
 // Where row (page, head, place) lies.  All products in 64 bits: a cache is larger than 4 GB.
 template <int ROW_BYTES>
-__device__ __forceinline__ uint8_t* codes_of(const Half& h, int heads, int page_shift, int64_t page, int head, int place) {
+__device__ __forceinline__ uint8_t* codes_of(const Half& h, int page_shift, int64_t page, int head, int place) {
     return h.codes + page * h.codes_page + ((static_cast<int64_t>(head) << page_shift) + place) * ROW_BYTES;
 }
-__device__ __forceinline__ uint16_t* scale_of(const Half& h, int heads, int page_shift, int64_t page, int head, int place) {
+__device__ __forceinline__ uint16_t* scale_of(const Half& h, int page_shift, int64_t page, int head, int place) {
     return h.scales + page * h.scales_page + (static_cast<int64_t>(head) << page_shift) + place;
 }
 
-// The butterfly (or its transpose) on rows of D elements, a row on D / E consecutive lanes of a warp, lane l with elements
-// E l .. E l + E - 1.  Stages of stride below E stay in a lane, the others are one exchange with the lane at that distance:
-// (a, b) -> (c a - s b, s a + c b), so a lane with the lower element of a pair takes c x - s x', one with the upper c x + s x'.
+// The butterfly (or, BACK, its transpose) on rows of D elements, a row on D / E consecutive lanes of a warp, lane l with elements
+// E l .. E l + E - 1, two in a 64-bit register.  Stages of stride below E stay in a lane, the others are one exchange with the lane at that
+// distance: (a, b) -> (c a - s b, s a + c b), so a lane with the lower element of a pair takes c x - s x', one with the upper c x + s x'.
 // The constants are the lane's own, read once and used for every row that the lane works on.
-template <int D, int E>
+template <int D, int E, bool BACK>
 struct Turn {
     static constexpr int kLanes = D / E;
     static constexpr int kStages = D == 64 ? 6 : 7;
     static constexpr int kIn = E == 2 ? 1 : (E == 4 ? 2 : 3);  // stages within a lane
     static_assert((D == 64 || D == 128) && (E == 2 || E == 4 || E == 8), "rows of a head");
-    float2 in[kIn][E / 2];             // (c, s) of the lane's pairs, in the order of their lower elements
-    float2 across[kStages - kIn][E];   // (c, -s or s) of each element's pair
+    float2 first[E / 2];                              // stage 0: (c, s) of the pair in each register
+    u64 in_c[kIn][E / 4 + 1], in_s[kIn][E / 4 + 1];   // stages 1 .. kIn - 1: of the pairs of registers (entry 0 and those behind E / 4: unused)
+    u64 c[kStages - kIn][E / 2], s[kStages - kIn][E / 2];
 
     __device__ __forceinline__ void load(const float2* tw, int lane) {
         const int base = (lane % kLanes) * E;
+        auto at = [&](int st, int i) {  // the constants of element i's pair
+            float2 v = load_plain(tw + st * (D / 2) + (((i >> (st + 1)) << st) | (i & ((1 << st) - 1))));
+            if (BACK) v.y = -v.y;
+            return v;
+        };
 #pragma unroll
-        for (int st = 0; st < kStages; ++st) {
-            const float2* t = tw + st * (D / 2);
+        for (int r = 0; r < E / 2; ++r) first[r] = at(0, base + 2 * r);
+#pragma unroll
+        for (int st = 1; st < kStages; ++st) {
             const int h = 1 << st;
-            if (st < kIn) {
-                int p = 0;
+            int n = 0;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if ((e & h) == 0) {
-                        const int i = base + e;
-                        in[st][p++] = load_plain(t + (((i >> (st + 1)) << st) | (i & (h - 1))));
-                    }
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int i = base + e;
-                    float2 c = load_plain(t + (((i >> (st + 1)) << st) | (i & (h - 1))));
-                    if ((i & h) == 0) c.y = -c.y;
-                    across[st - kIn][e] = c;
+            for (int r = 0; r < E / 2; ++r) {
+                const int i = base + 2 * r;
+                if (st < kIn && ((2 * r) & h) != 0) continue;
+                float2 a = at(st, i), b = at(st, i + 1);
+                if (st < kIn) {
+                    in_c[st][n] = pack2(a.x, b.x), in_s[st][n++] = pack2(a.y, b.y);
+                } else {
+                    if ((i & h) == 0) a.y = -a.y, b.y = -b.y;
+                    c[st - kIn][r] = pack2(a.x, b.x), s[st - kIn][r] = pack2(a.y, b.y);
                 }
             }
         }
     }
-    template <bool BACK>
-    __device__ __forceinline__ void stage_in(float (&x)[E], int st) const {
+    __device__ __forceinline__ void stage(u64 (&x)[E / 2], int st) const {
         const int h = 1 << st;
-        int p = 0;
+        if (st == 0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if ((e & h) == 0) {
-                const float2 c = in[st][p++];
-                const float s = BACK ? -c.y : c.y, a = x[e], b = x[e + h];
-                x[e] = fmaf(c.x, a, -s * b);
-                x[e + h] = fmaf(s, a, c.x * b);
+            for (int r = 0; r < E / 2; ++r) {
+                float a, b;
+                unpack2(x[r], a, b);
+                x[r] = pack2(fmaf(first[r].x, a, -first[r].y * b), fmaf(first[r].y, a, first[r].x * b));
             }
-    }
-    template <bool BACK>
-    __device__ __forceinline__ void stage_across(float (&x)[E], int st) const {
+        } else if (st < kIn) {
+            int n = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float2 c = across[st - kIn][e];
-            const float o = __shfl_xor_sync(0xFFFFFFFFu, x[e], (1 << st) / E);
-            x[e] = fmaf(c.x, x[e], (BACK ? -c.y : c.y) * o);
+            for (int r = 0; r < E / 2; ++r) {
+                if (((2 * r) & h) != 0) continue;
+                const u64 cc = in_c[st][n], ss = in_s[st][n++], a = x[r], b = x[r + h / 2];
+                x[r] = sub2(mul2(cc, a), mul2(ss, b));
+                x[r + h / 2] = fma2(ss, a, mul2(cc, b));
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < E / 2; ++r) {
+                uint32_t lo, hi;
+                unpack2u(x[r], lo, hi);
+                lo = __shfl_xor_sync(0xFFFFFFFFu, lo, h / E), hi = __shfl_xor_sync(0xFFFFFFFFu, hi, h / E);
+                x[r] = fma2(c[st - kIn][r], x[r], mul2(s[st - kIn][r], pack2u(lo, hi)));
+            }
         }
     }
-    __device__ __forceinline__ void forward(float (&x)[E]) const {
+    __device__ __forceinline__ void apply(float (&v)[E]) const {
+        u64 x[E / 2];
 #pragma unroll
-        for (int st = 0; st < kIn; ++st) stage_in<false>(x, st);
+        for (int r = 0; r < E / 2; ++r) x[r] = pack2(v[2 * r], v[2 * r + 1]);
 #pragma unroll
-        for (int st = kIn; st < kStages; ++st) stage_across<false>(x, st);
-    }
-    __device__ __forceinline__ void inverse(float (&x)[E]) const {
+        for (int st = 0; st < kStages; ++st) stage(x, BACK ? kStages - 1 - st : st);
 #pragma unroll
-        for (int st = kStages - 1; st >= kIn; --st) stage_across<true>(x, st);
-#pragma unroll
-        for (int st = kIn - 1; st >= 0; --st) stage_in<true>(x, st);
+        for (int r = 0; r < E / 2; ++r) unpack2(x[r], v[2 * r], v[2 * r + 1]);
     }
 };
 

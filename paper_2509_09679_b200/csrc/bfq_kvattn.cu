@@ -2,10 +2,12 @@
 //
 //     out = Q^T sum_j softmax_j(scale q . (s_j k_j)) (u_j v_j),  k, v the codes of the rotated rows, s, u their fp16 scales, q rotated by Q.
 //
-// The codes are exact in bf16, so both products run on the tensor cores without the scales: scores q . k_j times scale s_j in fp32,
-// probabilities times u_j rounded once to bf16 (2^-9 of each, independent of its neighbours).  Softmax is taken in one pass over the keys:
-// m is a reference that is at most 8 (a factor of 256) below the largest score so far, so that it, the sum and the products change only
-// when a score passes it by more than that.
+// The codes are exact in fp16, so both products run on the tensor cores without the scales: a row of q is taken times a power of two
+// that puts its largest element in [2^10, 2^11) (elements down to 2^-24 of that stay exact), q . k_j is summed in fp32 and multiplied by
+// s_j; probabilities times u_j are rounded once to fp16 (2^-11 of each, independent of its neighbours; bf16 would cost more than the output's own
+// rounding), on a power of two that follows the largest u so far.  Softmax is taken in one pass over the keys: m is a reference that is
+// at most 8 (a factor of 256) below the largest score so far, so that it, the sum and the products change only when a score passes it by more
+// than that.
 //
 // A CTA of four warps takes units of 64 keys, 16 keys to a warp, through a ring of stages that cp.async fills some units ahead
 // (16-byte chunks, chunk i of a unit at place i ^ (i / 8 mod 8): the reads below hit every bank once).  mma.m16n8k16: the 16 rows are
@@ -43,7 +45,7 @@ __device__ __forceinline__ void copies_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -65,23 +67,35 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at) {
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Codes i and i + 4 of a word of 8 codes of 4 bits (lower half, upper half), i < 4, as a bf16 pair: the code's bits, its top one
-// inverted, are the low mantissa bits of 128 .. 143 = 136 + code.
-__device__ __forceinline__ uint32_t pair4(uint32_t w, int i) { return sub_pair(((w >> (4 * i)) & 0x000F000Fu) ^ 0x43084308u, 0x43084308u); }
-// Codes i and i + 2 of a word of 4 codes of 8 bits, i < 2: the low seven bits on top of 128, less 128 or (sign) 256.
+__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Codes of a word as exact fp16 pairs (one of the lower half, one of the upper): the code's bits, its top one inverted, lie in the mantissa of
+// 1024 .. 2047.  4 bits: codes i and i + 4, i < 4; the odd ones lie four places up there, 1152 + 16 code.  8 bits: codes i and i + 2, i < 2.
+__device__ __forceinline__ uint32_t pair4(uint32_t w, int i) {
+    if (i >= 2) w >>= 8;
+    return i & 1 ? fma_pair((w & 0x00F000F0u) ^ 0x64806480u, 0x2C002C00u, 0xD480D480u)  // / 16 - 72
+                 : sub_pair((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);             // - 1032
+}
 __device__ __forceinline__ uint32_t pair8(uint32_t w, int i) {
-    w >>= 8 * i;
-    return sub_pair((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u);
+    if (i) w >>= 8;
+    return sub_pair((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);  // - 1152
 }
 
 // Where in the numbering of units a role of the CTA is.
@@ -178,15 +192,15 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
                 const int64_t found = key < ahead.tile.keys ? page_of(key) : -1, page = found < 0 ? 0 : found;
                 const bool there = found >= 0;  // else zeros
                 const uint32_t dst = stage + 16 * (i16 ^ ((i16 >> 3) & 7));
-                copy16(dst, codes_of<S::kRow>(p.cache.k, heads, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
-                copy16(dst + kUnit * S::kRow, codes_of<S::kRow>(p.cache.v, heads, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
+                copy16(dst, codes_of<S::kRow>(p.cache.k, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
+                copy16(dst + kUnit * S::kRow, codes_of<S::kRow>(p.cache.v, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
             }
             if (tid < 2 * kUnit / 8) {
                 const int key = key0 + 8 * (tid % (kUnit / 8));
                 const bool values = tid >= kUnit / 8;
                 const int64_t found = key < ahead.tile.keys ? page_of(key) : -1, page = found < 0 ? 0 : found;
                 const bool there = found >= 0;
-                copy16(stage + S::kScales + 16 * tid, scale_of(values ? p.cache.v : p.cache.k, heads, p.cache.page_shift, page, ahead.head, key & mask), there);
+                copy16(stage + S::kScales + 16 * tid, scale_of(values ? p.cache.v : p.cache.k, p.cache.page_shift, page, ahead.head, key & mask), there);
             }
             ahead.next(p);
         }
@@ -198,7 +212,10 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
     // ---- a pair's state: fragments of the queries, reference, sums and products -------------------------------------------
     uint32_t qa[kSteps][4];
     float m[2], l[2], o[kTilesD][4];
-    int limit[2];  // keys of rows g and g + 8
+    float row_scale_log2[2];  // softmax scale * log2 e over the row's power of two
+    float u_top, u_unit;      // power of two that no u so far passes; 128 / u_top: probabilities (at most 2^8) times u stay below 2^15
+    int limit[2];             // keys of rows g and g + 8
+    bool two;                 // there are rows 8 and up
     auto open = [&]() {
         const Tile& tl = now.tile;
 #pragma unroll
@@ -213,9 +230,16 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
                 const uint4 v = there ? load_plain(at + c) : make_uint4(0, 0, 0, 0);
                 w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
             }
-            auto pair = [&](int i, int j) {  // elements i and j (both even or both odd)
-                return (i & 1) ? __byte_perm(w[i / 2], w[j / 2], 0x7632) : __byte_perm(w[i / 2], w[j / 2], 0x5410);
-            };
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const int field = 264 - static_cast<int>(__float_as_uint(top) >> 23), power = field > 253 ? 253 : field;  // exponent of the factor
+            const float up = __uint_as_float(uint32_t(power) << 23);
+            row_scale_log2[half] = p.scale_log2 * __uint_as_float(uint32_t(254 - power) << 23);
+            auto element = [&](int i) { return up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
+            auto pair = [&](int i, int j) { return half_pair(element(i), element(j)); };
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 if constexpr (BITS == 4) {
@@ -229,6 +253,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
             const int own = tl.last0 + row / p.group + 1;
             limit[half] = there ? (own < tl.keys ? own : tl.keys) : 0;
         }
+        two = tl.rows > 8, u_top = 0.f, u_unit = 0.f;
 #pragma unroll
         for (int i = 0; i < kTilesD; ++i)
 #pragma unroll
@@ -255,7 +280,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
             const float safe = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) sum += ml[w].y * exp2_fast(ml[w].x - safe);
-            f[half] = exp2_fast(m[half] - safe);
+            f[half] = exp2_fast(m[half] - safe) * (u_top * (1.f / 128.f));
             if (warp == 0 && t == 0 && g + 8 * half < now.tile.rows) p.sums[entry * kTileRows + g + 8 * half] = make_float2(top, sum);
         }
         // d of accumulator i, column 2 t + j: see the values' order below
@@ -332,35 +357,54 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int key = key0 + 8 * j + 2 * t + c;
-                const float f = half_value(static_cast<uint16_t>(ks >> (16 * c))) * p.scale_log2;
+                const float f = half_value(static_cast<uint16_t>(ks >> (16 * c)));
                 u[j][c] = key < now.tile.keys ? half_value(static_cast<uint16_t>(vs >> (16 * c))) : 0.f;
-                s[j][c] = key < limit[0] ? s[j][c] * f : -INFINITY;
-                s[j][2 + c] = key < limit[1] ? s[j][2 + c] * f : -INFINITY;
-                over |= s[j][c] > m[0] + 8.f || s[j][2 + c] > m[1] + 8.f;
+                over |= u[j][c] > u_top;
+                s[j][c] = key < limit[0] ? s[j][c] * f * row_scale_log2[0] : -INFINITY;
+                over |= s[j][c] > m[0] + 8.f;
+                if (two) {
+                    s[j][2 + c] = key < limit[1] ? s[j][2 + c] * f * row_scale_log2[1] : -INFINITY;
+                    over |= s[j][2 + c] > m[1] + 8.f;
+                }
             }
         }
         if (__any_sync(0xFFFFFFFFu, over)) {
+            float most = fmaxf(fmaxf(u[0][0], u[0][1]), fmaxf(u[1][0], u[1][1]));
+            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+            float less = 1.f;  // on the products
+            if (most > u_top) {
+                const float top = __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u);  // above it
+                less = u_top / top, u_top = top, u_unit = 128.f / top;
+            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                float top = fmaxf(fmaxf(s[0][2 * half], s[0][2 * half + 1]), fmaxf(s[1][2 * half], s[1][2 * half + 1]));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                top = fmaxf(top, m[half]);
-                const float f = top == -INFINITY ? 1.f : exp2_fast(m[half] - top);
-                m[half] = top, l[half] *= f;
+                float f = 1.f;
+                if (half == 0 || two) {
+                    float top = fmaxf(fmaxf(s[0][2 * half], s[0][2 * half + 1]), fmaxf(s[1][2 * half], s[1][2 * half + 1]));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                    top = fmaxf(top, m[half]);
+                    f = top == -INFINITY ? 1.f : exp2_fast(m[half] - top);
+                    m[half] = top, l[half] *= f;
+                }
+                f *= less;
 #pragma unroll
                 for (int i = 0; i < kTilesD; ++i) o[i][2 * half] *= f, o[i][2 * half + 1] *= f;
             }
         }
-        uint32_t pa[4];
+        uint32_t pa[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) u[j][0] *= u_unit, u[j][1] *= u_unit;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
+            if (half == 1 && !two) break;
             const float ref = m[half] == -INFINITY ? 0.f : m[half];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float a = exp2_fast(s[j][2 * half] - ref), b = exp2_fast(s[j][2 * half + 1] - ref);
                 l[half] += a + b;
-                pa[half + 2 * j] = bf16_pair(a * u[j][0], b * u[j][1]);
+                pa[half + 2 * j] = half_pair(a * u[j][0], b * u[j][1]);
             }
         }
         // ---- values: matrix (8 keys) x (a 16-byte chunk), its 16-bit units across the lanes
@@ -413,7 +457,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
         }
         b = lo, place = token - first_token(p, b);
     }
-    Turn<D, kE> turn;
+    Turn<D, kE, true> turn;
     turn.load(p.tw, lane);
     float m = -INFINITY, l = 0.f, o[kE];
 #pragma unroll
@@ -452,7 +496,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     const float f = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
     for (int e = 0; e < kE; ++e) o[e] *= f;
-    turn.inverse(o);
+    turn.apply(o);
     uint8_t* out = const_cast<uint8_t*>(p.out.data) + (token * p.out.token + head * p.out.head + kE * lane) * 2;
     if constexpr (kE == 4) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]));
     else *reinterpret_cast<uint32_t*>(out) = bf16_pair(o[0], o[1]);

@@ -33,77 +33,137 @@ struct AppendParams {
     int* status;
 };
 
+// 8 elements of a row as they lie in memory, and as numbers
 template <bool F32>
-__device__ __forceinline__ void load8(const uint8_t* at, float (&x)[8]) {
-    if constexpr (F32) {
-        const float4 a = load_plain(reinterpret_cast<const float4*>(at)), b = load_plain(reinterpret_cast<const float4*>(at) + 1);
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-        const uint4 a = load_plain(reinterpret_cast<const uint4*>(at));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Raw {
+    uint4 w[F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const uint8_t* at) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) w[i] = load_plain(reinterpret_cast<const uint4*>(at) + i);
     }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        if constexpr (F32) {
+            const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i]);
+        } else {
+            const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+        }
+    }
+};
+__device__ __forceinline__ void load_floats8(const float* at, float (&x)[8]) {
+    Raw<true> r;
+    r.load(reinterpret_cast<const uint8_t*>(at));
+    r.get(x);
 }
 
-// 8 elements -> codes of 4 bits (one word) or 8 (two)
+// 8 elements -> codes of 4 bits (one word) or 8 (two): quant1's codes (clip(x inv), then round to nearest even), the rounding by an addition
+// that leaves the integer in the low bits
 template <int BITS>
 __device__ __forceinline__ void codes8(const float (&x)[8], float inv, uint32_t (&w)[BITS / 4]) {
-    constexpr int kTop = (1 << (BITS - 1)) - 1;
+    constexpr float kTop = (1 << (BITS - 1)) - 1;
+    uint32_t c[8];
 #pragma unroll
-    for (int i = 0; i < BITS / 4; ++i) w[i] = 0;
+    for (int e = 0; e < 8; ++e) c[e] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(x[e], inv), -kTop - 1.f), kTop), 12582912.f));
+    if constexpr (BITS == 4) {
+        w[0] = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t c = static_cast<uint32_t>(quant1(x[e], inv, -kTop - 1, kTop)) & ((1u << BITS) - 1);
-        w[e * BITS / 32] |= c << (e * BITS % 32);
+        for (int e = 0; e < 8; ++e) w[0] |= (c[e] & 15u) << (4 * e);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
     }
 }
 
+// The rows of a CTA are consecutive (a token's rows share its position's angles and its slot), kRowThreads / (D / 8) at a time.  A lane's row
+// by token and row of the token, without a division at each step.
+struct RowAt {
+    int64_t token, left;  // rows from this one to the CTA's last (<= 0: none)
+    int r;                // of the token's `heads`
+    __device__ __forceinline__ void start(int64_t rows, int heads, int rows_per_step) {
+        const int64_t steps = (rows + rows_per_step - 1) / rows_per_step, per = (steps + gridDim.x - 1) / gridDim.x * rows_per_step;
+        const int64_t from = per * blockIdx.x, to = from + per < rows ? from + per : rows, row = from + threadIdx.x / (kRowThreads / rows_per_step);
+        left = to - row, token = row / heads, r = static_cast<int>(row - token * heads);
+    }
+    __device__ __forceinline__ void next(int heads, int rows_per_step) {
+        left -= rows_per_step;
+        r += rows_per_step;
+        while (r >= heads) r -= heads, ++token;
+    }
+    __device__ __forceinline__ bool there() const { return left > 0; }
+};
+
+// Of a row's token: what the row after next needs is on its way while this one is worked on.
 template <int D, bool F32, int BITS>
 __global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p) {
-    constexpr int kLanes = D / 8, kRowsPerWarp = 32 / kLanes;
+    constexpr int kLanes = D / 8, kStep = kRowThreads / kLanes;
     grid_dep_wait();
     const int lane = threadIdx.x & 31, l = lane % kLanes;
-    Turn<D, 8> turn;
+    const int heads = p.q.heads + 2 * p.cache.heads;  // rows of a token: queries, keys, values
+    auto kind_of = [&](const RowAt& a) { return a.r < p.q.heads ? 0 : (a.r < p.q.heads + p.cache.heads ? 1 : 2); };
+    auto head_of = [&](const RowAt& a, int kind) { return a.r - (kind == 0 ? 0 : (kind == 1 ? p.q.heads : p.q.heads + p.cache.heads)); };
+    auto fetch = [&](const RowAt& a, Raw<F32>& raw) {
+        if (!a.there()) return;
+        const int kind = kind_of(a), head = head_of(a, kind);
+        const uint8_t* data = kind == 0 ? p.q.data : (kind == 1 ? p.k.data : p.v.data);
+        const int64_t st = kind == 0 ? p.q.token : (kind == 1 ? p.k.token : p.v.token), sh = kind == 0 ? p.q.head : (kind == 1 ? p.k.head : p.v.head);
+        raw.load(data + (a.token * st + head * sh + 8 * l) * (F32 ? 4 : 2));
+    };
+    RowAt at, ahead;
+    at.start(p.tokens * heads, heads, kStep);
+    Raw<F32> raw, raw_next;
+    fetch(at, raw);
+    int position = at.there() && p.positions != nullptr ? load_plain(p.positions + at.token) : 0, position_next = 0;
+    int64_t slot = at.there() ? load_plain(p.slots + at.token) : -1, slot_next = -1;
+    Turn<D, 8, false> turn;
     turn.load(p.tw, lane);
-    const int heads = p.q.heads + 2 * p.cache.heads;  // of a token, queries first
-    const int64_t rows = p.tokens * heads;
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kRowThreads / 32);
-    for (int64_t at = (static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRowsPerWarp; at < rows; at += warps * kRowsPerWarp) {
-        const int64_t row = at + lane / kLanes;
-        const bool there = row < rows;
-        const int64_t token = there ? row / heads : 0;
-        const int r = there ? static_cast<int>(row - token * heads) : 0;
-        const bool is_q = r < p.q.heads, is_k = !is_q && r < p.q.heads + p.cache.heads;
-        const int head = is_q ? r : (is_k ? r - p.q.heads : r - p.q.heads - p.cache.heads);
-        const Heads& from = is_q ? p.q : (is_k ? p.k : p.v);
-        float x[8];
-        load8<F32>(from.data + (token * from.token + head * from.head + 8 * l) * (F32 ? 4 : 2), x);
-        const float* norm = is_q ? p.q_norm : (is_k ? p.k_norm : nullptr);
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-#pragma unroll
-        for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        if (norm != nullptr) {
-            const float f = 1.f / sqrtf(sum * (1.f / D) + p.eps);
-            const float4 a = load_plain(reinterpret_cast<const float4*>(norm + 8 * l)), b = load_plain(reinterpret_cast<const float4*>(norm + 8 * l + 4));
-            const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= f * w[e];
-        }
-        if (p.positions != nullptr) {
-            const bool turned = (is_q || is_k) && 8 * l < p.rope_dims;
-            int64_t pos = there ? load_plain(p.positions + token) : 0;
-            if (pos < 0 || pos >= p.rope_rows) {
-                if (there) atomicExch(p.status, kBadIndex);
-                pos = 0;
+    for (; __any_sync(0xFFFFFFFFu, at.there()); at = ahead, raw = raw_next, position = position_next, slot = slot_next) {
+        const bool there = at.there();
+        const int kind = kind_of(at), head = head_of(at, kind);
+        const bool turned = there && p.positions != nullptr && kind < 2 && 8 * l < p.rope_dims, upper = !p.interleaved && 16 * l >= p.rope_dims;
+        float cs[8], sn[8];
+        if (turned) {
+            const bool fine = position >= 0 && position < p.rope_rows;
+            if (!fine) atomicExch(p.status, kBadIndex);
+            const float* table = p.rope + (fine ? position : 0) * int64_t(p.rope_dims);
+            if (p.interleaved) {
+                const float4 c = load_plain(reinterpret_cast<const float4*>(table + 4 * l)), s = load_plain(reinterpret_cast<const float4*>(table + p.rope_dims / 2 + 4 * l));
+                cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
+            } else {
+                const float* t = table + 8 * l - (upper ? p.rope_dims / 2 : 0);
+                load_floats8(t, cs), load_floats8(t + p.rope_dims / 2, sn);
             }
-            const float* table = p.rope + pos * p.rope_dims;
+        }
+        ahead = at;
+        ahead.next(heads, kStep);
+        fetch(ahead, raw_next);
+        if (ahead.there()) {
+            slot_next = load_plain(p.slots + ahead.token);
+            if (p.positions != nullptr) position_next = load_plain(p.positions + ahead.token);
+        }
+        float x[8];
+        raw.get(x);
+        const float* norm = kind == 0 ? p.q_norm : (kind == 1 ? p.k_norm : nullptr);
+        if (__any_sync(0xFFFFFFFFu, norm != nullptr)) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            if (norm != nullptr) {
+                const float f = 1.f / sqrtf(sum * (1.f / D) + p.eps);
+                float w[8];
+                load_floats8(norm + 8 * l, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= f * w[e];
+            }
+        }
+        if (__any_sync(0xFFFFFFFFu, turned)) {
             if (p.interleaved) {
                 if (turned) {
-                    const float4 c = load_plain(reinterpret_cast<const float4*>(table + 4 * l)), s = load_plain(reinterpret_cast<const float4*>(table + p.rope_dims / 2 + 4 * l));
-                    const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float a = x[2 * i], b = x[2 * i + 1];
@@ -112,50 +172,42 @@ __global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p) {
                     }
                 }
             } else {
-                const int half = p.rope_dims / 16;  // lanes of one half
-                const bool upper = l >= half;
-                const int other = (lane - l) + (turned ? (upper ? l - half : l + half) : l);
-                float o[8];
+                const int half = p.rope_dims / 16, other = turned ? (upper ? lane - half : lane + half) : lane;  // `half` lanes have a half
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(0xFFFFFFFFu, x[e], other);
-                if (turned) {
-                    const float* t = table + 8 * (upper ? l - half : l);
-                    float cs[8], sn[8];
-                    load8<true>(reinterpret_cast<const uint8_t*>(t), cs);
-                    load8<true>(reinterpret_cast<const uint8_t*>(t + p.rope_dims / 2), sn);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], cs[e], (upper ? o[e] : -o[e]) * sn[e]);
+                for (int e = 0; e < 8; ++e) {
+                    const float o = __shfl_sync(0xFFFFFFFFu, x[e], other);
+                    if (turned) x[e] = fmaf(x[e], cs[e], (upper ? o : -o) * sn[e]);
                 }
             }
         }
-        turn.forward(x);
+        turn.apply(x);
         float top = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         if (!there) continue;
-        if (is_q) {
-            uint4 v = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
-            *reinterpret_cast<uint4*>(const_cast<uint8_t*>(p.q_out.data) + (token * p.q_out.token + head * p.q_out.head + 8 * l) * 2) = v;
+        if (kind == 0) {
+            const uint4 v = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+            *reinterpret_cast<uint4*>(const_cast<uint8_t*>(p.q_out.data) + (at.token * p.q_out.token + head * p.q_out.head + 8 * l) * 2) = v;
             continue;
         }
-        const int64_t slot = load_plain(p.slots + token), page = slot >> p.cache.page_shift;
+        const int64_t page = slot >> p.cache.page_shift;
         if (slot < 0) continue;
         if (page >= p.cache.pages) {
             atomicExch(p.status, kBadIndex);
             continue;
         }
         const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
-        const Half& to = is_k ? p.cache.k : p.cache.v;
+        const Half to = kind == 1 ? p.cache.k : p.cache.v;
         float inv;
         const uint16_t scale = row_scale(top, (1 << (BITS - 1)) - 1, &inv);
         uint32_t w[BITS / 4];
         codes8<BITS>(x, inv, w);
-        uint8_t* c = codes_of<D * BITS / 8>(to, p.cache.heads, p.cache.page_shift, page, head, place) + l * BITS;
+        uint8_t* c = codes_of<D * BITS / 8>(to, p.cache.page_shift, page, head, place) + l * BITS;
         if constexpr (BITS == 4) *reinterpret_cast<uint32_t*>(c) = w[0];
         else *reinterpret_cast<uint2*>(c) = make_uint2(w[0], w[1]);
-        if (l == 0) *scale_of(to, p.cache.heads, p.cache.page_shift, page, head, place) = scale;
+        if (l == 0) *scale_of(to, p.cache.page_shift, page, head, place) = scale;
     }
 }
 
@@ -170,46 +222,59 @@ struct ReadParams {
 
 template <int D, bool F32, int BITS>
 __global__ void __launch_bounds__(kRowThreads) k_read(const ReadParams p) {
-    constexpr int kLanes = D / 8, kRowsPerWarp = 32 / kLanes;
+    constexpr int kLanes = D / 8, kStep = kRowThreads / kLanes;
     grid_dep_wait();
     const int lane = threadIdx.x & 31, l = lane % kLanes;
-    Turn<D, 8> turn;
-    turn.load(p.tw, lane);
-    const int heads = 2 * p.cache.heads;
-    const int64_t rows = p.tokens * heads;
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kRowThreads / 32);
-    for (int64_t at = (static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRowsPerWarp; at < rows; at += warps * kRowsPerWarp) {
-        const int64_t row = at + lane / kLanes;
-        const bool there = row < rows;
-        const int64_t token = there ? row / heads : 0;
-        const int r = there ? static_cast<int>(row - token * heads) : 0;
-        const bool is_k = r < p.cache.heads;
-        const int head = is_k ? r : r - p.cache.heads;
-        const int64_t slot = there ? load_plain(p.slots + token) : -1, page = slot >> p.cache.page_shift;
-        float x[8];
-        if (slot < 0 || page >= p.cache.pages) {
-            if (slot >= 0) atomicExch(p.status, kBadIndex);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        } else {
-            const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
-            const Half& from = is_k ? p.cache.k : p.cache.v;
-            const uint8_t* c = codes_of<D * BITS / 8>(from, p.cache.heads, p.cache.page_shift, page, head, place) + l * BITS;
-            const float s = half_value(*static_cast<volatile const uint16_t*>(scale_of(from, p.cache.heads, p.cache.page_shift, page, head, place)));
-            uint32_t w[2];
-            if constexpr (BITS == 4) {
-                w[0] = load_plain(reinterpret_cast<const uint32_t*>(c));
-            } else {
-                const uint2 u = load_plain(reinterpret_cast<const uint2*>(c));
-                w[0] = u.x, w[1] = u.y;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = s * static_cast<float>(static_cast<int32_t>(w[e * BITS / 32] << (32 - BITS - e * BITS % 32)) >> (32 - BITS));
+    const int heads = 2 * p.cache.heads;  // rows of a token: keys, values
+    struct Codes {
+        uint32_t w[2];
+        uint16_t scale;
+    };
+    auto slot_of = [&](const RowAt& a) { return a.there() ? load_plain(p.slots + a.token) : int64_t(-1); };
+    auto fetch = [&](const RowAt& a, int64_t slot) {
+        Codes c{};
+        const int64_t page = slot >> p.cache.page_shift;
+        if (slot < 0) return c;
+        if (page >= p.cache.pages) {
+            atomicExch(p.status, kBadIndex);
+            return c;
         }
-        turn.inverse(x);
-        if (!there) continue;
-        uint8_t* out = (is_k ? p.k : p.v) + ((token * p.cache.heads + head) * D + 8 * l) * (F32 ? 4 : 2);
+        const bool is_k = a.r < p.cache.heads;
+        const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1), head = is_k ? a.r : a.r - p.cache.heads;
+        const Half from = is_k ? p.cache.k : p.cache.v;
+        const uint8_t* at = codes_of<D * BITS / 8>(from, p.cache.page_shift, page, head, place) + l * BITS;
+        if constexpr (BITS == 4) {
+            c.w[0] = load_plain(reinterpret_cast<const uint32_t*>(at));
+        } else {
+            const uint2 u = load_plain(reinterpret_cast<const uint2*>(at));
+            c.w[0] = u.x, c.w[1] = u.y;
+        }
+        c.scale = *static_cast<volatile const uint16_t*>(scale_of(from, p.cache.page_shift, page, head, place));
+        return c;
+    };
+    RowAt at, ahead;
+    at.start(p.tokens * heads, heads, kStep);
+    ahead = at;
+    ahead.next(heads, kStep);
+    Codes codes = fetch(at, slot_of(at)), codes_next{};
+    int64_t slot = slot_of(ahead);  // of the next row
+    Turn<D, 8, true> turn;
+    turn.load(p.tw, lane);
+    for (; __any_sync(0xFFFFFFFFu, at.there()); codes = codes_next) {
+        codes_next = fetch(ahead, slot);
+        const RowAt now = at;
+        at = ahead;
+        ahead.next(heads, kStep);
+        slot = slot_of(ahead);
+        const float s = half_value(codes.scale);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = s * static_cast<float>(static_cast<int32_t>(codes.w[e * BITS / 32] << (32 - BITS - e * BITS % 32)) >> (32 - BITS));
+        turn.apply(x);
+        if (!now.there()) continue;
+        const bool is_k = now.r < p.cache.heads;
+        uint8_t* out = (is_k ? p.k : p.v) + ((now.token * p.cache.heads + (is_k ? now.r : now.r - p.cache.heads)) * D + 8 * l) * (F32 ? 4 : 2);
         if constexpr (F32) {
             reinterpret_cast<float4*>(out)[0] = make_float4(x[0], x[1], x[2], x[3]);
             reinterpret_cast<float4*>(out)[1] = make_float4(x[4], x[5], x[6], x[7]);
