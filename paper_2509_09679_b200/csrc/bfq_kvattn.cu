@@ -25,15 +25,15 @@ constexpr int kWarps = 4, kAttendThreads = 32 * kWarps;
 template <int D, int BITS>
 struct Stage {
     static constexpr int kRow = D * BITS / 8;             // bytes of a row's codes
-    static constexpr int kChunks = kUnit * kRow / 16;     // of a unit's keys (and as many of its values)
-    static constexpr int kScales = 2 * kUnit * kRow;      // keys' scales behind both, then the values'
-    static constexpr int kBytes = kScales + 4 * kUnit;
+    static constexpr int kChunks = kFewUnit * kRow / 16;     // of a unit's keys (and as many of its values)
+    static constexpr int kScales = 2 * kFewUnit * kRow;      // keys' scales behind both, then the values'
+    static constexpr int kBytes = kScales + 4 * kFewUnit;
     static constexpr int kCount = kBytes > 12000 ? 4 : 6;
 };
-constexpr int kMergeRows = 2 * kTileRows;
+constexpr int kMergeRows = 2 * kFewRows;
 template <int D, int BITS>
 constexpr size_t attend_smem() {
-    return size_t(Stage<D, BITS>::kCount) * Stage<D, BITS>::kBytes + sizeof(float) * kMergeRows * (D + 4) + 4 * kTileRows * sizeof(float2);
+    return size_t(Stage<D, BITS>::kCount) * Stage<D, BITS>::kBytes + sizeof(float) * kMergeRows * (D + 4) + 4 * kFewRows * sizeof(float2);
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
@@ -67,59 +67,6 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at) {
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// Codes of a word as exact fp16 pairs (one of the lower half, one of the upper): the code's bits, its top one inverted, lie in the mantissa of
-// 1024 .. 2047.  4 bits: codes i and i + 4, i < 4; the odd ones lie four places up there, 1152 + 16 code.  8 bits: codes i and i + 2, i < 2.
-__device__ __forceinline__ uint32_t pair4(uint32_t w, int i) {
-    if (i >= 2) w >>= 8;
-    return i & 1 ? fma_pair((w & 0x00F000F0u) ^ 0x64806480u, 0x2C002C00u, 0xD480D480u)  // / 16 - 72
-                 : sub_pair((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);             // - 1032
-}
-__device__ __forceinline__ uint32_t pair8(uint32_t w, int i) {
-    if (i) w >>= 8;
-    return sub_pair((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);  // - 1152
-}
-
-// Where in the numbering of units a role of the CTA is.
-struct Walk {
-    int entry, head, unit, units;  // unit of units within the pair
-    Tile tile;
-    __device__ __forceinline__ void enter(const AttendParams& p, int e) {  // the first entry from e on that has units
-        entry = e;
-        const int last = p.entries();
-        for (units = 0; entry < last; ++entry) {
-            tile = tile_of(p, entry);
-            units = units_of(tile);
-            if (units > 0) break;
-        }
-    }
-    __device__ __forceinline__ void next(const AttendParams& p) {
-        if (++unit < units) return;
-        unit = 0;
-        if (++head < p.cache.heads) return;
-        head = 0;
-        enter(p, entry + 1);
-    }
-};
-
 template <int D, int BITS>
 __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p) {
     using S = Stage<D, BITS>;
@@ -132,77 +79,38 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     grid_dep_wait();
 
-    // ---- this CTA's run of units -----------------------------------------------------------------------------------------
-    const int entries = p.entries(), heads = p.cache.heads;
-    const int each = (entries + kAttendThreads - 1) / kAttendThreads;
-    long long mine = 0;
-    for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_of(tile_of(p, e));
-    long long before = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, before, o);
-        if (lane >= o) before += v;
-    }
-    if (lane == 31) scan[warp] = before;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += scan[w];
-        total += scan[w];
-    }
-    before -= mine;
-    total *= heads;
-    const long long per = (total + gridDim.x - 1) / gridDim.x > 2 ? (total + gridDim.x - 1) / gridDim.x : 2;
-    const long long from = per * blockIdx.x, to = from + per < total ? from + per : total;
-    if (from >= to) return;
-    if (from >= before * heads && from < (before + mine) * heads) {  // one thread: the entry that holds `from` is one of its own
-        int e = tid * each;
-        for (;; ++e) {
-            const int u = units_of(tile_of(p, e));
-            if (from < (before + u) * heads) break;
-            before += u;
-        }
-        scan[kWarps] = e, scan[kWarps + 1] = from - before * heads;
-    }
-    __syncthreads();
-    Walk ahead;
-    ahead.enter(p, static_cast<int>(scan[kWarps]));
-    ahead.head = static_cast<int>(scan[kWarps + 1] / ahead.units), ahead.unit = static_cast<int>(scan[kWarps + 1] % ahead.units);
-    Walk now = ahead;
-    const int count = static_cast<int>(to - from);
+    const Part& part = p.few;
+    Walk<kFewRows, kFewUnit> ahead;
+    const Run run = find_run<kAttendThreads>(p, part, scan, &ahead);
+    if (run.count == 0) return;
+    Walk<kFewRows, kFewUnit> now = ahead;
+    const int count = run.count, heads = p.cache.heads;
 
     // ---- copies ----------------------------------------------------------------------------------------------------------
     auto fetch = [&](int i) {
         if (i < count) {
             const uint32_t stage = ring + (i % S::kCount) * S::kBytes;
-            const int key0 = ahead.unit * kUnit;
-            auto page_of = [&](int key) -> int64_t {
-                const int page = load_plain(ahead.tile.pages + (key >> p.cache.page_shift));
-                if (page >= 0 && page < p.cache.pages) return page;
-                atomicExch(p.status, kBadIndex);
-                return -1;
-            };
+            const int key0 = ahead.unit * kFewUnit;
             const int mask = (1 << p.cache.page_shift) - 1;
 #pragma unroll
             for (int c = 0; c < S::kChunks; c += kAttendThreads) {
                 const int i16 = c + tid;
                 if (S::kChunks % kAttendThreads != 0 && i16 >= S::kChunks) break;
                 const int key = key0 + i16 / (S::kRow / 16), part = i16 % (S::kRow / 16);
-                const int64_t found = key < ahead.tile.keys ? page_of(key) : -1, page = found < 0 ? 0 : found;
+                const int64_t found = key < ahead.tile.keys ? page_of(p, ahead.tile, key) : -1, page = found < 0 ? 0 : found;
                 const bool there = found >= 0;  // else zeros
                 const uint32_t dst = stage + 16 * (i16 ^ ((i16 >> 3) & 7));
                 copy16(dst, codes_of<S::kRow>(p.cache.k, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
-                copy16(dst + kUnit * S::kRow, codes_of<S::kRow>(p.cache.v, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
+                copy16(dst + kFewUnit * S::kRow, codes_of<S::kRow>(p.cache.v, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
             }
-            if (tid < 2 * kUnit / 8) {
-                const int key = key0 + 8 * (tid % (kUnit / 8));
-                const bool values = tid >= kUnit / 8;
-                const int64_t found = key < ahead.tile.keys ? page_of(key) : -1, page = found < 0 ? 0 : found;
+            if (tid < 2 * kFewUnit / 8) {
+                const int key = key0 + 8 * (tid % (kFewUnit / 8));
+                const bool values = tid >= kFewUnit / 8;
+                const int64_t found = key < ahead.tile.keys ? page_of(p, ahead.tile, key) : -1, page = found < 0 ? 0 : found;
                 const bool there = found >= 0;
                 copy16(stage + S::kScales + 16 * tid, scale_of(values ? p.cache.v : p.cache.k, p.cache.page_shift, page, ahead.head, key & mask), there);
             }
-            ahead.next(p);
+            ahead.next(p, part);
         }
         copies_commit();
     };
@@ -235,10 +143,9 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
             for (int i = 0; i < D / 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const int field = 264 - static_cast<int>(__float_as_uint(top) >> 23), power = field > 253 ? 253 : field;  // exponent of the factor
-            const float up = __uint_as_float(uint32_t(power) << 23);
-            row_scale_log2[half] = p.scale_log2 * __uint_as_float(uint32_t(254 - power) << 23);
-            auto element = [&](int i) { return up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
+            const RowPower power(top);
+            row_scale_log2[half] = p.scale_log2 * power.down;
+            auto element = [&](int i) { return power.up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
             auto pair = [&](int i, int j) { return half_pair(element(i), element(j)); };
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
@@ -259,15 +166,15 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     };
-    long long pair_from = from - now.unit;  // number of the pair's unit 0
+    long long pair_from = run.from - now.unit;  // number of the pair's unit 0
     auto close = [&](long long done) {      // after unit `done` (exclusive) of the numbering
-        const int pair = now.entry * heads + now.head;
+        const int pair = now.pair(p);
         const long long entry = blockIdx.x + pair;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 1);
             l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 2);
-            if (t == 0) warp_sums[warp * kTileRows + g + 8 * half] = make_float2(m[half], l[half]);
+            if (t == 0) warp_sums[warp * kFewRows + g + 8 * half] = make_float2(m[half], l[half]);
         }
         __syncthreads();
         float f[2];
@@ -276,12 +183,12 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
             float top = -INFINITY, sum = 0.f;
             float2 ml[kWarps];
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) ml[w] = warp_sums[w * kTileRows + g + 8 * half], top = fmaxf(top, ml[w].x);
+            for (int w = 0; w < kWarps; ++w) ml[w] = warp_sums[w * kFewRows + g + 8 * half], top = fmaxf(top, ml[w].x);
             const float safe = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) sum += ml[w].y * exp2_fast(ml[w].x - safe);
             f[half] = exp2_fast(m[half] - safe) * (u_top * (1.f / 128.f));
-            if (warp == 0 && t == 0 && g + 8 * half < now.tile.rows) p.sums[entry * kTileRows + g + 8 * half] = make_float2(top, sum);
+            if (warp == 0 && t == 0 && g + 8 * half < now.tile.rows) part.sums[entry * kFewRows + g + 8 * half] = make_float2(top, sum);
         }
         // d of accumulator i, column 2 t + j: see the values' order below
         auto column = [&](int i, int j) {
@@ -298,16 +205,16 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
                     *at = add ? *at + v : v;
                 }
         };
-        if (warp >= 2) put(merge + (warp - 2) * kTileRows * (D + 4), false);
+        if (warp >= 2) put(merge + (warp - 2) * kFewRows * (D + 4), false);
         __syncthreads();
-        if (warp < 2) put(merge + warp * kTileRows * (D + 4), true);
+        if (warp < 2) put(merge + warp * kFewRows * (D + 4), true);
         __syncthreads();
         for (int i = tid; i < now.tile.rows * (D / 4); i += kAttendThreads) {
             const int r = i / (D / 4), c = 4 * (i % (D / 4));
-            const float4 a = *reinterpret_cast<const float4*>(merge + r * (D + 4) + c), b = *reinterpret_cast<const float4*>(merge + (kTileRows + r) * (D + 4) + c);
-            *reinterpret_cast<float4*>(p.parts + (entry * kTileRows + r) * D + c) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+            const float4 a = *reinterpret_cast<const float4*>(merge + r * (D + 4) + c), b = *reinterpret_cast<const float4*>(merge + (kFewRows + r) * (D + 4) + c);
+            *reinterpret_cast<float4*>(part.parts + (entry * kFewRows + r) * D + c) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
         }
-        if (tid == 0 && pair_from >= from) p.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + now.units - 1) / per - blockIdx.x + 1));
+        if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + now.units - 1) / run.per - blockIdx.x + 1));
         pair_from = done;
     };
 
@@ -317,7 +224,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
         __syncthreads();
         fetch(i + S::kCount - 1);
         const uint32_t stage = ring + (i % S::kCount) * S::kBytes;
-        const int key0 = now.unit * kUnit + 16 * warp;
+        const int key0 = now.unit * kFewUnit + 16 * warp;
         // ---- scores of 16 keys: key 8 j + g of the warp's is column g of tile j
         float s[2][4];
 #pragma unroll
@@ -353,7 +260,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint32_t at = stage + S::kScales + 2 * (16 * warp + 8 * j + 2 * t);
-            const uint32_t ks = lds32(at), vs = lds32(at + 2 * kUnit);
+            const uint32_t ks = lds32(at), vs = lds32(at + 2 * kFewUnit);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int key = key0 + 8 * j + 2 * t + c;
@@ -413,7 +320,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
         for (int c = 0; c < kMats; c += 2) {
             const int key = 16 * warp + (lane & 15), i16 = key * kMats + c + (lane >> 4);
             uint32_t r[4];  // keys 0 .. 7 and 8 .. 15 of chunk c, then of chunk c + 1
-            ldmatrix4_trans(stage + kUnit * S::kRow + 16 * (i16 ^ ((i16 >> 3) & 7)), r);
+            ldmatrix4_trans(stage + kFewUnit * S::kRow + 16 * (i16 ^ ((i16 >> 3) & 7)), r);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -425,8 +332,8 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
                 }
         }
         if (now.unit + 1 == now.units || i + 1 == count) {
-            close(from + i + 1);
-            now.next(p);
+            close(run.from + i + 1);
+            now.next(p, part);
             if (i + 1 < count) open();
         } else {
             ++now.unit;
@@ -462,23 +369,24 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     float m = -INFINITY, l = 0.f, o[kE];
 #pragma unroll
     for (int e = 0; e < kE; ++e) o[e] = 0.f;
-    auto join = [&](int entry, int r) {
-        const Tile tile = tile_of(p, entry);
-        if (tile.keys == 0) return;
+    auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
+        const Part& part = tall ? p.tall : p.few;
+        const int rows = tall ? kTallRows : kFewRows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
+        if ((tall ? tile_of<kTallRows>(p, part, entry) : tile_of<kFewRows>(p, part, entry)).keys == 0) return;
         const int pair = entry * p.cache.heads + h;
-        const int2 ctas = load_plain(p.pairs + pair);
+        const int2 ctas = load_plain(part.pairs + pair);
         const int64_t first = static_cast<int64_t>(ctas.x) + pair;
         for (int i = 0; i < ctas.y; ++i) {
-            const int64_t at = (first + i) * kTileRows + r;
-            const float2 ml = load_plain(p.sums + at);
+            const int64_t at = (first + i) * rows + r;
+            const float2 ml = load_plain(part.sums + at);
             const float top = fmaxf(m, ml.x), safe = top == -INFINITY ? 0.f : top;
             const float fa = exp2_fast(m - safe), fb = exp2_fast(ml.x - safe);
             float v[kE];
             if constexpr (kE == 4) {
-                const float4 u = load_plain(reinterpret_cast<const float4*>(p.parts + at * D) + lane);
+                const float4 u = load_plain(reinterpret_cast<const float4*>(part.parts + at * D) + lane);
                 v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
             } else {
-                const float2 u = load_plain(reinterpret_cast<const float2*>(p.parts + at * D) + lane);
+                const float2 u = load_plain(reinterpret_cast<const float2*>(part.parts + at * D) + lane);
                 v[0] = u.x, v[1] = u.y;
             }
             m = top, l = l * fa + ml.y * fb;
@@ -486,12 +394,8 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
             for (int e = 0; e < kE; ++e) o[e] = o[e] * fa + v[e] * fb;
         }
     };
-    if (p.tiles_prefix > 0) {
-        const int r = token * p.group + head % p.group;
-        join(r / kTileRows, r % kTileRows);
-    }
-    const int r = place * p.group + head % p.group;
-    if (place < p.max_new) join(p.tiles_prefix + b * p.tiles_seq + r / kTileRows, r % kTileRows);
+    if (p.prefix_length > 0) join(p.prefix_tall != 0, -1, token * p.group + head % p.group);
+    if (place < p.max_new) join(p.seq_tall != 0, b, place * p.group + head % p.group);
     else if (lane == 0) atomicExch(p.status, kBadIndex);  // more new tokens than the call was told
     const float f = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -532,16 +436,26 @@ static cudaError_t ctas_of(const bfq_plan* plan, int bits, int* ctas) {
                          : (bits == 4 ? attend_ctas<128, 4>(plan, ctas) : attend_ctas<128, 8>(plan, ctas));
 }
 
-struct Room {
-    size_t pairs, sums, parts, bytes;
-};
-static Room room_of(const AttendParams& p, int n, int ctas) {
-    const size_t pairs = size_t(p.entries()) * p.cache.heads, entries = pairs + ctas;
-    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    Room r;
-    r.pairs = 0, r.sums = up(pairs * sizeof(int2)), r.parts = r.sums + up(entries * kTileRows * sizeof(float2));
-    r.bytes = r.parts + entries * kTileRows * n * sizeof(float);
-    return r;
+// Tiles of 256 rows where there are rows enough to pay for them.
+static bool use_tall(int64_t rows) { return rows > 48; }
+
+// The workspace: for each of the two kernels pairs, sums and parts.  Lays them out from `at` on (null: only counts); returns the bytes.
+static size_t lay_out(AttendParams* p, int n, int ctas_few, int ctas_tall, uint8_t* at) {
+    size_t bytes = 0;
+    auto take = [&](size_t b) {
+        uint8_t* here = at != nullptr ? at + bytes : nullptr;
+        bytes += (b + 255) / 256 * 256;
+        return here;
+    };
+    for (const bool tall : {false, true}) {
+        Part& part = tall ? p->tall : p->few;
+        const size_t pairs = size_t(p->entries(part)) * p->cache.heads, rows = (pairs + (tall ? ctas_tall : ctas_few)) * (tall ? kTallRows : kFewRows);
+        if (pairs == 0) continue;
+        part.pairs = reinterpret_cast<int2*>(take(pairs * sizeof(int2)));
+        part.sums = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
+        part.parts = reinterpret_cast<float*>(take(rows * n * sizeof(float)));
+    }
+    return bytes;
 }
 
 // checks everything that the host can see and lays the work out
@@ -571,9 +485,11 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     p->q_starts = in->q_starts, p->prefix = in->prefix, p->prefix_pages = in->prefix_pages, p->prefix_length = int(in->prefix_length);
     p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : in->max_new;
     const int64_t rows = (in->q_starts == nullptr ? in->batch : in->tokens) * int64_t(p->group), rows_seq = int64_t(p->max_new) * p->group;
-    const int64_t prefix_tiles = in->prefix_length > 0 ? (rows + kTileRows - 1) / kTileRows : 0, seq_tiles = (rows_seq + kTileRows - 1) / kTileRows;
-    if ((prefix_tiles + seq_tiles * in->batch) * cache->heads >= int64_t(1) << 30) return BFQ_ERR_TOO_LARGE;
-    p->tiles_prefix = int(prefix_tiles), p->tiles_seq = int(seq_tiles);
+    p->prefix_tall = use_tall(rows), p->seq_tall = use_tall(rows_seq);
+    const int tile_prefix = p->prefix_tall ? kTallRows : kFewRows, tile_seq = p->seq_tall ? kTallRows : kFewRows;
+    const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;
+    if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 30) return BFQ_ERR_TOO_LARGE;
+    (p->prefix_tall ? p->tall : p->few).tiles_prefix = int(tiles_prefix), (p->seq_tall ? p->tall : p->few).tiles_seq = int(tiles_seq);
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;
     return BFQ_OK;
@@ -584,13 +500,24 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
 
 using namespace bfq;
 
+namespace {
+// CTAs of the two launches; a kernel that has no work: 0
+cudaError_t ctas_of_both(const bfq_plan* plan, const kv::AttendParams& p, int* few, int* tall) {
+    *few = *tall = 0;
+    cudaError_t e = cudaSuccess;
+    if (p.entries(p.few) > 0) e = kv::ctas_of(plan, p.cache.bits, few);
+    if (e == cudaSuccess && p.entries(p.tall) > 0) e = kv::tall_ctas(plan, p.cache.bits, tall);
+    return e;
+}
+}  // namespace
+
 extern "C" size_t bfq_kv_attend_workspace(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_queries* in) {
     kv::AttendParams p{};
     if (kv::set_up(plan, cache, in, &p) != BFQ_OK || p.batch == 0) return 0;
     kv::OnDevice guard(plan->device);
-    int ctas = 0;
-    if (!guard.ok || kv::ctas_of(plan, cache->bits, &ctas) != cudaSuccess) return 0;
-    return kv::room_of(p, plan->n, ctas).bytes;
+    int few = 0, tall = 0;
+    if (!guard.ok || ctas_of_both(plan, p, &few, &tall) != cudaSuccess) return 0;
+    return kv::lay_out(&p, plan->n, few, tall, nullptr);
 }
 
 extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_queries* in, void* workspace, size_t workspace_bytes, void* stream) {
@@ -599,18 +526,18 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
     if (rc != BFQ_OK || p.batch == 0) return rc;
     kv::OnDevice guard(plan->device);
     if (!guard.ok) return BFQ_ERR_CUDA;
-    int ctas = 0;
-    cudaError_t e = kv::ctas_of(plan, cache->bits, &ctas);
+    int few = 0, tall = 0;
+    cudaError_t e = ctas_of_both(plan, p, &few, &tall);
     if (e == cudaSuccess) {
-        const kv::Room room = kv::room_of(p, plan->n, ctas);
-        if (workspace == nullptr || workspace_bytes < room.bytes) return BFQ_ERR_WORKSPACE;
+        if (workspace == nullptr || workspace_bytes < kv::lay_out(&p, plan->n, few, tall, nullptr)) return BFQ_ERR_WORKSPACE;
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return BFQ_ERR_ALIGN;
-        uint8_t* at = static_cast<uint8_t*>(workspace);
-        p.pairs = reinterpret_cast<int2*>(at + room.pairs), p.sums = reinterpret_cast<float2*>(at + room.sums), p.parts = reinterpret_cast<float*>(at + room.parts);
+        kv::lay_out(&p, plan->n, few, tall, static_cast<uint8_t*>(workspace));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         const bool four = cache->bits == 4;
-        e = plan->n == 64 ? (four ? kv::launch_attend<64, 4>(p, ctas, st) : kv::launch_attend<64, 8>(p, ctas, st))
-                          : (four ? kv::launch_attend<128, 4>(p, ctas, st) : kv::launch_attend<128, 8>(p, ctas, st));
+        if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
+        if (e == cudaSuccess && few > 0)
+            e = plan->n == 64 ? (four ? kv::launch_attend<64, 4>(p, few, st) : kv::launch_attend<64, 8>(p, few, st))
+                              : (four ? kv::launch_attend<128, 4>(p, few, st) : kv::launch_attend<128, 8>(p, few, st));
         if (e == cudaSuccess) {
             const dim3 grid(unsigned((p.tokens * p.q.heads + 3) / 4));
             e = plan->n == 64 ? launch_overlapped(kv::k_join<64>, grid, dim3(128), 0, st, p) : launch_overlapped(kv::k_join<128>, grid, dim3(128), 0, st, p);

@@ -1,18 +1,28 @@
 // Attention over the paged low-bit cache: the call as the kernels see it, and the order that its work is numbered in.
 //
-// A pair is (row tile, key head): up to kTileRows query rows that share a key head, a row being (token, query head of the group), tokens
+// A pair is (row tile, key head): up to ROWS query rows that share a key head, a row being (token, query head of the group), tokens
 // outermost.  Row tiles of the shared prefix come first (their rows are those of all tokens), then those of each sequence.  A pair's
-// keys are cut into units of kUnit; units are numbered pair by pair and every CTA takes an equal run of them, wherever sequences end.
+// keys are cut into units of UNIT; units are numbered pair by pair and every CTA takes an equal run of them, wherever sequences end.
 // What a CTA has of a pair is a partial result: per row the reference m, the sum l of exp2(s - m) and the sum of exp2(s - m) V.  It is
 // entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.
+//
+// Two kernels do this: one for few rows (tiles of 16 rows, units of 64 keys), one for many (256 rows, 128 keys).  A call gives the prefix's
+// tiles to one of them and the sequences' to the same one or the other; each has its own Part of the work.
 #pragma once
 #include "bfq_kv.cuh"
 
 namespace bfq {
 namespace kv {
 
-constexpr int kUnit = 64;  // keys of a unit
-constexpr int kTileRows = 16;
+constexpr int kFewRows = 16, kFewUnit = 64;
+constexpr int kTallRows = 256, kTallUnit = 128;
+
+struct Part {
+    int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
+    int2* pairs;                  // [pairs] first CTA, CTAs
+    float2* sums;                 // [entries][ROWS] m, l
+    float* parts;                 // [entries][ROWS][D]
+};
 
 struct AttendParams {
     Cache cache;
@@ -27,14 +37,12 @@ struct AttendParams {
     int prefix_pages, prefix_length;
     int64_t tokens;  // rows of q: at least those of the sequences
     int batch, group, max_new;
-    int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
-    float scale_log2;             // softmax scale * log2 e
+    float scale_log2;  // softmax scale * log2 e
     const float2* tw;
-    int2* pairs;        // [pairs] first CTA, CTAs
-    float2* sums;       // [entries][kTileRows] m, l
-    float* parts;       // [entries][kTileRows][D]
+    Part few, tall;
+    int prefix_tall, seq_tall;  // which of them has the prefix, the sequences
     int* status;
-    __host__ __device__ int entries() const { return tiles_prefix + batch * tiles_seq; }
+    __host__ __device__ int entries(const Part& part) const { return part.tiles_prefix + batch * part.tiles_seq; }
 };
 
 __device__ __forceinline__ int first_token(const AttendParams& p, int b) {
@@ -55,30 +63,156 @@ struct Tile {
     int last0;           // row r has keys 0 .. last0 + (row0 + r) / group; prefix: all
     const int32_t* pages;
 };
-__device__ __forceinline__ Tile tile_of(const AttendParams& p, int e) {
+template <int ROWS>
+__device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part, int e) {
     Tile t;
-    if (e < p.tiles_prefix) {
+    if (e < part.tiles_prefix) {
         const int tokens = first_token(p, p.batch);
-        t.row0 = e * kTileRows, t.token0 = 0;
+        t.row0 = e * ROWS, t.token0 = 0;
         const int left = tokens * p.group - t.row0;
-        t.rows = left < 0 ? 0 : (left < kTileRows ? left : kTileRows);
+        t.rows = left < 0 ? 0 : (left < ROWS ? left : ROWS);
         t.keys = t.rows > 0 ? p.prefix_length : 0;
         t.last0 = 1 << 30;
         t.pages = p.prefix;
         return t;
     }
-    const int b = (e - p.tiles_prefix) / p.tiles_seq, rt = (e - p.tiles_prefix) % p.tiles_seq;
+    const int b = (e - part.tiles_prefix) / part.tiles_seq, rt = (e - part.tiles_prefix) % part.tiles_seq;
     const int t0 = first_token(p, b), news = first_token(p, b + 1) - t0, n = cached_keys(p, b);
-    t.row0 = rt * kTileRows, t.token0 = t0;
+    t.row0 = rt * ROWS, t.token0 = t0;
     const int left = news * p.group - t.row0;
-    t.rows = left < 0 ? 0 : (left < kTileRows ? left : kTileRows);
+    t.rows = left < 0 ? 0 : (left < ROWS ? left : ROWS);
     t.last0 = n - news;
     const int need = t.rows > 0 ? t.last0 + (t.row0 + t.rows - 1) / p.group + 1 : 0;
     t.keys = need < 0 ? 0 : need;
     t.pages = p.block_table + b * p.table_ld;
     return t;
 }
-__device__ __forceinline__ int units_of(const Tile& t) { return (t.keys + kUnit - 1) / kUnit; }
+
+// Where in the numbering of units a role of a CTA is.
+template <int ROWS, int UNIT>
+struct Walk {
+    int entry, head, unit, units;  // unit of units within the pair
+    Tile tile;
+    __device__ __forceinline__ void enter(const AttendParams& p, const Part& part, int e) {  // the first entry from e on that has units
+        const int last = p.entries(part);
+        for (entry = e, units = 0; entry < last; ++entry) {
+            tile = tile_of<ROWS>(p, part, entry);
+            units = (tile.keys + UNIT - 1) / UNIT;
+            if (units > 0) break;
+        }
+    }
+    __device__ __forceinline__ void next_pair(const AttendParams& p, const Part& part) {
+        unit = 0;
+        if (++head < p.cache.heads) return;
+        head = 0;
+        enter(p, part, entry + 1);
+    }
+    __device__ __forceinline__ void next(const AttendParams& p, const Part& part) {
+        if (++unit == units) next_pair(p, part);
+    }
+    __device__ __forceinline__ int pair(const AttendParams& p) const { return entry * p.cache.heads + head; }
+};
+
+// A CTA's run of units, found by all its threads together from the lengths.
+struct Run {
+    long long from;  // the first one's number
+    long long per;   // units of every CTA but the last ones
+    int count;       // 0: none
+};
+template <int THREADS, int ROWS, int UNIT>
+__device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part, long long* scan, Walk<ROWS, UNIT>* walk) {  // scan: shared, THREADS / 32 + 2
+    constexpr int kWarps = THREADS / 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, entries = p.entries(part), heads = p.cache.heads;
+    const int each = (entries + THREADS - 1) / THREADS;
+    auto units_at = [&](int e) { return (tile_of<ROWS>(p, part, e).keys + UNIT - 1) / UNIT; };
+    long long mine = 0;
+    for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_at(e);
+    long long before = mine, total = 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        if (lane >= o) before += v;
+    }
+    if (lane == 31) scan[warp] = before;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) before += scan[w];
+        total += scan[w];
+    }
+    before -= mine;
+    total *= heads;
+    Run run;
+    run.per = (total + gridDim.x - 1) / gridDim.x > 2 ? (total + gridDim.x - 1) / gridDim.x : 2;
+    run.from = run.per * blockIdx.x;
+    const long long to = run.from + run.per < total ? run.from + run.per : total;
+    run.count = run.from < to ? static_cast<int>(to - run.from) : 0;
+    if (run.count == 0) return run;
+    if (run.from >= before * heads && run.from < (before + mine) * heads) {  // one thread: the entry that holds `from` is one of its own
+        int e = tid * each;
+        for (;; ++e) {
+            const int u = units_at(e);
+            if (run.from < (before + u) * heads) break;
+            before += u;
+        }
+        scan[kWarps] = e, scan[kWarps + 1] = run.from - before * heads;
+    }
+    __syncthreads();
+    walk->enter(p, part, static_cast<int>(scan[kWarps]));
+    walk->head = static_cast<int>(scan[kWarps + 1] / walk->units), walk->unit = static_cast<int>(scan[kWarps + 1] % walk->units);
+    return run;
+}
+
+// page of a key: -1, and reported, if the block table has none of the cache's
+__device__ __forceinline__ int64_t page_of(const AttendParams& p, const Tile& tile, int key) {
+    const int page = load_plain(tile.pages + (key >> p.cache.page_shift));
+    if (page >= 0 && page < p.cache.pages) return page;
+    atomicExch(p.status, kBadIndex);
+    return -1;
+}
+
+__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Codes of a word as exact fp16 pairs (one of the lower half, one of the upper): the code's bits, its top one inverted, lie in the mantissa of
+// 1024 .. 2047.  4 bits: codes i and i + 4, i < 4; the odd ones lie four places up there, 1152 + 16 code.  8 bits: codes i and i + 2, i < 2.
+__device__ __forceinline__ uint32_t pair4(uint32_t w, int i) {
+    if (i >= 2) w >>= 8;
+    return i & 1 ? fma_pair((w & 0x00F000F0u) ^ 0x64806480u, 0x2C002C00u, 0xD480D480u)  // / 16 - 72
+                 : sub_pair((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);             // - 1032
+}
+__device__ __forceinline__ uint32_t pair8(uint32_t w, int i) {
+    if (i) w >>= 8;
+    return sub_pair((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);  // - 1152
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The power of two that puts a row's largest element `top` in [2^10, 2^11): elements down to 2^-24 of it stay exact in fp16.
+struct RowPower {
+    float up, down;  // 2^e and 2^-e
+    __device__ __forceinline__ explicit RowPower(float top) {
+        const int field = 264 - static_cast<int>(__float_as_uint(top) >> 23), e = field > 253 ? 253 : field;
+        up = __uint_as_float(uint32_t(e) << 23), down = __uint_as_float(uint32_t(254 - e) << 23);
+    }
+};
+
+// the tall kernel (bfq_kvtall.cu): CTAs of a launch, and the launch
+cudaError_t tall_ctas(const bfq_plan* plan, int bits, int* ctas);
+cudaError_t tall_launch(const bfq_plan* plan, const AttendParams& p, int ctas, cudaStream_t st);
 
 }  // namespace kv
 }  // namespace bfq
