@@ -6,302 +6,527 @@
 //     keys, values s = fp16(max |y| / qmax), codes = clip(round(y / s)) in the page and place of the token's slot.
 // Values are rotated by Q alone.  bfq_kv_read: x = Q^T (s code), the rows at any slots in the model's basis.
 //
-// A row of D = 64 or 128 elements lies on D / 8 lanes, 8 elements (one 16-byte load of bf16) each: three stages of the butterfly in
-// a lane, the others by exchanges; more elements per lane would save exchanges and cost 16 registers of constants each per stage.
-// All sums in fp32.  What bounds it: instructions (about 30 per element and lane against 14 that the memory's rate would leave).
+// A thread owns a row of D = 64 or 128 elements, all of it in registers, so that norms, maxima and the stages of the butterfly need no
+// exchange between lanes; a warp takes 32 consecutive rows (a token's heads share its angles), copied into shared memory 16 bytes a lane, the next
+// 32 while these are worked on, and results go out the same way.  The butterfly's constants are the same for all lanes: they come from
+// shared memory by broadcast.  Its stages run in the scaled form, two FMAs a pair: with z = P w, P the product of the cosines
+// that an element has been through,
+//     lo: w <- w_lo - tan(t) (P_hi / P_lo) w_hi,   hi: w <- w_hi + tan(t) (P_lo / P_hi) w_lo,   P <- P cos(t)
+// and P multiplied in at the end.  Where some |P| is below 2^-40 (an angle close to an odd multiple of pi/2), and for 32 rows of which
+// one is not finite in that form, the plain stages are taken, four operations a pair.  All sums in fp32.
+//
+// What bounds it: fp32 operations, about 14 an element at 128 a cycle and SM, which is what the memory's rate leaves room for, too.  With a row
+// on 16 lanes (exchanges by shuffles, constants in registers, 12 warps on an SM) 16384 tokens of 32 + 2 x 8 heads took 420 us.
 #include "bfq_generic.cuh"
-#include "bfq_kv.cuh"
+#include "bfq_kvrows.cuh"
 #include "bfq_n4096.cuh"
 
 namespace bfq {
 namespace kv {
 
-constexpr int kRowThreads = 128;
+constexpr int kMostWarps = 4;  // of a CTA
 
-struct AppendParams {
-    Cache cache;
-    Heads q, k, v, q_out;  // q.heads = 0: no queries
-    const int64_t* slots;
-    const int32_t* positions;  // null: no rotation by position
-    const float* rope;         // [rope_rows][rope_dims]: cos of rope_dims / 2 frequencies, then sin
-    const float* q_norm;
-    const float* k_norm;
-    const float2* tw;
-    int64_t rope_rows, tokens;
-    float eps;
-    int rope_dims, interleaved;
-    int* status;
-};
+__device__ __forceinline__ uint4 shared_load(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void shared_store(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void copy_in(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// 8 elements of a row as they lie in memory, and as numbers
-template <bool F32>
-struct Raw {
-    uint4 w[F32 ? 2 : 1];
-    __device__ __forceinline__ void load(const uint8_t* at) {
-#pragma unroll
-        for (int i = 0; i < (F32 ? 2 : 1); ++i) w[i] = load_plain(reinterpret_cast<const uint4*>(at) + i);
-    }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        if constexpr (F32) {
-            const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i]);
-        } else {
-            const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+// The butterfly on a row in a thread's registers, elements 2 r and 2 r + 1 in register r.  Table in shared memory, 16 bytes an entry: stage 0:
+// (a, b) of registers 2 k and 2 k + 1, with lo <- lo + a hi, hi <- hi + b lo; the other stages: (a, a', b, b') of the k-th pair of registers;
+// then P, four elements an entry.
+template <int D, bool BACK>
+struct RowTurn {
+    static constexpr int kStages = D == 64 ? 6 : 7, kPerStage = D / 4;
+    static constexpr uint32_t kBytes = 16 * (kStages * kPerStage + D / 4);
+
+    // All threads of the CTA; products: D floats of shared memory.  Returns whether the scaled form can be taken.
+    __device__ static bool build(float* table, float* products, const float2* tw) {
+        float* const out = table + 4 * kStages * kPerStage;
+        for (int i = threadIdx.x; i < D; i += blockDim.x) products[i] = 1.f;
+        __syncthreads();
+        for (int n = 0; n < kStages; ++n) {
+            const int st = BACK ? kStages - 1 - n : n;
+            for (int j = threadIdx.x; j < D / 2; j += blockDim.x) {
+                const float2 t = load_plain(tw + st * (D / 2) + j);
+                const int lo = ((j >> st) << (st + 1)) | (j & ((1 << st) - 1)), hi = lo + (1 << st);
+                const float tangent = (BACK ? -t.y : t.y) / t.x, p = products[lo], q = products[hi], a = -tangent * (q / p), b = tangent * (p / q);
+                if (st == 0) {
+                    table[2 * j] = a, table[2 * j + 1] = b;
+                } else {  // pair j is half j & 1 of the registers' pair j / 2
+                    float* at = table + 4 * (st * kPerStage + (j >> 1)) + (j & 1);
+                    at[0] = a, at[2] = b;
+                }
+                products[lo] = p * t.x, products[hi] = q * t.x;
+            }
+            __syncthreads();
         }
+        int fine = 1;
+        for (int i = threadIdx.x; i < D; i += blockDim.x) {
+            out[i] = products[i];
+            fine &= fabsf(products[i]) >= 0x1p-40f;  // false for NaN too
+        }
+        return __syncthreads_and(fine) != 0;
     }
-};
-__device__ __forceinline__ void load_floats8(const float* at, float (&x)[8]) {
-    Raw<true> r;
-    r.load(reinterpret_cast<const uint8_t*>(at));
-    r.get(x);
-}
-
-// 8 elements -> codes of 4 bits (one word) or 8 (two): quant1's codes (clip(x inv), then round to nearest even), the rounding by an addition
-// that leaves the integer in the low bits
-template <int BITS>
-__device__ __forceinline__ void codes8(const float (&x)[8], float inv, uint32_t (&w)[BITS / 4]) {
-    constexpr float kTop = (1 << (BITS - 1)) - 1;
-    uint32_t c[8];
+    __device__ __forceinline__ static void scaled(u64 (&x)[D / 2], uint32_t table) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(x[e], inv), -kTop - 1.f), kTop), 12582912.f));
-    if constexpr (BITS == 4) {
-        w[0] = 0;
+        for (int n = 0; n < kStages; ++n) {
+            const int st = BACK ? kStages - 1 - n : n;
+            if (st == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[0] |= (c[e] & 15u) << (4 * e);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
-    }
-}
-
-// The rows of a CTA are consecutive (a token's rows share its position's angles and its slot), kRowThreads / (D / 8) at a time.  A lane's row
-// by token and row of the token, without a division at each step.
-struct RowAt {
-    int64_t token, left;  // rows from this one to the CTA's last (<= 0: none)
-    int r;                // of the token's `heads`
-    __device__ __forceinline__ void start(int64_t rows, int heads, int rows_per_step) {
-        const int64_t steps = (rows + rows_per_step - 1) / rows_per_step, per = (steps + gridDim.x - 1) / gridDim.x * rows_per_step;
-        const int64_t from = per * blockIdx.x, to = from + per < rows ? from + per : rows, row = from + threadIdx.x / (kRowThreads / rows_per_step);
-        left = to - row, token = row / heads, r = static_cast<int>(row - token * heads);
-    }
-    __device__ __forceinline__ void next(int heads, int rows_per_step) {
-        left -= rows_per_step;
-        r += rows_per_step;
-        while (r >= heads) r -= heads, ++token;
-    }
-    __device__ __forceinline__ bool there() const { return left > 0; }
-};
-
-// Of a row's token: what the row after next needs is on its way while this one is worked on.
-template <int D, bool F32, int BITS>
-__global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p) {
-    constexpr int kLanes = D / 8, kStep = kRowThreads / kLanes;
-    grid_dep_wait();
-    const int lane = threadIdx.x & 31, l = lane % kLanes;
-    const int heads = p.q.heads + 2 * p.cache.heads;  // rows of a token: queries, keys, values
-    auto kind_of = [&](const RowAt& a) { return a.r < p.q.heads ? 0 : (a.r < p.q.heads + p.cache.heads ? 1 : 2); };
-    auto head_of = [&](const RowAt& a, int kind) { return a.r - (kind == 0 ? 0 : (kind == 1 ? p.q.heads : p.q.heads + p.cache.heads)); };
-    auto fetch = [&](const RowAt& a, Raw<F32>& raw) {
-        if (!a.there()) return;
-        const int kind = kind_of(a), head = head_of(a, kind);
-        const uint8_t* data = kind == 0 ? p.q.data : (kind == 1 ? p.k.data : p.v.data);
-        const int64_t st = kind == 0 ? p.q.token : (kind == 1 ? p.k.token : p.v.token), sh = kind == 0 ? p.q.head : (kind == 1 ? p.k.head : p.v.head);
-        raw.load(data + (a.token * st + head * sh + 8 * l) * (F32 ? 4 : 2));
-    };
-    RowAt at, ahead;
-    at.start(p.tokens * heads, heads, kStep);
-    Raw<F32> raw, raw_next;
-    fetch(at, raw);
-    int position = at.there() && p.positions != nullptr ? load_plain(p.positions + at.token) : 0, position_next = 0;
-    int64_t slot = at.there() ? load_plain(p.slots + at.token) : -1, slot_next = -1;
-    Turn<D, 8, false> turn;
-    turn.load(p.tw, lane);
-    for (; __any_sync(0xFFFFFFFFu, at.there()); at = ahead, raw = raw_next, position = position_next, slot = slot_next) {
-        const bool there = at.there();
-        const int kind = kind_of(at), head = head_of(at, kind);
-        const bool turned = there && p.positions != nullptr && kind < 2 && 8 * l < p.rope_dims, upper = !p.interleaved && 16 * l >= p.rope_dims;
-        float cs[8], sn[8];
-        if (turned) {
-            const bool fine = position >= 0 && position < p.rope_rows;
-            if (!fine) atomicExch(p.status, kBadIndex);
-            const float* table = p.rope + (fine ? position : 0) * int64_t(p.rope_dims);
-            if (p.interleaved) {
-                const float4 c = load_plain(reinterpret_cast<const float4*>(table + 4 * l)), s = load_plain(reinterpret_cast<const float4*>(table + p.rope_dims / 2 + 4 * l));
-                cs[0] = c.x, cs[1] = c.y, cs[2] = c.z, cs[3] = c.w, sn[0] = s.x, sn[1] = s.y, sn[2] = s.z, sn[3] = s.w;
+                for (int k = 0; k < D / 4; ++k) {
+                    const uint4 c = shared_load(table + 16 * k);
+                    float a, b;
+                    unpack2(x[2 * k], a, b);
+                    x[2 * k] = pack2(fmaf(__uint_as_float(c.x), b, a), fmaf(__uint_as_float(c.y), a, b));
+                    unpack2(x[2 * k + 1], a, b);
+                    x[2 * k + 1] = pack2(fmaf(__uint_as_float(c.z), b, a), fmaf(__uint_as_float(c.w), a, b));
+                }
             } else {
-                const float* t = table + 8 * l - (upper ? p.rope_dims / 2 : 0);
-                load_floats8(t, cs), load_floats8(t + p.rope_dims / 2, sn);
+                const int h = 1 << (st - 1);  // in registers
+#pragma unroll
+                for (int k = 0; k < kPerStage; ++k) {
+                    const int lo = ((k / h) * 2 * h) + k % h, hi = lo + h;
+                    const uint4 c = shared_load(table + 16 * (st * kPerStage + k));
+                    const u64 a = x[lo], b = x[hi];
+                    x[lo] = fma2(pack2u(c.x, c.y), b, a), x[hi] = fma2(pack2u(c.z, c.w), a, b);
+                }
             }
         }
-        ahead = at;
-        ahead.next(heads, kStep);
-        fetch(ahead, raw_next);
-        if (ahead.there()) {
-            slot_next = load_plain(p.slots + ahead.token);
-            if (p.positions != nullptr) position_next = load_plain(p.positions + ahead.token);
+#pragma unroll
+        for (int k = 0; k < D / 4; ++k) {
+            const uint4 c = shared_load(table + 16 * (kStages * kPerStage + k));
+            x[2 * k] = mul2(x[2 * k], pack2u(c.x, c.y)), x[2 * k + 1] = mul2(x[2 * k + 1], pack2u(c.z, c.w));
         }
-        float x[8];
-        raw.get(x);
-        const float* norm = kind == 0 ? p.q_norm : (kind == 1 ? p.k_norm : nullptr);
-        if (__any_sync(0xFFFFFFFFu, norm != nullptr)) {
-            float sum = 0.f;
+    }
+    __device__ __forceinline__ static void plain(u64 (&x)[D / 2], const float2* tw) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+        for (int n = 0; n < kStages; ++n) {
+            const int st = BACK ? kStages - 1 - n : n;
 #pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            if (norm != nullptr) {
-                const float f = 1.f / sqrtf(sum * (1.f / D) + p.eps);
-                float w[8];
-                load_floats8(norm + 8 * l, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= f * w[e];
+            for (int j = 0; j < D / 2; ++j) {
+                const float2 t = load_plain(tw + st * (D / 2) + j);
+                const int lo = ((j >> st) << (st + 1)) | (j & ((1 << st) - 1)), hi = lo + (1 << st);
+                float v[2], w[2];
+                unpack2(x[lo / 2], v[0], v[1]), unpack2(x[hi / 2], w[0], w[1]);
+                const float s = BACK ? -t.y : t.y, a = v[lo & 1], b = st == 0 ? v[1] : w[hi & 1];
+                const float na = fmaf(t.x, a, -s * b), nb = fmaf(s, a, t.x * b);
+                if (st == 0) {
+                    x[lo / 2] = pack2(na, nb);
+                } else {
+                    v[lo & 1] = na, w[hi & 1] = nb;
+                    x[lo / 2] = pack2(v[0], v[1]), x[hi / 2] = pack2(w[0], w[1]);
+                }
             }
         }
-        if (__any_sync(0xFFFFFFFFu, turned)) {
-            if (p.interleaved) {
-                if (turned) {
+    }
+};
+
+// Which rows a warp has: chunks of 32 rows, a CTA's consecutive, its warps' in turn.
+struct Chunks {
+    int at, end, step;
+    __device__ __forceinline__ explicit Chunks(int rows) {
+        const int chunks = (rows + 31) / 32, per = (chunks + gridDim.x - 1) / gridDim.x, from = per * blockIdx.x;
+        step = blockDim.x >> 5;
+        end = from + per < chunks ? from + per : chunks;
+        at = from + (threadIdx.x >> 5);
+    }
+    __device__ __forceinline__ bool there() const { return at < end; }
+};
+
+// A warp's 32 rows of BYTES bytes each between memory and shared memory (PITCH apart there), 16 bytes a lane; `row` is the lane's own
+// row's address.  f(place in shared memory, address, row) for each 16 bytes of a row of which `bytes`, the row's own, covers them.
+template <int BYTES, int PITCH, class F>
+__device__ __forceinline__ void each_chunk(const uint8_t* row, int bytes, F&& f) {
+    constexpr int kLanes = BYTES / 16 < 32 ? BYTES / 16 : 32, kRows = 32 / kLanes, kTurns = BYTES / 16 / kLanes;
+    const int lane = threadIdx.x & 31, part = lane % kLanes;
+    const uint64_t address = reinterpret_cast<uint64_t>(row);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = x[2 * i], b = x[2 * i + 1];
-                        x[2 * i] = fmaf(a, cs[i], -b * sn[i]);
-                        x[2 * i + 1] = fmaf(b, cs[i], a * sn[i]);
+    for (int r = 0; r < 32; r += kRows) {
+        const int from = r + lane / kLanes;
+        const uint32_t lo = __shfl_sync(0xFFFFFFFFu, static_cast<uint32_t>(address), from), hi = __shfl_sync(0xFFFFFFFFu, static_cast<uint32_t>(address >> 32), from);
+        const int size = __shfl_sync(0xFFFFFFFFu, bytes, from);
+        uint8_t* const base = reinterpret_cast<uint8_t*>(static_cast<uint64_t>(hi) << 32 | lo);
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int off = 16 * (part + t * kLanes);
+            if (off < size) f(static_cast<uint32_t>(from * PITCH + off), base + off);
+        }
+    }
+}
+
+// 16 bytes of a row as numbers, in pairs
+template <bool F32>
+__device__ __forceinline__ void unpack_chunk(uint4 v, u64* x) {  // bf16: 4 pairs, fp32: 2
+    if constexpr (F32) {
+        x[0] = pack2u(v.x, v.y), x[1] = pack2u(v.z, v.w);
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = pack2u(w[i] << 16, w[i] & 0xFFFF0000u);
+    }
+}
+template <int D>
+__device__ __forceinline__ float largest(const u64 (&x)[D / 2]) {  // NaN elements do not count, as in the other quantizers
+    float top[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < D / 2; ++r) {
+        float a, b;
+        unpack2(x[r], a, b);
+        top[r & 3] = fmaxf(top[r & 3], fmaxf(fabsf(a), fabsf(b)));
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+// whether an infinity or a NaN is among them: a sum of zeros otherwise
+template <int D>
+__device__ __forceinline__ bool all_finite(const u64 (&x)[D / 2]) {
+    u64 sum = pack2(0.f, 0.f);
+    const u64 zero = pack2(0.f, 0.f);
+#pragma unroll
+    for (int r = 0; r < D / 2; ++r) sum = fma2(x[r], zero, sum);
+    float a, b;
+    unpack2(sum, a, b);
+    return a + b == 0.f;
+}
+template <int D>
+__device__ __forceinline__ void store_bf16(uint32_t to, const u64 (&x)[D / 2]) {
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpack2(x[4 * c + i], a, b);
+            w[i] = bf16_pair(a, b);
+        }
+        shared_store(to + 16 * c, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+
+// pairs (i, i + R / 2), R known to the compiler so that the row stays in registers
+template <int D, int R>
+__device__ __forceinline__ void turn_halves(u64 (&x)[D / 2], const float* table) {
+#pragma unroll
+    for (int i = 0; i < R / 8; ++i) {
+        const uint4 c = load_plain(reinterpret_cast<const uint4*>(table) + i), s = load_plain(reinterpret_cast<const uint4*>(table + R / 2) + i);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u64 cc = h ? pack2u(c.z, c.w) : pack2u(c.x, c.y), ss = h ? pack2u(s.z, s.w) : pack2u(s.x, s.y), a = x[2 * i + h], b = x[R / 4 + 2 * i + h];
+            x[2 * i + h] = sub2(mul2(cc, a), mul2(ss, b)), x[R / 4 + 2 * i + h] = fma2(ss, a, mul2(cc, b));
+        }
+    }
+}
+template <int D, int R = D>
+__device__ __forceinline__ void turn_halves_of(int dims, u64 (&x)[D / 2], const float* table) {
+    if (dims == R) turn_halves<D, R>(x, table);
+    else if constexpr (R > 16) turn_halves_of<D, R - 16>(dims, x, table);
+}
+template <int D>
+__device__ __forceinline__ void turn_neighbours(int dims, u64 (&x)[D / 2], const float* table) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+        if (8 * i < dims) {
+            const float4 c = load_plain(reinterpret_cast<const float4*>(table) + i), s = load_plain(reinterpret_cast<const float4*>(table + dims / 2) + i);
+            const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float a, b;
+                unpack2(x[4 * i + r], a, b);
+                x[4 * i + r] = pack2(fmaf(a, cs[r], -b * sn[r]), fmaf(b, cs[r], a * sn[r]));
+            }
+        }
+}
+
+template <int D, bool F32, int BITS>
+struct AppendSmem {
+    static constexpr int kIn = D * (F32 ? 4 : 2), kInPitch = kIn + 16, kOutPitch = 2 * D + 16, kCodes = D * BITS / 8;
+    static constexpr uint32_t kTable = RowTurn<D, false>::kBytes, kNorms = kTable, kProducts = kNorms + 3 * D * 4;  // weights of queries, keys, ones
+    static constexpr uint32_t kWarps = kProducts + D * 4, kWarp = 32 * (kInPitch + kOutPitch);
+    static constexpr uint32_t bytes(int warps) { return kWarps + warps * kWarp; }
+};
+
+template <int D, bool F32, int BITS>
+__global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_append(const AppendParams p) {
+    using S = AppendSmem<D, F32, BITS>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    grid_dep_wait();
+    const int lane = threadIdx.x & 31;
+    const uint32_t table = smem_u32(smem), norms = table + S::kNorms, in = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp, out = in + 32 * S::kInPitch;
+    const int heads = p.q.heads + 2 * p.cache.heads, rows = static_cast<int>(p.tokens) * heads;  // rows of a token: queries, keys, values
+    Chunks chunks(rows);
+    // The lane's row of a chunk.  Found anew wherever it is needed, so that it takes no registers while the row is worked on.
+    struct Row {
+        int token, kind, head;  // 0 query, 1 key, 2 value, -1 none
+    };
+    auto find = [&](int chunk) {
+        const int row = chunk * 32 + lane;
+        Row r{row / heads, -1, 0};
+        if (row < 0 || row >= rows) return Row{0, -1, 0};
+        const int i = row - r.token * heads;
+        r.kind = i < p.q.heads ? 0 : (i < p.q.heads + p.cache.heads ? 1 : 2);
+        r.head = r.kind == 0 ? i : (r.kind == 1 ? i - p.q.heads : i - p.q.heads - p.cache.heads);
+        return r;
+    };
+    auto data_of = [&](const Row& r) {
+        const Heads& from = r.kind == 0 ? p.q : (r.kind == 1 ? p.k : p.v);
+        return from.data + (r.token * from.token + r.head * from.head) * (F32 ? 4 : 2);
+    };
+    auto fetch = [&](const Row& r) { each_chunk<S::kIn, S::kInPitch>(data_of(r), r.kind >= 0 ? S::kIn : 0, [&](uint32_t at, uint8_t* from) { copy_in(in + at, from); }); };
+    auto position_of = [&](const Row& r) { return p.positions != nullptr && (r.kind == 0 || r.kind == 1) ? load_plain(p.positions + r.token) : 0; };
+    auto angles_of = [&](int position) { return p.rope + (position >= 0 && position < p.rope_rows ? position : 0) * int64_t(p.rope_dims); };
+    auto prefetch = [&](const Row& r, int position) {  // a row's angles, into the cache
+        if (p.positions == nullptr || r.kind < 0 || r.kind > 1) return;
+        const float* at = angles_of(position);
+        for (int i = 0; i < p.rope_dims; i += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(at + i));
+    };
+    {
+        const Row first = find(chunks.there() ? chunks.at : -1);
+        fetch(first);
+        prefetch(first, position_of(first));
+    }
+    for (int i = threadIdx.x; i < D; i += blockDim.x) {
+        float* w = reinterpret_cast<float*>(smem + S::kNorms);
+        w[i] = p.q_norm != nullptr ? load_plain(p.q_norm + i) : 1.f, w[D + i] = p.k_norm != nullptr ? load_plain(p.k_norm + i) : 1.f, w[2 * D + i] = 1.f;
+    }
+    const bool scaled = RowTurn<D, false>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
+    const bool normed = p.q_norm != nullptr || p.k_norm != nullptr;
+    for (; chunks.there(); chunks.at += chunks.step) {
+        u64 x[D / 2];
+        copies_done();
+        __syncwarp();
+        const Row now = find(chunks.at), next = find(chunks.at + chunks.step < chunks.end ? chunks.at + chunks.step : -1);
+        const bool turned = p.positions != nullptr && (now.kind == 0 || now.kind == 1);
+        const int position = position_of(now), position_next = position_of(next);
+        if (turned && (position < 0 || position >= p.rope_rows)) atomicExch(p.status, kBadIndex);
+        const float* const angles = angles_of(position);
+        auto prepare = [&]() {  // norm and position
+            if (normed) {
+                u64 sum = pack2(0.f, 0.f);
+#pragma unroll
+                for (int r = 0; r < D / 2; ++r) sum = fma2(x[r], x[r], sum);
+                float a, b;
+                unpack2(sum, a, b);
+                const bool own = (now.kind == 0 && p.q_norm != nullptr) || (now.kind == 1 && p.k_norm != nullptr);
+                const float f = own ? rsqrtf((a + b) * (1.f / D) + p.eps) : 1.f;
+                const u64 f2 = pack2(f, f);
+                const uint32_t w = norms + (own ? now.kind : 2) * D * 4;
+#pragma unroll
+                for (int k = 0; k < D / 4; ++k) {
+                    const uint4 c = shared_load(w + 16 * k);
+                    x[2 * k] = mul2(x[2 * k], mul2(f2, pack2u(c.x, c.y))), x[2 * k + 1] = mul2(x[2 * k + 1], mul2(f2, pack2u(c.z, c.w)));
+                }
+            }
+            if (turned) {
+                if (p.interleaved) turn_neighbours<D>(p.rope_dims, x, angles);
+                else turn_halves_of<D>(p.rope_dims, x, angles);
+            }
+        };
+        constexpr int kPairs = F32 ? 2 : 4;  // of 16 bytes
+        for (bool plain = !scaled, again = false;; plain = again = true) {  // once, or again from memory in the plain form
+#pragma unroll
+            for (int c = 0; c < S::kIn / 16; ++c) {
+                uint4 v;
+                if (!again) v = shared_load(in + lane * S::kInPitch + 16 * c);
+                else v = now.kind >= 0 ? load_plain(reinterpret_cast<const uint4*>(data_of(now)) + c) : make_uint4(0, 0, 0, 0);
+                unpack_chunk<F32>(v, x + kPairs * c);
+            }
+            if (!again) {
+                __syncwarp();
+                fetch(next);
+            }
+            prepare();
+            if (!again) prefetch(next, position_next);
+            if (plain) RowTurn<D, false>::plain(x, p.tw);
+            else RowTurn<D, false>::scaled(x, table);
+            if (plain || __all_sync(0xFFFFFFFFu, now.kind < 0 || all_finite<D>(x))) break;
+        }
+        uint8_t* to = nullptr;
+        int bytes = 0;
+        if (now.kind == 0) {
+            store_bf16<D>(out + lane * S::kOutPitch, x);
+            to = const_cast<uint8_t*>(p.q_out.data) + (now.token * p.q_out.token + now.head * p.q_out.head) * 2, bytes = 2 * D;
+        } else if (now.kind > 0) {
+            constexpr float kTop = (1 << (BITS - 1)) - 1;
+            const float top = largest<D>(x), scale = fminf(top * (1.f / kTop), 65504.f);
+            const uint16_t stored = __half_as_ushort(__float2half_rn(scale));
+            const float s = half_value(stored), inv = s > 0.f ? __fdividef(1.f, s) : 0.f;
+            const u64 inv2 = pack2(inv, inv), magic = pack2(12582912.f, 12582912.f);  // the sum's low bits are the nearest integer
+            const bool clip = !(top * inv < kTop + 0.499f);                           // a scale that was rounded down far, or cut
+#pragma unroll
+            for (int c = 0; c < S::kCodes / 16; ++c) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    constexpr int kCodesOfWord = 32 / BITS;
+                    uint32_t v[kCodesOfWord];
+#pragma unroll
+                    for (int e = 0; e < kCodesOfWord; e += 2) {
+                        u64 y = mul2(x[((4 * c + i) * kCodesOfWord + e) / 2], inv2);
+                        if (clip) {
+                            float a, b;
+                            unpack2(y, a, b);
+                            y = pack2(fminf(fmaxf(a, -kTop - 1.f), kTop), fminf(fmaxf(b, -kTop - 1.f), kTop));
+                        }
+                        unpack2u(add2(y, magic), v[e], v[e + 1]);
+                    }
+                    if constexpr (BITS == 4) {
+                        uint32_t b[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) b[e] = (v[2 * e] & 15u) | (v[2 * e + 1] << 4);
+                        w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                    } else {
+                        w[i] = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
                     }
                 }
-            } else {
-                const int half = p.rope_dims / 16, other = turned ? (upper ? lane - half : lane + half) : lane;  // `half` lanes have a half
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float o = __shfl_sync(0xFFFFFFFFu, x[e], other);
-                    if (turned) x[e] = fmaf(x[e], cs[e], (upper ? o : -o) * sn[e]);
-                }
+                shared_store(out + lane * S::kOutPitch + 16 * c, make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            const int64_t slot = load_plain(p.slots + now.token), page = slot >> p.cache.page_shift;
+            if (slot >= 0 && page >= p.cache.pages) atomicExch(p.status, kBadIndex);
+            if (slot >= 0 && page < p.cache.pages) {
+                const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
+                const Half& half = now.kind == 1 ? p.cache.k : p.cache.v;
+                to = codes_of<S::kCodes>(half, p.cache.page_shift, page, now.head, place), bytes = S::kCodes;
+                *scale_of(half, p.cache.page_shift, page, now.head, place) = stored;
             }
         }
-        turn.apply(x);
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-#pragma unroll
-        for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        if (!there) continue;
-        if (kind == 0) {
-            const uint4 v = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
-            *reinterpret_cast<uint4*>(const_cast<uint8_t*>(p.q_out.data) + (at.token * p.q_out.token + head * p.q_out.head + 8 * l) * 2) = v;
-            continue;
-        }
-        const int64_t page = slot >> p.cache.page_shift;
-        if (slot < 0) continue;
-        if (page >= p.cache.pages) {
-            atomicExch(p.status, kBadIndex);
-            continue;
-        }
-        const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
-        const Half to = kind == 1 ? p.cache.k : p.cache.v;
-        float inv;
-        const uint16_t scale = row_scale(top, (1 << (BITS - 1)) - 1, &inv);
-        uint32_t w[BITS / 4];
-        codes8<BITS>(x, inv, w);
-        uint8_t* c = codes_of<D * BITS / 8>(to, p.cache.page_shift, page, head, place) + l * BITS;
-        if constexpr (BITS == 4) *reinterpret_cast<uint32_t*>(c) = w[0];
-        else *reinterpret_cast<uint2*>(c) = make_uint2(w[0], w[1]);
-        if (l == 0) *scale_of(to, p.cache.page_shift, page, head, place) = scale;
+        __syncwarp();
+        each_chunk<2 * D, S::kOutPitch>(to, bytes, [&](uint32_t at, uint8_t* dst) { *reinterpret_cast<uint4*>(dst) = shared_load(out + at); });
     }
 }
 
-struct ReadParams {
-    Cache cache;
-    const int64_t* slots;
-    const float2* tw;
-    uint8_t *k, *v;  // [tokens][heads][D]
-    int64_t tokens;
-    int* status;
+template <int D, bool F32, int BITS>
+struct ReadSmem {
+    static constexpr int kIn = D * BITS / 8, kInPitch = kIn + 16, kOut = D * (F32 ? 4 : 2), kOutPitch = kOut + 16;
+    static constexpr uint32_t kTable = RowTurn<D, true>::kBytes, kProducts = kTable, kWarps = kProducts + D * 4, kWarp = 32 * (kInPitch + kOutPitch);
+    static constexpr uint32_t bytes(int warps) { return kWarps + warps * kWarp; }
 };
 
 template <int D, bool F32, int BITS>
-__global__ void __launch_bounds__(kRowThreads) k_read(const ReadParams p) {
-    constexpr int kLanes = D / 8, kStep = kRowThreads / kLanes;
+__global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_read(const ReadParams p) {
+    using S = ReadSmem<D, F32, BITS>;
+    extern __shared__ __align__(16) uint8_t smem[];
     grid_dep_wait();
-    const int lane = threadIdx.x & 31, l = lane % kLanes;
-    const int heads = 2 * p.cache.heads;  // rows of a token: keys, values
-    struct Codes {
-        uint32_t w[2];
+    const int lane = threadIdx.x & 31;
+    const uint32_t table = smem_u32(smem), in = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp, out = in + 32 * S::kInPitch;
+    const int heads = 2 * p.cache.heads, rows = static_cast<int>(p.tokens) * heads;  // rows of a token: keys, values
+    Chunks chunks(rows);
+    struct Row {
+        const uint8_t* data;  // null: zeros
         uint16_t scale;
     };
-    auto slot_of = [&](const RowAt& a) { return a.there() ? load_plain(p.slots + a.token) : int64_t(-1); };
-    auto fetch = [&](const RowAt& a, int64_t slot) {
-        Codes c{};
-        const int64_t page = slot >> p.cache.page_shift;
-        if (slot < 0) return c;
+    auto find = [&](int chunk) {
+        Row r{};
+        const int row = chunk * 32 + lane;
+        if (row < 0 || row >= rows) return r;
+        const int token = row / heads, i = row - token * heads, head = i < p.cache.heads ? i : i - p.cache.heads;
+        const int64_t slot = load_plain(p.slots + token), page = slot >> p.cache.page_shift;
+        if (slot < 0) return r;
         if (page >= p.cache.pages) {
             atomicExch(p.status, kBadIndex);
-            return c;
+            return r;
         }
-        const bool is_k = a.r < p.cache.heads;
-        const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1), head = is_k ? a.r : a.r - p.cache.heads;
-        const Half from = is_k ? p.cache.k : p.cache.v;
-        const uint8_t* at = codes_of<D * BITS / 8>(from, p.cache.page_shift, page, head, place) + l * BITS;
-        if constexpr (BITS == 4) {
-            c.w[0] = load_plain(reinterpret_cast<const uint32_t*>(at));
-        } else {
-            const uint2 u = load_plain(reinterpret_cast<const uint2*>(at));
-            c.w[0] = u.x, c.w[1] = u.y;
-        }
-        c.scale = *static_cast<volatile const uint16_t*>(scale_of(from, p.cache.page_shift, page, head, place));
-        return c;
+        const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
+        const Half& half = i < p.cache.heads ? p.cache.k : p.cache.v;
+        r.data = codes_of<S::kIn>(half, p.cache.page_shift, page, head, place);
+        r.scale = *static_cast<volatile const uint16_t*>(scale_of(half, p.cache.page_shift, page, head, place));
+        return r;
     };
-    RowAt at, ahead;
-    at.start(p.tokens * heads, heads, kStep);
-    ahead = at;
-    ahead.next(heads, kStep);
-    Codes codes = fetch(at, slot_of(at)), codes_next{};
-    int64_t slot = slot_of(ahead);  // of the next row
-    Turn<D, 8, true> turn;
-    turn.load(p.tw, lane);
-    for (; __any_sync(0xFFFFFFFFu, at.there()); codes = codes_next) {
-        codes_next = fetch(ahead, slot);
-        const RowAt now = at;
-        at = ahead;
-        ahead.next(heads, kStep);
-        slot = slot_of(ahead);
-        const float s = half_value(codes.scale);
-        float x[8];
+    auto to_of = [&](int chunk) -> uint8_t* {
+        const int row = chunk * 32 + lane, token = row / heads, i = row - token * heads;
+        if (row >= rows) return nullptr;
+        return (i < p.cache.heads ? p.k : p.v) + (int64_t(token) * p.cache.heads + (i < p.cache.heads ? i : i - p.cache.heads)) * S::kOut;
+    };
+    auto fetch = [&](const Row& r) { each_chunk<S::kIn, S::kInPitch>(r.data, r.data != nullptr ? S::kIn : 0, [&](uint32_t at, uint8_t* from) { copy_in(in + at, from); }); };
+    Row now = find(chunks.there() ? chunks.at : -1);
+    fetch(now);
+    const bool scaled = RowTurn<D, true>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
+    for (; chunks.there(); chunks.at += chunks.step) {
+        copies_done();
+        __syncwarp();
+        uint4 raw[S::kIn / 16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = s * static_cast<float>(static_cast<int32_t>(codes.w[e * BITS / 32] << (32 - BITS - e * BITS % 32)) >> (32 - BITS));
-        turn.apply(x);
-        if (!now.there()) continue;
-        const bool is_k = now.r < p.cache.heads;
-        uint8_t* out = (is_k ? p.k : p.v) + ((now.token * p.cache.heads + (is_k ? now.r : now.r - p.cache.heads)) * D + 8 * l) * (F32 ? 4 : 2);
-        if constexpr (F32) {
-            reinterpret_cast<float4*>(out)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4*>(out)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-            *reinterpret_cast<uint4*>(out) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+        for (int c = 0; c < S::kIn / 16; ++c) raw[c] = now.data != nullptr ? shared_load(in + lane * S::kInPitch + 16 * c) : make_uint4(0, 0, 0, 0);
+        __syncwarp();
+        const Row next = find(chunks.at + chunks.step < chunks.end ? chunks.at + chunks.step : -1);
+        fetch(next);
+        // codes are at most 128 and scales at most 65504: the scaled form, at most 2^40 times that, stays finite
+        const float s = half_value(now.scale);
+        const u64 s2 = pack2(s, s), base = pack2(-8388608.f - (1 << (BITS - 1)), -8388608.f - (1 << (BITS - 1)));
+        u64 x[D / 2];
+#pragma unroll
+        for (int c = 0; c < S::kIn / 16; ++c) {
+            const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                constexpr int kCodesOfWord = 32 / BITS;
+                const uint32_t v = w[i] ^ (BITS == 4 ? 0x88888888u : 0x80808080u);  // code + 2^(bits - 1): low bits on top of 2^23
+#pragma unroll
+                for (int e = 0; e < kCodesOfWord; e += 2) {
+                    const uint32_t lo = (v >> (e * BITS)) & ((1u << BITS) - 1), hi = (v >> (e * BITS + BITS)) & ((1u << BITS) - 1);
+                    x[((4 * c + i) * kCodesOfWord + e) / 2] = mul2(s2, add2(pack2u(lo | 0x4B000000u, hi | 0x4B000000u), base));
+                }
+            }
         }
+        if (scaled) RowTurn<D, true>::scaled(x, table);
+        else RowTurn<D, true>::plain(x, p.tw);
+        if constexpr (F32) {
+#pragma unroll
+            for (int c = 0; c < D / 4; ++c) {
+                uint4 v;
+                unpack2u(x[2 * c], v.x, v.y), unpack2u(x[2 * c + 1], v.z, v.w);
+                shared_store(out + lane * S::kOutPitch + 16 * c, v);
+            }
+        } else {
+            store_bf16<D>(out + lane * S::kOutPitch, x);
+        }
+        __syncwarp();
+        uint8_t* const to = to_of(chunks.at);
+        each_chunk<S::kOut, S::kOutPitch>(to, to != nullptr ? S::kOut : 0, [&](uint32_t at, uint8_t* dst) { *reinterpret_cast<uint4*>(dst) = shared_load(out + at); });
+        now = next;
     }
 }
 
-// enough CTAs for every row, at most `per_sm` on an SM
-static dim3 row_grid(const bfq_plan* plan, int64_t rows, int rows_per_warp, int per_sm) {
-    const int64_t rows_per_cta = rows_per_warp * (kRowThreads / 32), want = (rows + rows_per_cta - 1) / rows_per_cta;
-    const int64_t most = int64_t(plan->sm_count) * per_sm;
-    return dim3(unsigned(want < most ? want : most));
+template <class S, class Kernel, class Params>
+static cudaError_t launch_rows(const bfq_plan* plan, Kernel kern, int* per_sm, int64_t rows, const Params& p, cudaStream_t st) {
+    int& occ = per_sm[plan->device];
+    if (occ == 0) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::bytes(kMostWarps)));
+        int n = 0;
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * kMostWarps, S::bytes(kMostWarps));
+        if (e != cudaSuccess) return e;
+        occ = n > 0 ? n : 1;
+    }
+    const int64_t want = (rows + 32 * kMostWarps - 1) / (32 * kMostWarps), most = int64_t(plan->sm_count) * occ;
+    return launch_overlapped(kern, dim3(unsigned(want < most ? want : most)), dim3(32 * kMostWarps), S::bytes(kMostWarps), st, p);
 }
+static bool few_rows(int64_t rows) { return rows < 65536; }
 
+template <int D, bool F32, int BITS>
+static cudaError_t launch_append_bits(const bfq_plan* plan, const AppendParams& p, cudaStream_t st) {
+    static int per_sm[kMaxDevices] = {0};
+    return launch_rows<AppendSmem<D, F32, BITS>>(plan, k_append<D, F32, BITS>, per_sm, p.tokens * (p.q.heads + 2 * p.cache.heads), p, st);
+}
 template <int D, bool F32>
 static cudaError_t launch_append(const bfq_plan* plan, const AppendParams& p, cudaStream_t st) {
-    const dim3 grid = row_grid(plan, p.tokens * (p.q.heads + 2 * p.cache.heads), 256 / D, 4);
-    return p.cache.bits == 4 ? launch_overlapped(k_append<D, F32, 4>, grid, dim3(kRowThreads), 0, st, p)
-                             : launch_overlapped(k_append<D, F32, 8>, grid, dim3(kRowThreads), 0, st, p);
+    if (few_rows(p.tokens * (p.q.heads + 2 * p.cache.heads))) return append_few_launch(plan, p, F32, st);
+    return p.cache.bits == 4 ? launch_append_bits<D, F32, 4>(plan, p, st) : launch_append_bits<D, F32, 8>(plan, p, st);
+}
+template <int D, bool F32, int BITS>
+static cudaError_t launch_read_bits(const bfq_plan* plan, const ReadParams& p, cudaStream_t st) {
+    static int per_sm[kMaxDevices] = {0};
+    return launch_rows<ReadSmem<D, F32, BITS>>(plan, k_read<D, F32, BITS>, per_sm, p.tokens * 2 * p.cache.heads, p, st);
 }
 template <int D, bool F32>
 static cudaError_t launch_read(const bfq_plan* plan, const ReadParams& p, cudaStream_t st) {
-    const dim3 grid = row_grid(plan, p.tokens * 2 * p.cache.heads, 256 / D, 4);
-    return p.cache.bits == 4 ? launch_overlapped(k_read<D, F32, 4>, grid, dim3(kRowThreads), 0, st, p)
-                             : launch_overlapped(k_read<D, F32, 8>, grid, dim3(kRowThreads), 0, st, p);
+    if (few_rows(p.tokens * 2 * p.cache.heads)) return read_few_launch(plan, p, F32, st);
+    return p.cache.bits == 4 ? launch_read_bits<D, F32, 4>(plan, p, st) : launch_read_bits<D, F32, 8>(plan, p, st);
 }
 
 }  // namespace kv
@@ -315,7 +540,7 @@ extern "C" int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const in
     int rc = kv::check_cache(plan, cache, &p.cache);
     if (rc != BFQ_OK) return rc;
     if (xt != BFQ_F32 && xt != BFQ_BF16) return BFQ_ERR_DTYPE;
-    if (tokens < 0 || tokens >= int64_t(1) << 40) return BFQ_ERR_STRIDE;
+    if (tokens < 0 || tokens >= int64_t(1) << 31) return BFQ_ERR_STRIDE;
     if (tokens == 0) return BFQ_OK;
     if (slots == nullptr || k == nullptr || v == nullptr || (q == nullptr) != (q_out == nullptr)) return BFQ_ERR_NULL;
     const int n = plan->n, esize = xt == BFQ_F32 ? 4 : 2;
@@ -324,6 +549,7 @@ extern "C" int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const in
     if (rc == BFQ_OK && q != nullptr) rc = kv::check_heads(q, n, esize, &p.q);
     if (rc == BFQ_OK && q != nullptr) rc = kv::check_heads(q_out, n, 2, &p.q_out);
     if (rc != BFQ_OK) return rc;
+    if (tokens * (p.q.heads + 2 * int64_t(cache->heads)) >= (int64_t(1) << 31) - 64) return BFQ_ERR_STRIDE;
     if (k->heads != cache->heads || v->heads != cache->heads || (q != nullptr && q_out->heads != q->heads)) return BFQ_ERR_STRIDE;
     if ((reinterpret_cast<uintptr_t>(slots) & 7u) != 0) return BFQ_ERR_ALIGN;
     if (at != nullptr) {
@@ -352,7 +578,7 @@ extern "C" int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int6
     const int rc = kv::check_cache(plan, cache, &p.cache);
     if (rc != BFQ_OK) return rc;
     if (t != BFQ_F32 && t != BFQ_BF16) return BFQ_ERR_DTYPE;
-    if (tokens < 0 || tokens >= int64_t(1) << 40) return BFQ_ERR_STRIDE;
+    if (tokens < 0 || tokens >= int64_t(1) << 31 || tokens * cache->heads >= int64_t(1) << 30) return BFQ_ERR_STRIDE;
     if (tokens == 0) return BFQ_OK;
     if (slots == nullptr || k == nullptr || v == nullptr) return BFQ_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(slots) & 7u) != 0 || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) != 0) return BFQ_ERR_ALIGN;

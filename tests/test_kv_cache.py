@@ -168,6 +168,69 @@ def test_append(n, bits, page, dtype, hq, hkv, tokens, norm, dims, interleaved):
         assert torch.equal(now, old), name
 
 
+def check_nearest(codes, scales, y, bits):
+    """Every code is a nearest one, up to 1e-4 of a step, on a scale within one fp16 step: check_quant without its count of codes next to a
+    boundary.  Angles that are multiples of pi / 2 in fp32 have cosines of some 4e-8, so a rotated bf16 row is its elements to that part, and those
+    lie on exact ties k + 1/2 of the fp16 scale in bulk: which side they fall on is below fp32's 2^-24 = 6e-8, and both are right."""
+    got, s = oracle.unpack(codes.cpu().numpy(), bits).astype(np.float64), to_f64(scales)
+    top = 2.0 ** (bits - 1) - 1
+    want = np.minimum(np.abs(y).max(1) / top, 65504)
+    assert (np.abs(s - want) <= 2.0 ** -10 * want + 2.0 ** -25).all()
+    pre = np.clip(y / np.where(s > 0, s, np.inf)[:, None], -top - 1, top)
+    assert (np.abs(got - pre) <= 0.5 + 1e-4).all()
+
+
+MANY = [(128, 4, 64, torch.bfloat16, 8, 4), (128, 8, 32, torch.float32, 5, 1), (64, 8, 16, torch.bfloat16, 3, 1), (64, 4, 128, torch.float32, 30, 5)]
+
+
+@gpu
+@pytest.mark.parametrize("n,bits,page,dtype,hq,hkv", MANY)
+@pytest.mark.parametrize("angles,size", [("normal", 1.0), ("right", 1.0), ("normal", 1e30), ("normal", 1e-30)])
+def test_append_and_read_many(n, bits, page, dtype, hq, hkv, angles, size):
+    """Rows enough for the kernels that batches of prompts take, also with angles whose cosines vanish, and rows that are very large or small
+    (a scale stops at 65504, and is zero below fp16's smallest number)."""
+    p, theta = make_plan(n)
+    if angles == "right":
+        theta = np.pi / 2 * np.random.default_rng(1).integers(-2, 3, theta.shape).astype(np.float64)
+        theta = theta.astype(np.float32).astype(np.float64)
+        p.set_angles(torch.from_numpy(theta.astype(np.float32)).to(DEV))
+    tokens = 65700 // (hq + 2 * hkv) + 3
+    g = torch.Generator().manual_seed(17)
+    qkv = size * torch.randn((tokens, hq + 2 * hkv, n), generator=g)
+    qkv[5] *= 1e-3
+    qkv[7, :, :] = 0
+    qkv = qkv.to(dtype)
+    dev = qkv.to(DEV)
+    cache = KVCache.empty(tokens // page + 2, hkv, n, page, bits, DEV)
+    slots = torch.randperm(cache.pages * page, generator=g)[:tokens]
+    slots[1::9] = -1
+    table, positions = rope_table(300, n // 2), torch.randint(0, 300, (tokens,), generator=g, dtype=torch.int32)
+    norm = size == 1.0
+    w = 1 + 0.3 * torch.randn((2, n), generator=g)
+    some = dict(q_norm=w[0].to(DEV), k_norm=w[1].to(DEV)) if norm else {}
+    q = p.append_kv(cache, dev[:, hq:hq + hkv], dev[:, hq + hkv:], slots.to(DEV), q=dev[:, :hq], positions=positions.to(DEV), rope=table.to(DEV), **some)
+    assert p.device_status() == 0
+    x = to_f64(qkv)
+    turn = lambda t, weight: positioned(t, to_f64(weight) if norm else None, 1e-6, positions.numpy(), to_f64(table), False)
+    wq = oracle.forward(theta, turn(x[:, :hq], w[0]).reshape(-1, n)).reshape(tokens, hq, n)
+    assert (np.abs(to_f64(q) - wq) <= 2.0 ** -8 * np.abs(wq) + 1e-5 * np.linalg.norm(wq, axis=-1, keepdims=True) + 1e-37).all()
+    keep = (slots >= 0).numpy()
+    at = slots[slots >= 0].to(DEV)
+    got = p.read_kv(cache, slots.to(DEV), torch.float32), p.read_kv(cache, slots.to(DEV))
+    for i, (which, ref) in enumerate((("k", turn(x[:, hq:hq + hkv], w[1])), ("v", x[:, hq + hkv:]))):
+        codes, scales = rows_at(cache, which, at)
+        y = oracle.forward(theta, ref[keep].reshape(-1, n))
+        (check_quant if angles != "right" else check_nearest)(codes.reshape(-1, codes.shape[-1]), scales.reshape(-1), y, bits)
+        rows = np.zeros((tokens, hkv, n))
+        rows[keep] = oracle.dequantize(oracle.unpack(codes.reshape(-1, codes.shape[-1]).cpu().numpy(), bits),
+                                       scales.reshape(-1).cpu().view(torch.int16).numpy().view(np.uint16)).reshape(-1, hkv, n)
+        back = oracle.inverse(theta, rows.reshape(-1, n)).reshape(rows.shape)
+        tol = 1e-5 * np.linalg.norm(rows, axis=-1, keepdims=True)
+        assert (np.abs(to_f64(got[0][i]) - back) <= tol).all()
+        assert (np.abs(to_f64(got[1][i]) - back) <= tol + 2.0 ** -8 * np.abs(back)).all()
+    assert p.device_status() == 0
+
+
 @gpu
 def test_append_without_queries_and_in_place():
     p, theta = make_plan(128)
