@@ -9,11 +9,15 @@
 // at most 8 (a factor of 256) below the largest score so far, so that it, the sum and the products change only when a score passes it by more
 // than that.
 //
-// A CTA of four warps takes units of 64 keys, 16 keys to a warp, through a ring of stages that cp.async fills some units ahead
-// (16-byte chunks, chunk i of a unit at place i ^ (i / 8 mod 8): the reads below hit every bank once).  mma.m16n8k16: the 16 rows are
-// the queries of a key head's group.  Keys come as words of a row, 8 (4) codes at a time; which k index of the product an element gets is
+// A CTA of four warps takes units of 128 keys, 32 keys to a warp, from a ring of stages that TMA fills ahead (a box for each page and half,
+// swizzled so that the reads below hit every bank once).  mma.m16n8k16 with the keys, then the values' elements, as its 16 rows and 8 queries
+// as its columns: with the queries as rows a group of four would leave three quarters of the tensor cores' work idle and twice
+// the registers taken.  Keys come as words of a row, 8 (4) codes at a time; which k index of the product an element gets is
 // free as long as the queries' fragments have the same order, so no code moves between lanes.  Values come by ldmatrix.trans on 16-bit
-// units of 4 (2) codes: the halves of a register are two keys' codes of the same elements, which is what the second product needs.
+// units of 4 (2) codes: the halves of a register are two keys' codes of the same element, which is what the second product needs of its
+// left operand; the probabilities, keys by queries, are turned by movmatrix into its right one.
+//
+// What bounds it: instructions, some two thirds of them codes to fp16 (9 for 8 codes of 4 bits, 10 for 8 of 8).
 #include "bfq_kvattn.cuh"
 #include "bfq_n4096.cuh"
 
@@ -22,28 +26,17 @@ namespace kv {
 
 constexpr int kWarps = 4, kAttendThreads = 32 * kWarps;
 
-template <int D, int BITS>
+template <int D, int BITS, int NB>
 struct Stage {
-    static constexpr int kRow = D * BITS / 8;             // bytes of a row's codes
-    static constexpr int kChunks = kFewUnit * kRow / 16;     // of a unit's keys (and as many of its values)
-    static constexpr int kScales = 2 * kFewUnit * kRow;      // keys' scales behind both, then the values'
-    static constexpr int kBytes = kScales + 4 * kFewUnit;
-    static constexpr int kCount = kBytes > 12000 ? 4 : 6;
+    static constexpr int kRow = D * BITS / 8;              // bytes of a row's codes
+    static constexpr uint32_t kScales = 2 * kUnit * kRow;  // keys' scales behind both halves' codes, then the values'
+    static constexpr uint32_t kBytes = (kScales + 4 * kUnit + 1023) / 1024 * 1024;
+    static constexpr int kCount = 2;  // 3 stages: 108 us where 2 and four CTAs on an SM take 102 (64 sequences, 276 K keys, 4 bits)
+    static constexpr int kPitch = D + 4;                   // of a merged row, floats
+    static constexpr uint32_t kMerge = kCount * kBytes, kSums = kMerge + 2 * 8 * NB * kPitch * 4, kBars = kSums + kWarps * 8 * NB * 8;
+    static constexpr uint32_t kSmem = kBars + 2 * kCount * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
-constexpr int kMergeRows = 2 * kFewRows;
-template <int D, int BITS>
-constexpr size_t attend_smem() {
-    return size_t(Stage<D, BITS>::kCount) * Stage<D, BITS>::kBytes + sizeof(float) * kMergeRows * (D + 4) + 4 * kFewRows * sizeof(float2);
-}
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -51,6 +44,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t at) {
     uint4 v;
@@ -62,73 +60,84 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t lds32(uint32_t at) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ float lds_half(uint32_t at) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+    return half_value(v);
 }
-template <int D, int BITS>
-__global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p) {
-    using S = Stage<D, BITS>;
-    constexpr int kSteps = D / 16, kTilesD = D / 8;
-    extern __shared__ __align__(128) uint8_t smem[];
-    float* const merge = reinterpret_cast<float*>(smem + S::kCount * S::kBytes);  // [2][16][D + 4]
-    float2* const warp_sums = reinterpret_cast<float2*>(merge + kMergeRows * (D + 4));
-    __shared__ long long scan[kWarps + 3];
-    const uint32_t ring = smem_u32(smem);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    grid_dep_wait();
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
+// NB: blocks of 8 queries
+template <int D, int BITS, int NB>
+__global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using S = Stage<D, BITS, NB>;
+    constexpr int kSteps = D / 16, kRows = 8 * NB;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ long long scan[kWarps + 2];
+    __shared__ volatile int dead;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    float* const merge = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kMerge);  // [2][rows][pitch]
+    float2* const warp_sums = reinterpret_cast<float2*>(smem_raw + (base - smem_u32(smem_raw)) + S::kSums);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    auto full = [&](int s) { return base + S::kBars + 8u * s; };
+    auto empty = [&](int s) { return base + S::kBars + 8u * (S::kCount + s); };
+    grid_dep_wait();
     const Part& part = p.few;
-    Walk<kFewRows, kFewUnit> ahead;
+    Walk ahead;
     const Run run = find_run<kAttendThreads>(p, part, scan, &ahead);
     if (run.count == 0) return;
-    Walk<kFewRows, kFewUnit> now = ahead;
-    const int count = run.count, heads = p.cache.heads;
+    Walk now = ahead;
+    const int count = run.count;
+    if (tid == 0) {
+        for (int s = 0; s < S::kCount; ++s) mbar_init(full(s), 1), mbar_init(empty(s), kWarps);
+        mbar_init_fence();
+        dead = 0;
+    }
+    __syncthreads();
 
-    // ---- copies ----------------------------------------------------------------------------------------------------------
+    // ---- the first warp sends for units, a page to a lane -------------------------------------------------------------------
     auto fetch = [&](int i) {
-        if (i < count) {
-            const uint32_t stage = ring + (i % S::kCount) * S::kBytes;
-            const int key0 = ahead.unit * kFewUnit;
-            const int mask = (1 << p.cache.page_shift) - 1;
-#pragma unroll
-            for (int c = 0; c < S::kChunks; c += kAttendThreads) {
-                const int i16 = c + tid;
-                if (S::kChunks % kAttendThreads != 0 && i16 >= S::kChunks) break;
-                const int key = key0 + i16 / (S::kRow / 16), part = i16 % (S::kRow / 16);
-                const int64_t found = key < ahead.tile.keys ? page_of(p, ahead.tile, key) : -1, page = found < 0 ? 0 : found;
-                const bool there = found >= 0;  // else zeros
-                const uint32_t dst = stage + 16 * (i16 ^ ((i16 >> 3) & 7));
-                copy16(dst, codes_of<S::kRow>(p.cache.k, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
-                copy16(dst + kFewUnit * S::kRow, codes_of<S::kRow>(p.cache.v, p.cache.page_shift, page, ahead.head, key & mask) + 16 * part, there);
-            }
-            if (tid < 2 * kFewUnit / 8) {
-                const int key = key0 + 8 * (tid % (kFewUnit / 8));
-                const bool values = tid >= kFewUnit / 8;
-                const int64_t found = key < ahead.tile.keys ? page_of(p, ahead.tile, key) : -1, page = found < 0 ? 0 : found;
-                const bool there = found >= 0;
-                copy16(stage + S::kScales + 16 * tid, scale_of(values ? p.cache.v : p.cache.k, p.cache.page_shift, page, ahead.head, key & mask), there);
-            }
-            ahead.next(p, part);
+        if (warp != 0 || i >= count) return;
+        const int s = i % S::kCount;
+        if (i >= S::kCount) wait_for(empty(s), (i / S::kCount - 1) & 1, &dead, p.status);
+        const int page_keys = 1 << p.cache.page_shift, box = page_keys < kUnit ? page_keys : kUnit;
+        const int key = ahead.unit * kUnit + lane * box;
+        const bool there = lane * box < kUnit && key < ahead.tile.keys;
+        const uint32_t stage = base + s * S::kBytes;
+        if (lane == 0) {
+            const int left = ahead.tile.keys - ahead.unit * kUnit, boxes = ((left < kUnit ? left : kUnit) + box - 1) / box;
+            mbar_expect_tx(full(s), boxes * box * (2 * S::kRow + 4));
         }
-        copies_commit();
+        __syncwarp();
+        if (there) {
+            const int64_t found = page_of(p, ahead.tile, key), page = found < 0 ? 0 : found;
+            const int row = (ahead.head << p.cache.page_shift) + (key & (page_keys - 1));
+            tma_load_3d(stage + lane * box * S::kRow, &k_map, 0, row, static_cast<int>(page), full(s));
+            tma_load_3d(stage + (kUnit + lane * box) * S::kRow, &v_map, 0, row, static_cast<int>(page), full(s));
+            bulk_load(stage + S::kScales + lane * box * 2, p.cache.k.scales + page * p.cache.k.scales_page + row, box * 2, full(s));
+            bulk_load(stage + S::kScales + (kUnit + lane * box) * 2, p.cache.v.scales + page * p.cache.v.scales_page + row, box * 2, full(s));
+        }
+        __syncwarp();
+        ahead.next(p, part);
     };
 #pragma unroll
     for (int i = 0; i < S::kCount - 1; ++i) fetch(i);
+    // place of a 16-byte chunk, numbered row by row, in a swizzled half of a stage
+    auto place = [](int i16) { return 16u * (i16 ^ ((i16 >> 3) & (S::kRow / 16 - 1))); };
 
     // ---- a pair's state: fragments of the queries, reference, sums and products -------------------------------------------
-    uint32_t qa[kSteps][4];
-    float m[2], l[2], o[kTilesD][4];
-    float row_scale_log2[2];  // softmax scale * log2 e over the row's power of two
-    float u_top, u_unit;      // power of two that no u so far passes; 128 / u_top: probabilities (at most 2^8) times u stay below 2^15
-    int limit[2];             // keys of rows g and g + 8
-    bool two;                 // there are rows 8 and up
+    uint32_t qb[NB][kSteps][2];
+    float m[NB][2], l[NB][2], o[NB][kSteps][4];  // of queries 8 b + 2 t and + 1; o: element rows of 16
+    float row_scale_log2[NB][2];                 // softmax scale * log2 e over the row's power of two
+    int limit[NB][2];                            // keys of the row
+    float u_top, u_unit;  // power of two that no u so far passes; 128 / u_top: probabilities (at most 2^8) times u stay below 2^15
     auto open = [&]() {
         const Tile& tl = now.tile;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = g + 8 * half, row = tl.row0 + r;
+        for (int b = 0; b < NB; ++b) {
+            const int r = 8 * b + g, row = tl.row0 + r;  // the row that the lane holds a part of
             const bool there = r < tl.rows;
             const int token = tl.token0 + row / p.group, head = now.head * p.group + row % p.group;
             const uint4* at = reinterpret_cast<const uint4*>(p.q.data + (there ? (token * p.q.token + head * p.q.head + t * (D / 4)) * 2 : 0));
@@ -144,75 +153,86 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             const RowPower power(top);
-            row_scale_log2[half] = p.scale_log2 * power.down;
             auto element = [&](int i) { return power.up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
             auto pair = [&](int i, int j) { return half_pair(element(i), element(j)); };
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 if constexpr (BITS == 4) {
                     const int d = 8 * (s / 2) + 2 * (s & 1);
-                    qa[s][half] = pair(d, d + 4), qa[s][2 + half] = pair(d + 1, d + 5);
+                    qb[b][s][0] = pair(d, d + 4), qb[b][s][1] = pair(d + 1, d + 5);
                 } else {
-                    qa[s][half] = pair(4 * s, 4 * s + 2), qa[s][2 + half] = pair(4 * s + 1, 4 * s + 3);
+                    qb[b][s][0] = pair(4 * s, 4 * s + 2), qb[b][s][1] = pair(4 * s + 1, 4 * s + 3);
                 }
             }
-            m[half] = -INFINITY, l[half] = 0.f;
-            const int own = tl.last0 + row / p.group + 1;
-            limit[half] = there ? (own < tl.keys ? own : tl.keys) : 0;
+            const int own = tl.last0 + row / p.group + 1, keys = there ? (own < tl.keys ? own : tl.keys) : 0;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {  // from the lanes of the rows that this lane's columns are
+                row_scale_log2[b][c] = p.scale_log2 * __shfl_sync(0xFFFFFFFFu, power.down, 4 * (2 * t + c));
+                limit[b][c] = __shfl_sync(0xFFFFFFFFu, keys, 4 * (2 * t + c));
+                m[b][c] = -INFINITY, l[b][c] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[b][i][j] = 0.f;
         }
-        two = tl.rows > 8, u_top = 0.f, u_unit = 0.f;
-#pragma unroll
-        for (int i = 0; i < kTilesD; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+        u_top = 0.f, u_unit = 0.f;
     };
     long long pair_from = run.from - now.unit;  // number of the pair's unit 0
-    auto close = [&](long long done) {      // after unit `done` (exclusive) of the numbering
+    auto close = [&](long long done) {          // after unit `done` (exclusive) of the numbering
         const int pair = now.pair(p);
         const long long entry = blockIdx.x + pair;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 1);
-            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 2);
-            if (t == 0) warp_sums[warp * kFewRows + g + 8 * half] = make_float2(m[half], l[half]);
-        }
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[b][c] += __shfl_xor_sync(0xFFFFFFFFu, l[b][c], x);
+                if (g == 0) warp_sums[warp * kRows + 8 * b + 2 * t + c] = make_float2(m[b][c], l[b][c]);
+            }
         __syncthreads();
-        float f[2];
+        float f[NB][2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float top = -INFINITY, sum = 0.f;
-            float2 ml[kWarps];
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) ml[w] = warp_sums[w * kFewRows + g + 8 * half], top = fmaxf(top, ml[w].x);
-            const float safe = top == -INFINITY ? 0.f : top;
+            for (int c = 0; c < 2; ++c) {
+                const int r = 8 * b + 2 * t + c;
+                float top = -INFINITY, sum = 0.f;
+                float2 ml[kWarps];
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) sum += ml[w].y * exp2_fast(ml[w].x - safe);
-            f[half] = exp2_fast(m[half] - safe) * (u_top * (1.f / 128.f));
-            if (warp == 0 && t == 0 && g + 8 * half < now.tile.rows) part.sums[entry * kFewRows + g + 8 * half] = make_float2(top, sum);
-        }
-        // d of accumulator i, column 2 t + j: see the values' order below
-        auto column = [&](int i, int j) {
-            constexpr int kPer = 32 / BITS / 2;  // codes of a 16-bit unit
-            return (i / kPer) * 8 * kPer + kPer * (2 * t + j) + i % kPer;
+                for (int w = 0; w < kWarps; ++w) ml[w] = warp_sums[w * kRows + r], top = fmaxf(top, ml[w].x);
+                const float safe = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) sum += ml[w].y * exp2_fast(ml[w].x - safe);
+                f[b][c] = exp2_fast(m[b][c] - safe) * (u_top * (1.f / 128.f));
+                if (warp == 0 && g == 0 && r < now.tile.rows) part.sums[entry * kRows + r] = make_float2(top, sum);
+            }
+        // element of accumulator i, row g + 8 j: see the values' order below
+        auto element_of = [&](int i, int j) {
+            constexpr int kPer = 16 / BITS;  // codes of a 16-bit unit
+            const int n = 2 * i + j;         // chunk n / kPer, unit g, code n % kPer of the unit
+            return (n / kPer) * 8 * kPer + kPer * g + n % kPer;
         };
         auto put = [&](float* to, bool add) {
 #pragma unroll
-            for (int i = 0; i < kTilesD; ++i)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float* at = to + (g + 8 * (j >> 1)) * (D + 4) + column(i, j & 1);
-                    const float v = o[i][j] * f[j >> 1];
-                    *at = add ? *at + v : v;
-                }
+                for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float* at = to + (8 * b + 2 * t + (j & 1)) * S::kPitch + element_of(i, j >> 1);
+                        const float v = o[b][i][j] * f[b][j & 1];
+                        *at = add ? *at + v : v;
+                    }
         };
-        if (warp >= 2) put(merge + (warp - 2) * kFewRows * (D + 4), false);
+        if (warp >= 2) put(merge + (warp - 2) * kRows * S::kPitch, false);
         __syncthreads();
-        if (warp < 2) put(merge + warp * kFewRows * (D + 4), true);
+        if (warp < 2) put(merge + warp * kRows * S::kPitch, true);
         __syncthreads();
         for (int i = tid; i < now.tile.rows * (D / 4); i += kAttendThreads) {
             const int r = i / (D / 4), c = 4 * (i % (D / 4));
-            const float4 a = *reinterpret_cast<const float4*>(merge + r * (D + 4) + c), b = *reinterpret_cast<const float4*>(merge + (kFewRows + r) * (D + 4) + c);
-            *reinterpret_cast<float4*>(part.parts + (entry * kFewRows + r) * D + c) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+            const float4 a = *reinterpret_cast<const float4*>(merge + r * S::kPitch + c), b = *reinterpret_cast<const float4*>(merge + (kRows + r) * S::kPitch + c);
+            *reinterpret_cast<float4*>(part.parts + (entry * kRows + r) * D + c) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
         }
         if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + now.units - 1) / run.per - blockIdx.x + 1));
         pair_from = done;
@@ -220,126 +240,129 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p)
 
     open();
     for (int i = 0; i < count; ++i) {
-        copies_wait<S::kCount - 2>();
-        __syncthreads();
         fetch(i + S::kCount - 1);
-        const uint32_t stage = ring + (i % S::kCount) * S::kBytes;
-        const int key0 = now.unit * kFewUnit + 16 * warp;
-        // ---- scores of 16 keys: key 8 j + g of the warp's is column g of tile j
-        float s[2][4];
+        wait_for(full(i % S::kCount), (i / S::kCount) & 1, &dead, p.status);
+        const uint32_t stage = base + (i % S::kCount) * S::kBytes;
+        const int key0 = now.unit * kUnit + 32 * warp;
+        // ---- scores of 32 keys: rows g and g + 8 of product j are keys 16 j + g and 16 j + 8 + g of the warp's
+        float s[NB][2][4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int key = 16 * warp + 8 * j + g;
-            constexpr int kWords = D * BITS / 128;  // of a lane
-            uint32_t w[kWords];
-            if constexpr (kWords == 2) {
-                const int i16 = key * (S::kRow / 16) + (t >> 1);
-                const uint2 v = lds64(stage + 16 * (i16 ^ ((i16 >> 3) & 7)) + 8 * (t & 1));
-                w[0] = v.x, w[1] = v.y;
-            } else {
+            constexpr int kWords = D * BITS / 128;  // of a lane and key
+            uint32_t w[2][kWords];
 #pragma unroll
-                for (int c = 0; c < kWords / 4; ++c) {
-                    const int i16 = key * (S::kRow / 16) + t * (kWords / 4) + c;
-                    const uint4 v = lds128(stage + 16 * (i16 ^ ((i16 >> 3) & 7)));
-                    w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
+            for (int h = 0; h < 2; ++h) {
+                const int key = 32 * warp + 16 * j + 8 * h + g;
+                if constexpr (kWords == 2) {
+                    const uint2 v = lds64(stage + place(key * (S::kRow / 16) + (t >> 1)) + 8 * (t & 1));
+                    w[h][0] = v.x, w[h][1] = v.y;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kWords / 4; ++c) {
+                        const uint4 v = lds128(stage + place(key * (S::kRow / 16) + t * (kWords / 4) + c));
+                        w[h][4 * c] = v.x, w[h][4 * c + 1] = v.y, w[h][4 * c + 2] = v.z, w[h][4 * c + 3] = v.w;
+                    }
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[j][c] = 0.f;
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[b][j][c] = 0.f;
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
-                uint32_t b0, b1;
-                if constexpr (BITS == 4) b0 = pair4(w[st / 2], 2 * (st & 1)), b1 = pair4(w[st / 2], 2 * (st & 1) + 1);
-                else b0 = pair8(w[st], 0), b1 = pair8(w[st], 1);
-                mma16816(s[j], qa[st][0], qa[st][1], qa[st][2], qa[st][3], b0, b1);
+                uint32_t a[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (BITS == 4) a[h] = pair4(w[h][st / 2], 2 * (st & 1)), a[2 + h] = pair4(w[h][st / 2], 2 * (st & 1) + 1);
+                    else a[h] = pair8(w[h][st], 0), a[2 + h] = pair8(w[h][st], 1);
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) mma16816(s[b][j], a[0], a[1], a[2], a[3], qb[b][st][0], qb[b][st][1]);
             }
         }
         // ---- scales, masks, probabilities
-        float u[2][2];
+        float u[4];  // keys 8 x + g
         bool over = false;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t at = stage + S::kScales + 2 * (16 * warp + 8 * j + 2 * t);
-            const uint32_t ks = lds32(at), vs = lds32(at + 2 * kFewUnit);
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t at = stage + S::kScales + 2 * (32 * warp + 8 * x + g);
+            const int key = key0 + 8 * x + g;
+            const float f = lds_half(at);
+            u[x] = key < now.tile.keys ? lds_half(at + 2 * kUnit) : 0.f;
+            over |= u[x] > u_top;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int key = key0 + 8 * j + 2 * t + c;
-                const float f = half_value(static_cast<uint16_t>(ks >> (16 * c)));
-                u[j][c] = key < now.tile.keys ? half_value(static_cast<uint16_t>(vs >> (16 * c))) : 0.f;
-                over |= u[j][c] > u_top;
-                s[j][c] = key < limit[0] ? s[j][c] * f * row_scale_log2[0] : -INFINITY;
-                over |= s[j][c] > m[0] + 8.f;
-                if (two) {
-                    s[j][2 + c] = key < limit[1] ? s[j][2 + c] * f * row_scale_log2[1] : -INFINITY;
-                    over |= s[j][2 + c] > m[1] + 8.f;
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float& v = s[b][x >> 1][2 * (x & 1) + c];
+                    v = key < limit[b][c] ? v * f * row_scale_log2[b][c] : -INFINITY;
+                    over |= v > m[b][c] + 8.f;
                 }
-            }
         }
         if (__any_sync(0xFFFFFFFFu, over)) {
-            float most = fmaxf(fmaxf(u[0][0], u[0][1]), fmaxf(u[1][0], u[1][1]));
-            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+            float most = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3]));
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, x));
             float less = 1.f;  // on the products
             if (most > u_top) {
                 const float top = __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u);  // above it
                 less = u_top / top, u_top = top, u_unit = 128.f / top;
             }
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float f = 1.f;
-                if (half == 0 || two) {
-                    float top = fmaxf(fmaxf(s[0][2 * half], s[0][2 * half + 1]), fmaxf(s[1][2 * half], s[1][2 * half + 1]));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                    top = fmaxf(top, m[half]);
-                    f = top == -INFINITY ? 1.f : exp2_fast(m[half] - top);
-                    m[half] = top, l[half] *= f;
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float top = fmaxf(fmaxf(s[b][0][c], s[b][0][2 + c]), fmaxf(s[b][1][c], s[b][1][2 + c]));
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                    top = fmaxf(top, m[b][c]);
+                    const float f = top == -INFINITY ? 1.f : exp2_fast(m[b][c] - top);
+                    m[b][c] = top, l[b][c] *= f;
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k) o[b][k][c] *= f * less, o[b][k][2 + c] *= f * less;
                 }
-                f *= less;
-#pragma unroll
-                for (int i = 0; i < kTilesD; ++i) o[i][2 * half] *= f, o[i][2 * half + 1] *= f;
-            }
         }
-        uint32_t pa[4] = {0, 0, 0, 0};
+        uint32_t pb[NB][4];  // keys 8 x + 2 t and + 1 of query 8 b + g
 #pragma unroll
-        for (int j = 0; j < 2; ++j) u[j][0] *= u_unit, u[j][1] *= u_unit;
+        for (int b = 0; b < NB; ++b) {
+            const float r0 = m[b][0] == -INFINITY ? 0.f : m[b][0], r1 = m[b][1] == -INFINITY ? 0.f : m[b][1];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half == 1 && !two) break;
-            const float ref = m[half] == -INFINITY ? 0.f : m[half];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float a = exp2_fast(s[j][2 * half] - ref), b = exp2_fast(s[j][2 * half + 1] - ref);
-                l[half] += a + b;
-                pa[half + 2 * j] = half_pair(a * u[j][0], b * u[j][1]);
+            for (int x = 0; x < 4; ++x) {
+                const float e0 = exp2_fast(s[b][x >> 1][2 * (x & 1)] - r0), e1 = exp2_fast(s[b][x >> 1][2 * (x & 1) + 1] - r1), v = u[x] * u_unit;
+                l[b][0] += e0, l[b][1] += e1;
+                pb[b][x] = transpose8(half_pair(e0 * v, e1 * v));
             }
         }
         // ---- values: matrix (8 keys) x (a 16-byte chunk), its 16-bit units across the lanes
         constexpr int kPer = 16 / BITS, kMats = S::kRow / 16;
 #pragma unroll
-        for (int c = 0; c < kMats; c += 2) {
-            const int key = 16 * warp + (lane & 15), i16 = key * kMats + c + (lane >> 4);
-            uint32_t r[4];  // keys 0 .. 7 and 8 .. 15 of chunk c, then of chunk c + 1
-            ldmatrix4_trans(stage + kFewUnit * S::kRow + 16 * (i16 ^ ((i16 >> 3) & 7)), r);
+        for (int c = 0; c < kMats; ++c) {
+            uint32_t r[4];  // keys 8 x of chunk c
+            ldmatrix4_trans(stage + kUnit * S::kRow + place((32 * warp + lane) * kMats + c), r);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int n = 0; n < kPer; n += 2)
 #pragma unroll
-                for (int n = 0; n < kPer; ++n) {
-                    uint32_t b0, b1;
-                    if constexpr (BITS == 4) b0 = pair4(r[2 * h], n), b1 = pair4(r[2 * h + 1], n);
-                    else b0 = pair8(r[2 * h], n), b1 = pair8(r[2 * h + 1], n);
-                    mma16816(o[(c + h) * kPer + n], pa[0], pa[1], pa[2], pa[3], b0, b1);
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t a[4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if constexpr (BITS == 4) a[h] = pair4(r[2 * j], n + h), a[2 + h] = pair4(r[2 * j + 1], n + h);
+                        else a[h] = pair8(r[2 * j], n + h), a[2 + h] = pair8(r[2 * j + 1], n + h);
+                    }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) mma16816(o[b][(c * kPer + n) / 2], a[0], a[1], a[2], a[3], pb[b][2 * j], pb[b][2 * j + 1]);
                 }
         }
+        __syncwarp();
+        if (lane == 0) arrive(empty(i % S::kCount));
         if (now.unit + 1 == now.units || i + 1 == count) {
             close(run.from + i + 1);
-            now.next(p, part);
+            now.next_pair(p, part);
             if (i + 1 < count) open();
         } else {
             ++now.unit;
         }
     }
-    copies_wait<0>();
 }
 
 // Joins a row's partial results (the shared prefix's, then its sequence's), turns it back by Q^T and rounds it once.  A warp for each
@@ -371,27 +394,37 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     for (int e = 0; e < kE; ++e) o[e] = 0.f;
     auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
         const Part& part = tall ? p.tall : p.few;
-        const int rows = tall ? kTallRows : kFewRows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
-        if ((tall ? tile_of<kTallRows>(p, part, entry) : tile_of<kFewRows>(p, part, entry)).keys == 0) return;
+        const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
+        if (tile_of(p, part, entry).keys == 0) return;
         const int pair = entry * p.cache.heads + h;
         const int2 ctas = load_plain(part.pairs + pair);
         const int64_t first = static_cast<int64_t>(ctas.x) + pair;
-        for (int i = 0; i < ctas.y; ++i) {
-            const int64_t at = (first + i) * rows + r;
-            const float2 ml = load_plain(part.sums + at);
-            const float top = fmaxf(m, ml.x), safe = top == -INFINITY ? 0.f : top;
-            const float fa = exp2_fast(m - safe), fb = exp2_fast(ml.x - safe);
-            float v[kE];
-            if constexpr (kE == 4) {
-                const float4 u = load_plain(reinterpret_cast<const float4*>(part.parts + at * D) + lane);
-                v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
-            } else {
-                const float2 u = load_plain(reinterpret_cast<const float2*>(part.parts + at * D) + lane);
-                v[0] = u.x, v[1] = u.y;
-            }
-            m = top, l = l * fa + ml.y * fb;
+        for (int i0 = 0; i0 < ctas.y; i0 += 32) {  // a lane has one of 32 results' m and l
+            const int n = ctas.y - i0 < 32 ? ctas.y - i0 : 32;
+            const float2 ml = lane < n ? load_plain(part.sums + (first + i0 + lane) * rows + r) : make_float2(-INFINITY, 0.f);
+            float top = ml.x;
 #pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] = o[e] * fa + v[e] * fb;
+            for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+            top = fmaxf(top, m);
+            const float safe = top == -INFINITY ? 0.f : top, old = exp2_fast(m - safe), mine = exp2_fast(ml.x - safe);
+            float sum = mine * ml.y;
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+            m = top, l = l * old + sum;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[e] *= old;
+#pragma unroll 8
+            for (int i = 0; i < n; ++i) {
+                const float f = __shfl_sync(0xFFFFFFFFu, mine, i);
+                const float* at = part.parts + ((first + i0 + i) * rows + r) * D + kE * lane;
+                if constexpr (kE == 4) {
+                    const float4 u = load_plain(reinterpret_cast<const float4*>(at));
+                    o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]), o[2] = fmaf(f, u.z, o[2]), o[3] = fmaf(f, u.w, o[3]);
+                } else {
+                    const float2 u = load_plain(reinterpret_cast<const float2*>(at));
+                    o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]);
+                }
+            }
         }
     };
     if (p.prefix_length > 0) join(p.prefix_tall != 0, -1, token * p.group + head % p.group);
@@ -408,32 +441,51 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     // a length or a start outside its range was taken as the nearest one inside
     if (lane == 0 && head == 0 && place == 0) {
         const int n = load_plain(p.lengths + b);
-        if (n < 0 || n > p.table_width << p.cache.page_shift) atomicExch(p.status, kBadIndex);
+        if (n != cached_keys(p, b)) atomicExch(p.status, kBadIndex);
     }
 }
 
-// CTAs of the first kernel: all that the chip runs at once
-template <int D, int BITS>
-static cudaError_t attend_ctas(const bfq_plan* plan, int* ctas) {
+// A half of the cache as boxes of a page's rows of a head, at most kUnit of them: {bytes of a row, rows of a page, pages}
+static bool encode_half(CUtensorMap* map, const Half& half, const Cache& cache, int row_bytes) {
+    const EncodeTiledFn encode = encode_tiled();
+    if (encode == nullptr) return false;
+    const int page = 1 << cache.page_shift;
+    const cuuint64_t dims[3] = {cuuint64_t(row_bytes), cuuint64_t(cache.heads) << cache.page_shift, cuuint64_t(cache.pages > 0 ? cache.pages : 1)};
+    const cuuint64_t strides[2] = {cuuint64_t(row_bytes), cuuint64_t(half.codes_page)};
+    const cuuint32_t box[3] = {cuuint32_t(row_bytes), cuuint32_t(page < kUnit ? page : kUnit), 1}, estr[3] = {1, 1, 1};
+    const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : (row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, half.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// One of the kernel's forms: CTAs of a launch, all that the chip runs at once (ctas), or the launch (st).
+template <int D, int BITS, int NB>
+static cudaError_t attend_form(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
+    using S = Stage<D, BITS, NB>;
     static int per_sm[kMaxDevices] = {0};
     int& occ = per_sm[plan->device];
     if (occ == 0) {
-        cudaError_t e = cudaFuncSetAttribute(k_attend<D, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(attend_smem<D, BITS>()));
+        cudaError_t e = cudaFuncSetAttribute(k_attend<D, BITS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::kSmem));
         int n = 0;
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<D, BITS>, kAttendThreads, attend_smem<D, BITS>());
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<D, BITS, NB>, kAttendThreads, S::kSmem);
         if (e != cudaSuccess) return e;
         occ = n > 0 ? n : 1;
     }
-    *ctas = plan->sm_count * occ;
-    return cudaSuccess;
+    if (ctas != nullptr) {
+        *ctas = plan->sm_count * occ;
+        return cudaSuccess;
+    }
+    CUtensorMap k_map, v_map;
+    if (!encode_half(&k_map, p.cache.k, p.cache, S::kRow) || !encode_half(&v_map, p.cache.v, p.cache, S::kRow)) return cudaErrorInvalidValue;
+    return launch_overlapped(k_attend<D, BITS, NB>, dim3(unsigned(plan->sm_count * occ)), dim3(kAttendThreads), S::kSmem, st, p, k_map, v_map);
 }
 template <int D, int BITS>
-static cudaError_t launch_attend(const AttendParams& p, int ctas, cudaStream_t st) {
-    return launch_overlapped(k_attend<D, BITS>, dim3(unsigned(ctas)), dim3(kAttendThreads), attend_smem<D, BITS>(), st, p);
+static cudaError_t attend_rows(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
+    return p.few.rows == 8 ? attend_form<D, BITS, 1>(plan, p, ctas, st) : attend_form<D, BITS, 2>(plan, p, ctas, st);
 }
-static cudaError_t ctas_of(const bfq_plan* plan, int bits, int* ctas) {
-    return plan->n == 64 ? (bits == 4 ? attend_ctas<64, 4>(plan, ctas) : attend_ctas<64, 8>(plan, ctas))
-                         : (bits == 4 ? attend_ctas<128, 4>(plan, ctas) : attend_ctas<128, 8>(plan, ctas));
+static cudaError_t attend(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
+    return plan->n == 64 ? (p.cache.bits == 4 ? attend_rows<64, 4>(plan, p, ctas, st) : attend_rows<64, 8>(plan, p, ctas, st))
+                         : (p.cache.bits == 4 ? attend_rows<128, 4>(plan, p, ctas, st) : attend_rows<128, 8>(plan, p, ctas, st));
 }
 
 // Tiles of 256 rows where there are rows enough to pay for them.
@@ -449,7 +501,7 @@ static size_t lay_out(AttendParams* p, int n, int ctas_few, int ctas_tall, uint8
     };
     for (const bool tall : {false, true}) {
         Part& part = tall ? p->tall : p->few;
-        const size_t pairs = size_t(p->entries(part)) * p->cache.heads, rows = (pairs + (tall ? ctas_tall : ctas_few)) * (tall ? kTallRows : kFewRows);
+        const size_t pairs = size_t(p->entries(part)) * p->cache.heads, rows = (pairs + (tall ? ctas_tall : ctas_few)) * part.rows;
         if (pairs == 0) continue;
         part.pairs = reinterpret_cast<int2*>(take(pairs * sizeof(int2)));
         part.sums = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
@@ -467,7 +519,7 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
         in->table_ld < in->table_width || in->prefix_length < 0 || in->prefix_pages < 0)
         return BFQ_ERR_STRIDE;
     if ((int64_t(in->table_width) << p->cache.page_shift) >= int64_t(1) << 30 || in->prefix_length >= int64_t(1) << 30 ||
-        in->prefix_length > int64_t(in->prefix_pages) << p->cache.page_shift)
+        in->prefix_length > int64_t(in->prefix_pages) << p->cache.page_shift || (in->prefix_length > 0 && cache->pages == 0))
         return BFQ_ERR_STRIDE;
     if (!(in->scale == in->scale) || in->scale - in->scale != 0.f) return BFQ_ERR_STRIDE;  // not finite
     if (in->tokens == 0 || in->batch == 0) return BFQ_OK;
@@ -482,11 +534,13 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
         if ((reinterpret_cast<uintptr_t>(at) & 3u) != 0) return BFQ_ERR_ALIGN;
     if (in->q_starts == nullptr ? in->tokens < in->batch : in->max_new < 1 || in->max_new > in->tokens) return BFQ_ERR_STRIDE;
     p->lse = in->lse, p->block_table = in->block_table, p->table_ld = in->table_ld, p->table_width = in->table_width, p->lengths = in->lengths;
-    p->q_starts = in->q_starts, p->prefix = in->prefix, p->prefix_pages = in->prefix_pages, p->prefix_length = int(in->prefix_length);
+    p->q_starts = in->q_starts, p->prefix = in->prefix, p->prefix_pages = in->prefix_pages, p->prefix_length = cache->pages > 0 ? int(in->prefix_length) : 0;
     p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : in->max_new;
     const int64_t rows = (in->q_starts == nullptr ? in->batch : in->tokens) * int64_t(p->group), rows_seq = int64_t(p->max_new) * p->group;
     p->prefix_tall = use_tall(rows), p->seq_tall = use_tall(rows_seq);
-    const int tile_prefix = p->prefix_tall ? kTallRows : kFewRows, tile_seq = p->seq_tall ? kTallRows : kFewRows;
+    p->tall.rows = kTallRows;
+    p->few.rows = (p->seq_tall || rows_seq <= 8) && (in->prefix_length == 0 || p->prefix_tall || rows <= 8) ? 8 : 16;
+    const int tile_prefix = p->prefix_tall ? kTallRows : p->few.rows, tile_seq = p->seq_tall ? kTallRows : p->few.rows;
     const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;
     if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 30) return BFQ_ERR_TOO_LARGE;
     (p->prefix_tall ? p->tall : p->few).tiles_prefix = int(tiles_prefix), (p->seq_tall ? p->tall : p->few).tiles_seq = int(tiles_seq);
@@ -505,7 +559,7 @@ namespace {
 cudaError_t ctas_of_both(const bfq_plan* plan, const kv::AttendParams& p, int* few, int* tall) {
     *few = *tall = 0;
     cudaError_t e = cudaSuccess;
-    if (p.entries(p.few) > 0) e = kv::ctas_of(plan, p.cache.bits, few);
+    if (p.entries(p.few) > 0) e = kv::attend(plan, p, few, nullptr);
     if (e == cudaSuccess && p.entries(p.tall) > 0) e = kv::tall_ctas(plan, p.cache.bits, tall);
     return e;
 }
@@ -533,11 +587,8 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return BFQ_ERR_ALIGN;
         kv::lay_out(&p, plan->n, few, tall, static_cast<uint8_t*>(workspace));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
-        const bool four = cache->bits == 4;
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
-        if (e == cudaSuccess && few > 0)
-            e = plan->n == 64 ? (four ? kv::launch_attend<64, 4>(p, few, st) : kv::launch_attend<64, 8>(p, few, st))
-                              : (four ? kv::launch_attend<128, 4>(p, few, st) : kv::launch_attend<128, 8>(p, few, st));
+        if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, st);
         if (e == cudaSuccess) {
             const dim3 grid(unsigned((p.tokens * p.q.heads + 3) / 4));
             e = plan->n == 64 ? launch_overlapped(kv::k_join<64>, grid, dim3(128), 0, st, p) : launch_overlapped(kv::k_join<128>, grid, dim3(128), 0, st, p);

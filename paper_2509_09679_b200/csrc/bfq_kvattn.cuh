@@ -1,12 +1,12 @@
 // Attention over the paged low-bit cache: the call as the kernels see it, and the order that its work is numbered in.
 //
-// A pair is (row tile, key head): up to ROWS query rows that share a key head, a row being (token, query head of the group), tokens
+// A pair is (row tile, key head): up to `rows` query rows that share a key head, a row being (token, query head of the group), tokens
 // outermost.  Row tiles of the shared prefix come first (their rows are those of all tokens), then those of each sequence.  A pair's
-// keys are cut into units of UNIT; units are numbered pair by pair and every CTA takes an equal run of them, wherever sequences end.
+// keys are cut into units; units are numbered pair by pair and every CTA takes an equal run of them, wherever sequences end.
 // What a CTA has of a pair is a partial result: per row the reference m, the sum l of exp2(s - m) and the sum of exp2(s - m) V.  It is
 // entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.
 //
-// Two kernels do this: one for few rows (tiles of 16 rows, units of 64 keys), one for many (256 rows, 128 keys).  A call gives the prefix's
+// Two kernels do this: one for few rows (tiles of 8 or 16 rows), one for many (256 rows).  A call gives the prefix's
 // tiles to one of them and the sequences' to the same one or the other; each has its own Part of the work.
 #pragma once
 #include "bfq_kv.cuh"
@@ -14,14 +14,15 @@
 namespace bfq {
 namespace kv {
 
-constexpr int kFewRows = 16, kFewUnit = 64;
-constexpr int kTallRows = 256, kTallUnit = 128;
+constexpr int kUnit = 128;  // keys
+constexpr int kTallRows = 256;
 
 struct Part {
+    int rows;                     // of a tile
     int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
     int2* pairs;                  // [pairs] first CTA, CTAs
-    float2* sums;                 // [entries][ROWS] m, l
-    float* parts;                 // [entries][ROWS][D]
+    float2* sums;                 // [entries][rows] m, l
+    float* parts;                 // [entries][rows][D]
 };
 
 struct AttendParams {
@@ -51,7 +52,7 @@ __device__ __forceinline__ int first_token(const AttendParams& p, int b) {
     return t < 0 ? 0 : (t > p.tokens ? static_cast<int>(p.tokens) : t);
 }
 __device__ __forceinline__ int cached_keys(const AttendParams& p, int b) {
-    const int n = load_plain(p.lengths + b), most = p.table_width << p.cache.page_shift;
+    const int n = load_plain(p.lengths + b), most = p.cache.pages > 0 ? p.table_width << p.cache.page_shift : 0;
     return n < 0 ? 0 : (n > most ? most : n);
 }
 
@@ -63,14 +64,14 @@ struct Tile {
     int last0;           // row r has keys 0 .. last0 + (row0 + r) / group; prefix: all
     const int32_t* pages;
 };
-template <int ROWS>
 __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part, int e) {
     Tile t;
+    const int rows = part.rows;
     if (e < part.tiles_prefix) {
         const int tokens = first_token(p, p.batch);
-        t.row0 = e * ROWS, t.token0 = 0;
+        t.row0 = e * rows, t.token0 = 0;
         const int left = tokens * p.group - t.row0;
-        t.rows = left < 0 ? 0 : (left < ROWS ? left : ROWS);
+        t.rows = left < 0 ? 0 : (left < rows ? left : rows);
         t.keys = t.rows > 0 ? p.prefix_length : 0;
         t.last0 = 1 << 30;
         t.pages = p.prefix;
@@ -78,9 +79,9 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     }
     const int b = (e - part.tiles_prefix) / part.tiles_seq, rt = (e - part.tiles_prefix) % part.tiles_seq;
     const int t0 = first_token(p, b), news = first_token(p, b + 1) - t0, n = cached_keys(p, b);
-    t.row0 = rt * ROWS, t.token0 = t0;
+    t.row0 = rt * rows, t.token0 = t0;
     const int left = news * p.group - t.row0;
-    t.rows = left < 0 ? 0 : (left < ROWS ? left : ROWS);
+    t.rows = left < 0 ? 0 : (left < rows ? left : rows);
     t.last0 = n - news;
     const int need = t.rows > 0 ? t.last0 + (t.row0 + t.rows - 1) / p.group + 1 : 0;
     t.keys = need < 0 ? 0 : need;
@@ -89,15 +90,14 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
 }
 
 // Where in the numbering of units a role of a CTA is.
-template <int ROWS, int UNIT>
 struct Walk {
     int entry, head, unit, units;  // unit of units within the pair
     Tile tile;
     __device__ __forceinline__ void enter(const AttendParams& p, const Part& part, int e) {  // the first entry from e on that has units
         const int last = p.entries(part);
         for (entry = e, units = 0; entry < last; ++entry) {
-            tile = tile_of<ROWS>(p, part, entry);
-            units = (tile.keys + UNIT - 1) / UNIT;
+            tile = tile_of(p, part, entry);
+            units = (tile.keys + kUnit - 1) / kUnit;
             if (units > 0) break;
         }
     }
@@ -116,15 +116,15 @@ struct Walk {
 // A CTA's run of units, found by all its threads together from the lengths.
 struct Run {
     long long from;  // the first one's number
-    long long per;   // units of every CTA but the last ones
+    long long per;   // units of every CTA but the last
     int count;       // 0: none
 };
-template <int THREADS, int ROWS, int UNIT>
-__device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part, long long* scan, Walk<ROWS, UNIT>* walk) {  // scan: shared, THREADS / 32 + 2
+template <int THREADS>
+__device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part, long long* scan, Walk* walk) {  // scan: shared, THREADS / 32 + 2
     constexpr int kWarps = THREADS / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, entries = p.entries(part), heads = p.cache.heads;
     const int each = (entries + THREADS - 1) / THREADS;
-    auto units_at = [&](int e) { return (tile_of<ROWS>(p, part, e).keys + UNIT - 1) / UNIT; };
+    auto units_at = [&](int e) { return (tile_of(p, part, e).keys + kUnit - 1) / kUnit; };
     long long mine = 0;
     for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_at(e);
     long long before = mine, total = 0;
@@ -142,7 +142,7 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     before -= mine;
     total *= heads;
     Run run;
-    run.per = (total + gridDim.x - 1) / gridDim.x > 2 ? (total + gridDim.x - 1) / gridDim.x : 2;
+    run.per = total > 0 ? (total + gridDim.x - 1) / gridDim.x : 1;
     run.from = run.per * blockIdx.x;
     const long long to = run.from + run.per < total ? run.from + run.per : total;
     run.count = run.from < to ? static_cast<int>(to - run.from) : 0;
@@ -209,6 +209,19 @@ struct RowPower {
         up = __uint_as_float(uint32_t(e) << 23), down = __uint_as_float(uint32_t(254 - e) << 23);
     }
 };
+
+// Waits for a phase, with a limit.  Once one wait has given up all others of the CTA return at once (what they wait for may never come): the
+// kernel ends with meaningless outputs and the status word says so.
+constexpr int kWaitLimit = 1 << 22;
+__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+    for (int i = 0; i < kWaitLimit; ++i) {
+        if (mbar_try_wait(bar, parity)) return;
+        if (*dead) return;
+    }
+    *dead = 1;
+    atomicExch(status, 3);
+}
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 // the tall kernel (bfq_kvtall.cu): CTAs of a launch, and the launch
 cudaError_t tall_ctas(const bfq_plan* plan, int bits, int* ctas);

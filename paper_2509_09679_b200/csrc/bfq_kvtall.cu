@@ -22,7 +22,6 @@ namespace kv {
 
 constexpr int kTallThreads = 13 * 32;
 constexpr int kConvert = 128;  // threads that turn codes into operands
-constexpr int kTallLimit = 1 << 22;
 
 template <int D>
 struct TallSmem {
@@ -35,17 +34,6 @@ struct TallSmem {
 };
 enum Bar { kKvFull = 0, kKvEmpty = 2, kSFull = 4, kPFull = 6, kQFull = 8, kOFull = 10, kBarCount = 12 };
 
-// Waits for a phase, with a limit.  Once one wait has given up all others of the CTA return at once (what they wait for may never come): the
-// kernel ends with meaningless outputs and the status word says so.
-__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
-    for (int i = 0; i < kTallLimit; ++i) {
-        if (mbar_try_wait(bar, parity)) return;
-        if (*dead) return;
-    }
-    *dead = 1;
-    atomicExch(status, 3);
-}
-__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -87,7 +75,6 @@ __host__ __device__ constexpr int order(int i) {
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendParams p) {
     using M = TallSmem<D>;
-    using W = Walk<kTallRows, kTallUnit>;
     constexpr int kRow = D * BITS / 8;
     extern __shared__ uint8_t smem_raw[];
     __shared__ long long scan[kTallThreads / 32 + 2];
@@ -101,7 +88,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     auto scales_at = [&](int s) { return base + M::kScales + s * M::kScalesBytes; };
     grid_dep_wait();
     const Part& part = p.tall;
-    W walk;
+    Walk walk;
     const Run run = find_run<kTallThreads>(p, part, scan, &walk);
     if (run.count == 0) return;
     if (tid == 0) {
@@ -202,8 +189,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         for (int i = 0; i < count; ++i) {
             if (active) {
                 const uint32_t k_scales = scales_at(i & 1), v_scales = k_scales + 512;
-                const int key0 = walk.unit * kTallUnit;
-                const bool edge = key0 + kTallUnit > least;  // some row of the warp ends in this unit, or has ended
+                const int key0 = walk.unit * kUnit;
+                const bool edge = key0 + kUnit > least;  // some row of the warp ends in this unit, or has ended
                 wait_for(bar(kKvFull + (i & 1)), (i >> 1) & 1, &dead, p.status);  // for the scales
                 wait_for(bar(kSFull + tile), s_phase, &dead, p.status);
                 s_phase ^= 1;
@@ -298,7 +285,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         // 16-byte pieces: the eight lanes of a phase of the stores below write chunks of one half to eight different places of 16 bytes
         constexpr int kPer = BITS == 4 ? 2 : 4;          // pieces of 64 elements
         constexpr int kKeys = 32 / (kPer * (D / 64));    // keys of a warp's 32 pieces
-        constexpr int kTurns = kTallUnit / kKeys / 4;
+        constexpr int kTurns = kUnit / kKeys / 4;
         const int part_of = lane % kPer, key_low = lane / kPer % (8 / kPer);
         const int half = D == 128 ? lane >> 3 & 1 : 0, key_of = key_low + (8 / kPer) * (D == 128 ? lane >> 4 : lane >> 3);
         uint4 k_raw[kTurns], v_raw[kTurns];
@@ -307,7 +294,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             const int mask = (1 << p.cache.page_shift) - 1;
 #pragma unroll
             for (int c = 0; c < kTurns; ++c) {
-                const int key = walk.unit * kTallUnit + (c * 4 + w) * kKeys + key_of;
+                const int key = walk.unit * kUnit + (c * 4 + w) * kKeys + key_of;
                 const int64_t page = key < walk.tile.keys ? page_of(p, walk.tile, key) : -1;
                 k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0);
                 if (page >= 0) {
@@ -316,7 +303,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                     v_raw[c] = load_plain(reinterpret_cast<const uint4*>(codes_of<kRow>(p.cache.v, p.cache.page_shift, page, walk.head, key & mask) + at));
                 }
             }
-            const int key = walk.unit * kTallUnit + r;
+            const int key = walk.unit * kUnit + r;
             const int64_t page = key < walk.tile.keys ? page_of(p, walk.tile, key) : -1;
             scale_raw = 0;
             if (page >= 0) {
@@ -391,7 +378,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             auto issue_products = [&](int tile, int s, bool accumulate) {
                 const uint32_t b = stage_at(s) + M::kTile;
     #pragma unroll
-                for (int k = 0; k < kTallUnit / 16; ++k) mma_ts(products(tile), scores(tile) + 8 * k, operand(b + 2048 * k, 16384), kProductsDesc, accumulate || k > 0);
+                for (int k = 0; k < kUnit / 16; ++k) mma_ts(products(tile), scores(tile) + 8 * k, operand(b + 2048 * k, 16384), kProductsDesc, accumulate || k > 0);
             };
             bool first = true;
             for (int i = 0; i < count; ++i) {
