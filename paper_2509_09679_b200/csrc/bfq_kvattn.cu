@@ -9,7 +9,7 @@
 // at most 8 (a factor of 256) below the largest score so far, so that it, the sum and the products change only when a score passes it by more
 // than that.
 //
-// A CTA of four warps takes units of 128 keys, 32 keys to a warp, from a ring of stages that TMA fills ahead (a box for each page and half,
+// A CTA of four warps takes units of 128 keys, 32 keys to a warp, each warp from a ring of its own that it fills ahead by TMA (a box for each page and half,
 // swizzled so that the reads below hit every bank once).  mma.m16n8k16 with the keys, then the values' elements, as its 16 rows and 8 queries
 // as its columns: with the queries as rows a group of four would leave three quarters of the tensor cores' work idle and twice
 // the registers taken.  Keys come as words of a row, 8 (4) codes at a time; which k index of the product an element gets is
@@ -26,15 +26,18 @@ namespace kv {
 
 constexpr int kWarps = 4, kAttendThreads = 32 * kWarps;
 
+constexpr int kKeys = kUnit / kWarps;  // of a warp
+
+// Shared memory: for each warp kCount stages of its 32 keys' and values' codes, the same of their scales, a tile's merged products, sums, barriers.
 template <int D, int BITS, int NB>
 struct Stage {
-    static constexpr int kRow = D * BITS / 8;              // bytes of a row's codes
-    static constexpr uint32_t kScales = 2 * kUnit * kRow;  // keys' scales behind both halves' codes, then the values'
-    static constexpr uint32_t kBytes = (kScales + 4 * kUnit + 1023) / 1024 * 1024;
-    static constexpr int kCount = 2;  // 3 stages: 108 us where 2 and four CTAs on an SM take 102 (64 sequences, 276 K keys, 4 bits)
-    static constexpr int kPitch = D + 4;                   // of a merged row, floats
-    static constexpr uint32_t kMerge = kCount * kBytes, kSums = kMerge + 2 * 8 * NB * kPitch * 4, kBars = kSums + kWarps * 8 * NB * 8;
-    static constexpr uint32_t kSmem = kBars + 2 * kCount * 8 + 1024;  // and what rounding the base up to 1024 takes
+    static constexpr int kRow = D * BITS / 8;  // bytes of a row's codes
+    static constexpr int kCount = kRow == 128 ? 2 : 3;
+    static constexpr uint32_t kBytes = 2 * kKeys * kRow, kScaleBytes = 4 * kKeys;
+    static constexpr int kPitch = D + 4;  // of a merged row, floats
+    static constexpr uint32_t kScales = kWarps * kCount * kBytes, kMerge = kScales + kWarps * kCount * kScaleBytes, kSums = kMerge + 8 * NB * kPitch * 4,
+                              kBars = kSums + kWarps * 8 * NB * 8;
+    static constexpr uint32_t kSmem = kBars + kWarps * kCount * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -78,11 +81,12 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
     __shared__ long long scan[kWarps + 2];
     __shared__ volatile int dead;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    float* const merge = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kMerge);  // [2][rows][pitch]
+    float* const merge = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kMerge);  // [rows][pitch]
     float2* const warp_sums = reinterpret_cast<float2*>(smem_raw + (base - smem_u32(smem_raw)) + S::kSums);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    auto full = [&](int s) { return base + S::kBars + 8u * s; };
-    auto empty = [&](int s) { return base + S::kBars + 8u * (S::kCount + s); };
+    auto full = [&](int s) { return base + S::kBars + 8u * (warp * S::kCount + s); };
+    auto stage_at = [&](int s) { return base + (warp * S::kCount + s) * S::kBytes; };
+    auto scales_at = [&](int s) { return base + S::kScales + (warp * S::kCount + s) * S::kScaleBytes; };
     grid_dep_wait();
     const Part& part = p.few;
     Walk ahead;
@@ -91,39 +95,42 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
     Walk now = ahead;
     const int count = run.count;
     if (tid == 0) {
-        for (int s = 0; s < S::kCount; ++s) mbar_init(full(s), 1), mbar_init(empty(s), kWarps);
+        for (int s = 0; s < kWarps * S::kCount; ++s) mbar_init(base + S::kBars + 8u * s, 1);
         mbar_init_fence();
         dead = 0;
     }
     __syncthreads();
 
-    // ---- the first warp sends for units, a page to a lane -------------------------------------------------------------------
+    // ---- the warp's keys of the unit ahead, a page to a lane; the pages' numbers are looked up one unit earlier still -----------
+    const int page_keys = 1 << p.cache.page_shift, box = page_keys < kKeys ? page_keys : kKeys;
+    constexpr int64_t kNone = -(int64_t(1) << 32);
+    int64_t page = kNone;  // of the lane's box; kNone: it has no keys
+    auto look = [&](int i) {
+        const int key = ahead.unit * kUnit + kKeys * warp + lane * box;
+        page = i < count && lane * box < kKeys && key < ahead.tile.keys ? load_plain(ahead.tile.pages + (key >> p.cache.page_shift)) : kNone;
+    };
     auto fetch = [&](int i) {
-        if (warp != 0 || i >= count) return;
-        const int s = i % S::kCount;
-        if (i >= S::kCount) wait_for(empty(s), (i / S::kCount - 1) & 1, &dead, p.status);
-        const int page_keys = 1 << p.cache.page_shift, box = page_keys < kUnit ? page_keys : kUnit;
-        const int key = ahead.unit * kUnit + lane * box;
-        const bool there = lane * box < kUnit && key < ahead.tile.keys;
-        const uint32_t stage = base + s * S::kBytes;
-        if (lane == 0) {
-            const int left = ahead.tile.keys - ahead.unit * kUnit, boxes = ((left < kUnit ? left : kUnit) + box - 1) / box;
-            mbar_expect_tx(full(s), boxes * box * (2 * S::kRow + 4));
-        }
+        if (i >= count) return;
+        const int s = i % S::kCount, first = ahead.unit * kUnit + kKeys * warp, row = (ahead.head << p.cache.page_shift) + ((first + lane * box) & (page_keys - 1));
+        const bool there = page != kNone;
+        const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, there));
+        if (lane == 0) mbar_expect_tx(full(s), boxes * box * (2 * S::kRow + 4));
         __syncwarp();
         if (there) {
-            const int64_t found = page_of(p, ahead.tile, key), page = found < 0 ? 0 : found;
-            const int row = (ahead.head << p.cache.page_shift) + (key & (page_keys - 1));
-            tma_load_3d(stage + lane * box * S::kRow, &k_map, 0, row, static_cast<int>(page), full(s));
-            tma_load_3d(stage + (kUnit + lane * box) * S::kRow, &v_map, 0, row, static_cast<int>(page), full(s));
-            bulk_load(stage + S::kScales + lane * box * 2, p.cache.k.scales + page * p.cache.k.scales_page + row, box * 2, full(s));
-            bulk_load(stage + S::kScales + (kUnit + lane * box) * 2, p.cache.v.scales + page * p.cache.v.scales_page + row, box * 2, full(s));
+            if (page < 0 || page >= p.cache.pages) atomicExch(p.status, kBadIndex), page = 0;
+            const uint32_t codes = stage_at(s) + lane * box * S::kRow, scales = scales_at(s) + lane * box * 2;
+            tma_load_3d(codes, &k_map, 0, row, static_cast<int>(page), full(s));
+            tma_load_3d(codes + kKeys * S::kRow, &v_map, 0, row, static_cast<int>(page), full(s));
+            bulk_load(scales, p.cache.k.scales + page * p.cache.k.scales_page + row, box * 2, full(s));
+            bulk_load(scales + kKeys * 2, p.cache.v.scales + page * p.cache.v.scales_page + row, box * 2, full(s));
         }
         __syncwarp();
         ahead.next(p, part);
+        look(i + 1);
     };
+    look(0);
 #pragma unroll
-    for (int i = 0; i < S::kCount - 1; ++i) fetch(i);
+    for (int i = 0; i < S::kCount; ++i) fetch(i);
     // place of a 16-byte chunk, numbered row by row, in a swizzled half of a stage
     auto place = [](int i16) { return 16u * (i16 ^ ((i16 >> 3) & (S::kRow / 16 - 1))); };
 
@@ -225,14 +232,13 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
                         *at = add ? *at + v : v;
                     }
         };
-        if (warp >= 2) put(merge + (warp - 2) * kRows * S::kPitch, false);
-        __syncthreads();
-        if (warp < 2) put(merge + warp * kRows * S::kPitch, true);
-        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) {  // in this order, so that the sums are the same each time
+            if (warp == w) put(merge, w > 0);
+            __syncthreads();
+        }
         for (int i = tid; i < now.tile.rows * (D / 4); i += kAttendThreads) {
             const int r = i / (D / 4), c = 4 * (i % (D / 4));
-            const float4 a = *reinterpret_cast<const float4*>(merge + r * S::kPitch + c), b = *reinterpret_cast<const float4*>(merge + (kRows + r) * S::kPitch + c);
-            *reinterpret_cast<float4*>(part.parts + (entry * kRows + r) * D + c) = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+            *reinterpret_cast<float4*>(part.parts + (entry * kRows + r) * D + c) = *reinterpret_cast<const float4*>(merge + r * S::kPitch + c);
         }
         if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + now.units - 1) / run.per - blockIdx.x + 1));
         pair_from = done;
@@ -240,121 +246,122 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
 
     open();
     for (int i = 0; i < count; ++i) {
-        fetch(i + S::kCount - 1);
-        wait_for(full(i % S::kCount), (i / S::kCount) & 1, &dead, p.status);
-        const uint32_t stage = base + (i % S::kCount) * S::kBytes;
-        const int key0 = now.unit * kUnit + 32 * warp;
-        // ---- scores of 32 keys: rows g and g + 8 of product j are keys 16 j + g and 16 j + 8 + g of the warp's
-        float s[NB][2][4];
+        const int slot = i % S::kCount, key0 = now.unit * kUnit + kKeys * warp;
+        const uint32_t stage = stage_at(slot), scales = scales_at(slot);
+        wait_for(full(slot), (i / S::kCount) & 1, &dead, p.status);
+        if (key0 < now.tile.keys) {
+            // ---- scores of 32 keys: rows g and g + 8 of product j are keys 16 j + g and 16 j + 8 + g of the warp's
+            float s[NB][2][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            constexpr int kWords = D * BITS / 128;  // of a lane and key
-            uint32_t w[2][kWords];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int key = 32 * warp + 16 * j + 8 * h + g;
-                if constexpr (kWords == 2) {
-                    const uint2 v = lds64(stage + place(key * (S::kRow / 16) + (t >> 1)) + 8 * (t & 1));
-                    w[h][0] = v.x, w[h][1] = v.y;
-                } else {
-#pragma unroll
-                    for (int c = 0; c < kWords / 4; ++c) {
-                        const uint4 v = lds128(stage + place(key * (S::kRow / 16) + t * (kWords / 4) + c));
-                        w[h][4 * c] = v.x, w[h][4 * c + 1] = v.y, w[h][4 * c + 2] = v.z, w[h][4 * c + 3] = v.w;
-                    }
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) s[b][j][c] = 0.f;
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                uint32_t a[4];
+            for (int j = 0; j < 2; ++j) {
+                constexpr int kWords = D * BITS / 128;  // of a lane and key
+                uint32_t w[2][kWords];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if constexpr (BITS == 4) a[h] = pair4(w[h][st / 2], 2 * (st & 1)), a[2 + h] = pair4(w[h][st / 2], 2 * (st & 1) + 1);
-                    else a[h] = pair8(w[h][st], 0), a[2 + h] = pair8(w[h][st], 1);
+                    const int key = 16 * j + 8 * h + g;
+                    if constexpr (kWords == 2) {
+                        const uint2 v = lds64(stage + place(key * (S::kRow / 16) + (t >> 1)) + 8 * (t & 1));
+                        w[h][0] = v.x, w[h][1] = v.y;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kWords / 4; ++c) {
+                            const uint4 v = lds128(stage + place(key * (S::kRow / 16) + t * (kWords / 4) + c));
+                            w[h][4 * c] = v.x, w[h][4 * c + 1] = v.y, w[h][4 * c + 2] = v.z, w[h][4 * c + 3] = v.w;
+                        }
+                    }
                 }
 #pragma unroll
-                for (int b = 0; b < NB; ++b) mma16816(s[b][j], a[0], a[1], a[2], a[3], qb[b][st][0], qb[b][st][1]);
-            }
-        }
-        // ---- scales, masks, probabilities
-        float u[4];  // keys 8 x + g
-        bool over = false;
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const uint32_t at = stage + S::kScales + 2 * (32 * warp + 8 * x + g);
-            const int key = key0 + 8 * x + g;
-            const float f = lds_half(at);
-            u[x] = key < now.tile.keys ? lds_half(at + 2 * kUnit) : 0.f;
-            over |= u[x] > u_top;
+                    for (int c = 0; c < 4; ++c) s[b][j][c] = 0.f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float& v = s[b][x >> 1][2 * (x & 1) + c];
-                    v = key < limit[b][c] ? v * f * row_scale_log2[b][c] : -INFINITY;
-                    over |= v > m[b][c] + 8.f;
-                }
-        }
-        if (__any_sync(0xFFFFFFFFu, over)) {
-            float most = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3]));
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, x));
-            float less = 1.f;  // on the products
-            if (most > u_top) {
-                const float top = __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u);  // above it
-                less = u_top / top, u_top = top, u_unit = 128.f / top;
-            }
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float top = fmaxf(fmaxf(s[b][0][c], s[b][0][2 + c]), fmaxf(s[b][1][c], s[b][1][2 + c]));
-#pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-                    top = fmaxf(top, m[b][c]);
-                    const float f = top == -INFINITY ? 1.f : exp2_fast(m[b][c] - top);
-                    m[b][c] = top, l[b][c] *= f;
-#pragma unroll
-                    for (int k = 0; k < kSteps; ++k) o[b][k][c] *= f * less, o[b][k][2 + c] *= f * less;
-                }
-        }
-        uint32_t pb[NB][4];  // keys 8 x + 2 t and + 1 of query 8 b + g
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const float r0 = m[b][0] == -INFINITY ? 0.f : m[b][0], r1 = m[b][1] == -INFINITY ? 0.f : m[b][1];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float e0 = exp2_fast(s[b][x >> 1][2 * (x & 1)] - r0), e1 = exp2_fast(s[b][x >> 1][2 * (x & 1) + 1] - r1), v = u[x] * u_unit;
-                l[b][0] += e0, l[b][1] += e1;
-                pb[b][x] = transpose8(half_pair(e0 * v, e1 * v));
-            }
-        }
-        // ---- values: matrix (8 keys) x (a 16-byte chunk), its 16-bit units across the lanes
-        constexpr int kPer = 16 / BITS, kMats = S::kRow / 16;
-#pragma unroll
-        for (int c = 0; c < kMats; ++c) {
-            uint32_t r[4];  // keys 8 x of chunk c
-            ldmatrix4_trans(stage + kUnit * S::kRow + place((32 * warp + lane) * kMats + c), r);
-#pragma unroll
-            for (int n = 0; n < kPer; n += 2)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int st = 0; st < kSteps; ++st) {
                     uint32_t a[4];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if constexpr (BITS == 4) a[h] = pair4(r[2 * j], n + h), a[2 + h] = pair4(r[2 * j + 1], n + h);
-                        else a[h] = pair8(r[2 * j], n + h), a[2 + h] = pair8(r[2 * j + 1], n + h);
+                        if constexpr (BITS == 4) a[h] = pair4(w[h][st / 2], 2 * (st & 1)), a[2 + h] = pair4(w[h][st / 2], 2 * (st & 1) + 1);
+                        else a[h] = pair8(w[h][st], 0), a[2 + h] = pair8(w[h][st], 1);
                     }
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) mma16816(o[b][(c * kPer + n) / 2], a[0], a[1], a[2], a[3], pb[b][2 * j], pb[b][2 * j + 1]);
+                    for (int b = 0; b < NB; ++b) mma16816(s[b][j], a[0], a[1], a[2], a[3], qb[b][st][0], qb[b][st][1]);
                 }
+            }
+            // ---- scales, masks, probabilities
+            float u[4];  // keys 8 x + g
+            bool over = false;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t at = scales + 2 * (8 * x + g);
+                const int key = key0 + 8 * x + g;
+                const float f = lds_half(at);
+                u[x] = key < now.tile.keys ? lds_half(at + 2 * kKeys) : 0.f;
+                over |= u[x] > u_top;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float& v = s[b][x >> 1][2 * (x & 1) + c];
+                        v = key < limit[b][c] ? v * f * row_scale_log2[b][c] : -INFINITY;
+                        over |= v > m[b][c] + 8.f;
+                    }
+            }
+            if (__any_sync(0xFFFFFFFFu, over)) {
+                float most = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3]));
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, x));
+                float less = 1.f;  // on the products
+                if (most > u_top) {
+                    const float top = __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u);  // above it
+                    less = u_top / top, u_top = top, u_unit = 128.f / top;
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float top = fmaxf(fmaxf(s[b][0][c], s[b][0][2 + c]), fmaxf(s[b][1][c], s[b][1][2 + c]));
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                        top = fmaxf(top, m[b][c]);
+                        const float f = top == -INFINITY ? 1.f : exp2_fast(m[b][c] - top);
+                        m[b][c] = top, l[b][c] *= f;
+#pragma unroll
+                        for (int k = 0; k < kSteps; ++k) o[b][k][c] *= f * less, o[b][k][2 + c] *= f * less;
+                    }
+            }
+            uint32_t pb[NB][4];  // keys 8 x + 2 t and + 1 of query 8 b + g
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const float r0 = m[b][0] == -INFINITY ? 0.f : m[b][0], r1 = m[b][1] == -INFINITY ? 0.f : m[b][1];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float e0 = exp2_fast(s[b][x >> 1][2 * (x & 1)] - r0), e1 = exp2_fast(s[b][x >> 1][2 * (x & 1) + 1] - r1), v = u[x] * u_unit;
+                    l[b][0] += e0, l[b][1] += e1;
+                    pb[b][x] = transpose8(half_pair(e0 * v, e1 * v));
+                }
+            }
+            // ---- values: matrix (8 keys) x (a 16-byte chunk), its 16-bit units across the lanes
+            constexpr int kPer = 16 / BITS, kMats = S::kRow / 16;
+#pragma unroll
+            for (int c = 0; c < kMats; ++c) {
+                uint32_t r[4];  // keys 8 x of chunk c
+                ldmatrix4_trans(stage + kKeys * S::kRow + place(lane * kMats + c), r);
+#pragma unroll
+                for (int n = 0; n < kPer; n += 2)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t a[4];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if constexpr (BITS == 4) a[h] = pair4(r[2 * j], n + h), a[2 + h] = pair4(r[2 * j + 1], n + h);
+                            else a[h] = pair8(r[2 * j], n + h), a[2 + h] = pair8(r[2 * j + 1], n + h);
+                        }
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) mma16816(o[b][(c * kPer + n) / 2], a[0], a[1], a[2], a[3], pb[b][2 * j], pb[b][2 * j + 1]);
+                    }
+            }
         }
         __syncwarp();
-        if (lane == 0) arrive(empty(i % S::kCount));
+        fetch(i + S::kCount);
         if (now.unit + 1 == now.units || i + 1 == count) {
             close(run.from + i + 1);
             now.next_pair(p, part);
@@ -445,14 +452,14 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     }
 }
 
-// A half of the cache as boxes of a page's rows of a head, at most kUnit of them: {bytes of a row, rows of a page, pages}
+// A half of the cache as boxes of a page's rows of a head, at most kKeys of them: {bytes of a row, rows of a page, pages}
 static bool encode_half(CUtensorMap* map, const Half& half, const Cache& cache, int row_bytes) {
     const EncodeTiledFn encode = encode_tiled();
     if (encode == nullptr) return false;
     const int page = 1 << cache.page_shift;
     const cuuint64_t dims[3] = {cuuint64_t(row_bytes), cuuint64_t(cache.heads) << cache.page_shift, cuuint64_t(cache.pages > 0 ? cache.pages : 1)};
     const cuuint64_t strides[2] = {cuuint64_t(row_bytes), cuuint64_t(half.codes_page)};
-    const cuuint32_t box[3] = {cuuint32_t(row_bytes), cuuint32_t(page < kUnit ? page : kUnit), 1}, estr[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {cuuint32_t(row_bytes), cuuint32_t(page < kKeys ? page : kKeys), 1}, estr[3] = {1, 1, 1};
     const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : (row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, half.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
