@@ -71,10 +71,13 @@ __device__ __forceinline__ float lds_half(uint32_t at) {
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+struct Maps {
+    CUtensorMap k_codes, v_codes;
+};
 
 // NB: blocks of 8 queries
 template <int D, int BITS, int NB>
-__global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+__global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 1024 ? 3 : 4)) k_attend(const AttendParams p, const __grid_constant__ Maps maps) {
     using S = Stage<D, BITS, NB>;
     constexpr int kSteps = D / 16, kRows = 8 * NB;
     extern __shared__ uint8_t smem_raw[];
@@ -84,6 +87,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
     float* const merge = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kMerge);  // [rows][pitch]
     float2* const warp_sums = reinterpret_cast<float2*>(smem_raw + (base - smem_u32(smem_raw)) + S::kSums);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const Unpack<BITS> unpack;
     auto full = [&](int s) { return base + S::kBars + 8u * (warp * S::kCount + s); };
     auto stage_at = [&](int s) { return base + (warp * S::kCount + s) * S::kBytes; };
     auto scales_at = [&](int s) { return base + S::kScales + (warp * S::kCount + s) * S::kScaleBytes; };
@@ -102,43 +106,49 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
     __syncthreads();
 
     // ---- the warp's keys of the unit ahead, a page to a lane; the pages' numbers are looked up one unit earlier still -----------
-    const int page_keys = 1 << p.cache.page_shift, box = page_keys < kKeys ? page_keys : kKeys;
+    const int page_keys = 1 << p.cache.page_shift, box = page_keys < kKeys ? page_keys : kKeys, own = kKeys * warp + lane * box;
+    const bool a_box = lane * box < kKeys;
     constexpr int64_t kNone = -(int64_t(1) << 32);
     int64_t page = kNone;  // of the lane's box; kNone: it has no keys
-    auto look = [&](int i) {
-        const int key = ahead.unit * kUnit + kKeys * warp + lane * box;
-        page = i < count && lane * box < kKeys && key < ahead.tile.keys ? load_plain(ahead.tile.pages + (key >> p.cache.page_shift)) : kNone;
+    int sent = 0;          // units
+    auto look = [&]() {
+        const int key = ahead.unit * kUnit + own;
+        page = sent < count && a_box && key < ahead.tile.keys ? load_plain(ahead.tile.pages + (key >> p.cache.page_shift)) : kNone;
     };
-    auto fetch = [&](int i) {
-        if (i >= count) return;
-        const int s = i % S::kCount, first = ahead.unit * kUnit + kKeys * warp, row = (ahead.head << p.cache.page_shift) + ((first + lane * box) & (page_keys - 1));
-        const bool there = page != kNone;
-        const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, there));
-        if (lane == 0) mbar_expect_tx(full(s), boxes * box * (2 * S::kRow + 4));
+    auto fetch = [&](int slot) {
+        if (sent >= count) return;
+        ++sent;
+        const int row = (ahead.head << p.cache.page_shift) + ((ahead.unit * kUnit + own) & (page_keys - 1));
+        const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, page != kNone));
+        if (lane == 0) mbar_expect_tx(full(slot), boxes * box * (2 * S::kRow + 4));
         __syncwarp();
-        if (there) {
+        if (page != kNone) {
             if (page < 0 || page >= p.cache.pages) atomicExch(p.status, kBadIndex), page = 0;
-            const uint32_t codes = stage_at(s) + lane * box * S::kRow, scales = scales_at(s) + lane * box * 2;
-            tma_load_3d(codes, &k_map, 0, row, static_cast<int>(page), full(s));
-            tma_load_3d(codes + kKeys * S::kRow, &v_map, 0, row, static_cast<int>(page), full(s));
-            bulk_load(scales, p.cache.k.scales + page * p.cache.k.scales_page + row, box * 2, full(s));
-            bulk_load(scales + kKeys * 2, p.cache.v.scales + page * p.cache.v.scales_page + row, box * 2, full(s));
+            const int at = static_cast<int>(page);
+            const uint32_t codes = stage_at(slot) + lane * box * S::kRow, scales = scales_at(slot) + lane * box * 2;
+            tma_load_3d(codes, &maps.k_codes, 0, row, at, full(slot));
+            tma_load_3d(codes + kKeys * S::kRow, &maps.v_codes, 0, row, at, full(slot));
+            bulk_load(scales, p.cache.k.scales + page * p.cache.k.scales_page + row, box * 2, full(slot));
+            bulk_load(scales + kKeys * 2, p.cache.v.scales + page * p.cache.v.scales_page + row, box * 2, full(slot));
         }
         __syncwarp();
         ahead.next(p, part);
-        look(i + 1);
+        look();
     };
-    look(0);
+    look();
 #pragma unroll
     for (int i = 0; i < S::kCount; ++i) fetch(i);
-    // place of a 16-byte chunk, numbered row by row, in a swizzled half of a stage
-    auto place = [](int i16) { return 16u * (i16 ^ ((i16 >> 3) & (S::kRow / 16 - 1))); };
+    // place of 16-byte chunk c of row r of a swizzled half of a stage: r kRow + 16 (c ^ its swizzle), which rows 8 apart share
+    auto swizzle = [](int r) { return S::kRow == 128 ? r & 7 : (S::kRow == 64 ? r >> 1 & 3 : r >> 2 & 1); };
+    const uint32_t k_lane = g * S::kRow + 16 * ((t * S::kRow / 64) ^ swizzle(g)) + (S::kRow == 32 ? 8 * (t & 1) : 0);  // its first chunk of row g
+    const uint32_t v_lane = kKeys * S::kRow + lane * S::kRow + 16 * swizzle(lane & 7);
 
     // ---- a pair's state: fragments of the queries, reference, sums and products -------------------------------------------
     uint32_t qb[NB][kSteps][2];
     float m[NB][2], l[NB][2], o[NB][kSteps][4];  // of queries 8 b + 2 t and + 1; o: element rows of 16
-    float row_scale_log2[NB][2];                 // softmax scale * log2 e over the row's power of two
-    int limit[NB][2];                            // keys of the row
+    // m and scores are in units of the row's power of two; times `unit`, softmax scale * log2 e over it, they are exponents of 2
+    float unit[NB][2], over_at[NB][2];  // a score above over_at moves m
+    int limit[NB][2], least;            // keys of the row; of the tile's rows, at least
     float u_top, u_unit;  // power of two that no u so far passes; 128 / u_top: probabilities (at most 2^8) times u stay below 2^15
     auto open = [&]() {
         const Tile& tl = now.tile;
@@ -160,7 +170,8 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             const RowPower power(top);
-            auto element = [&](int i) { return power.up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
+            const float up = p.scale_log2 < 0.f ? -power.up : power.up;
+            auto element = [&](int i) { return up * __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); };
             auto pair = [&](int i, int j) { return half_pair(element(i), element(j)); };
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
@@ -174,9 +185,9 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
             const int own = tl.last0 + row / p.group + 1, keys = there ? (own < tl.keys ? own : tl.keys) : 0;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {  // from the lanes of the rows that this lane's columns are
-                row_scale_log2[b][c] = p.scale_log2 * __shfl_sync(0xFFFFFFFFu, power.down, 4 * (2 * t + c));
+                unit[b][c] = fmaxf(fabsf(p.scale_log2) * __shfl_sync(0xFFFFFFFFu, power.down, 4 * (2 * t + c)), 1e-30f);  // times -infinity is that
                 limit[b][c] = __shfl_sync(0xFFFFFFFFu, keys, 4 * (2 * t + c));
-                m[b][c] = -INFINITY, l[b][c] = 0.f;
+                m[b][c] = over_at[b][c] = -INFINITY, l[b][c] = 0.f;
             }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
@@ -184,6 +195,10 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
                 for (int j = 0; j < 4; ++j) o[b][i][j] = 0.f;
         }
         u_top = 0.f, u_unit = 0.f;
+        least = tl.keys;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) least = min(least, 8 * b + g < tl.rows ? tl.last0 + (tl.row0 + 8 * b + g) / p.group + 1 : least);
+        least = __reduce_min_sync(0xFFFFFFFFu, least);
     };
     long long pair_from = run.from - now.unit;  // number of the pair's unit 0
     auto close = [&](long long done) {          // after unit `done` (exclusive) of the numbering
@@ -195,7 +210,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
             for (int c = 0; c < 2; ++c) {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[b][c] += __shfl_xor_sync(0xFFFFFFFFu, l[b][c], x);
-                if (g == 0) warp_sums[warp * kRows + 8 * b + 2 * t + c] = make_float2(m[b][c], l[b][c]);
+                if (g == 0) warp_sums[warp * kRows + 8 * b + 2 * t + c] = make_float2(m[b][c] * unit[b][c], l[b][c]);
             }
         __syncthreads();
         float f[NB][2];
@@ -211,7 +226,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
                 const float safe = top == -INFINITY ? 0.f : top;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) sum += ml[w].y * exp2_fast(ml[w].x - safe);
-                f[b][c] = exp2_fast(m[b][c] - safe) * (u_top * (1.f / 128.f));
+                f[b][c] = exp2_fast(m[b][c] * unit[b][c] - safe) * (u_top * (1.f / 128.f));
                 if (warp == 0 && g == 0 && r < now.tile.rows) part.sums[entry * kRows + r] = make_float2(top, sum);
             }
         // element of accumulator i, row g + 8 j: see the values' order below
@@ -245,10 +260,12 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
     };
 
     open();
+    int slot = 0;
+    uint32_t phase = 0;
     for (int i = 0; i < count; ++i) {
-        const int slot = i % S::kCount, key0 = now.unit * kUnit + kKeys * warp;
+        const int key0 = now.unit * kUnit + kKeys * warp;
         const uint32_t stage = stage_at(slot), scales = scales_at(slot);
-        wait_for(full(slot), (i / S::kCount) & 1, &dead, p.status);
+        wait_for(full(slot), phase, &dead, p.status);
         if (key0 < now.tile.keys) {
             // ---- scores of 32 keys: rows g and g + 8 of product j are keys 16 j + g and 16 j + 8 + g of the warp's
             float s[NB][2][4];
@@ -258,14 +275,14 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
                 uint32_t w[2][kWords];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int key = 16 * j + 8 * h + g;
+                    const uint32_t at = stage + k_lane + (16 * j + 8 * h) * S::kRow;
                     if constexpr (kWords == 2) {
-                        const uint2 v = lds64(stage + place(key * (S::kRow / 16) + (t >> 1)) + 8 * (t & 1));
+                        const uint2 v = lds64(at);
                         w[h][0] = v.x, w[h][1] = v.y;
                     } else {
 #pragma unroll
                         for (int c = 0; c < kWords / 4; ++c) {
-                            const uint4 v = lds128(stage + place(key * (S::kRow / 16) + t * (kWords / 4) + c));
+                            const uint4 v = lds128(at ^ (16 * c));
                             w[h][4 * c] = v.x, w[h][4 * c + 1] = v.y, w[h][4 * c + 2] = v.z, w[h][4 * c + 3] = v.w;
                         }
                     }
@@ -279,8 +296,8 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
                     uint32_t a[4];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if constexpr (BITS == 4) a[h] = pair4(w[h][st / 2], 2 * (st & 1)), a[2 + h] = pair4(w[h][st / 2], 2 * (st & 1) + 1);
-                        else a[h] = pair8(w[h][st], 0), a[2 + h] = pair8(w[h][st], 1);
+                        if constexpr (BITS == 4) a[h] = unpack(w[h][st / 2], 2 * (st & 1)), a[2 + h] = unpack(w[h][st / 2], 2 * (st & 1) + 1);
+                        else a[h] = unpack(w[h][st], 0), a[2 + h] = unpack(w[h][st], 1);
                     }
 #pragma unroll
                     for (int b = 0; b < NB; ++b) mma16816(s[b][j], a[0], a[1], a[2], a[3], qb[b][st][0], qb[b][st][1]);
@@ -289,21 +306,25 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
             // ---- scales, masks, probabilities
             float u[4];  // keys 8 x + g
             bool over = false;
+            const bool edge = key0 + kKeys > least;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const uint32_t at = scales + 2 * (8 * x + g);
-                const int key = key0 + 8 * x + g;
                 const float f = lds_half(at);
-                u[x] = key < now.tile.keys ? lds_half(at + 2 * kKeys) : 0.f;
+                u[x] = lds_half(at + 2 * kKeys);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) s[b][x >> 1][2 * (x & 1)] *= f, s[b][x >> 1][2 * (x & 1) + 1] *= f;
+                if (edge) {
+                    const int key = key0 + 8 * x + g;
+                    u[x] = key < now.tile.keys ? u[x] : 0.f;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) s[b][x >> 1][2 * (x & 1) + c] = key < limit[b][c] ? s[b][x >> 1][2 * (x & 1) + c] : -INFINITY;
+                }
                 over |= u[x] > u_top;
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float& v = s[b][x >> 1][2 * (x & 1) + c];
-                        v = key < limit[b][c] ? v * f * row_scale_log2[b][c] : -INFINITY;
-                        over |= v > m[b][c] + 8.f;
-                    }
+                for (int b = 0; b < NB; ++b) over |= s[b][x >> 1][2 * (x & 1)] > over_at[b][0] || s[b][x >> 1][2 * (x & 1) + 1] > over_at[b][1];
             }
             if (__any_sync(0xFFFFFFFFu, over)) {
                 float most = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3]));
@@ -322,8 +343,8 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
                         top = fmaxf(top, m[b][c]);
-                        const float f = top == -INFINITY ? 1.f : exp2_fast(m[b][c] - top);
-                        m[b][c] = top, l[b][c] *= f;
+                        const float f = top == -INFINITY ? 1.f : exp2_fast((m[b][c] - top) * unit[b][c]);
+                        m[b][c] = top, l[b][c] *= f, over_at[b][c] = top == -INFINITY ? top : top + 8.f / unit[b][c];
 #pragma unroll
                         for (int k = 0; k < kSteps; ++k) o[b][k][c] *= f * less, o[b][k][2 + c] *= f * less;
                     }
@@ -331,10 +352,11 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
             uint32_t pb[NB][4];  // keys 8 x + 2 t and + 1 of query 8 b + g
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const float r0 = m[b][0] == -INFINITY ? 0.f : m[b][0], r1 = m[b][1] == -INFINITY ? 0.f : m[b][1];
+                const float r0 = m[b][0] == -INFINITY ? 0.f : -m[b][0] * unit[b][0], r1 = m[b][1] == -INFINITY ? 0.f : -m[b][1] * unit[b][1];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float e0 = exp2_fast(s[b][x >> 1][2 * (x & 1)] - r0), e1 = exp2_fast(s[b][x >> 1][2 * (x & 1) + 1] - r1), v = u[x] * u_unit;
+                    const float e0 = exp2_fast(fmaf(s[b][x >> 1][2 * (x & 1)], unit[b][0], r0)), e1 = exp2_fast(fmaf(s[b][x >> 1][2 * (x & 1) + 1], unit[b][1], r1)),
+                                v = u[x] * u_unit;
                     l[b][0] += e0, l[b][1] += e1;
                     pb[b][x] = transpose8(half_pair(e0 * v, e1 * v));
                 }
@@ -344,24 +366,22 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend(const AttendParams p,
 #pragma unroll
             for (int c = 0; c < kMats; ++c) {
                 uint32_t r[4];  // keys 8 x of chunk c
-                ldmatrix4_trans(stage + kKeys * S::kRow + place(lane * kMats + c), r);
+                ldmatrix4_trans((stage + v_lane) ^ (16 * c), r);
 #pragma unroll
                 for (int n = 0; n < kPer; n += 2)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t a[4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if constexpr (BITS == 4) a[h] = pair4(r[2 * j], n + h), a[2 + h] = pair4(r[2 * j + 1], n + h);
-                            else a[h] = pair8(r[2 * j], n + h), a[2 + h] = pair8(r[2 * j + 1], n + h);
-                        }
+                        for (int h = 0; h < 2; ++h) a[h] = unpack(r[2 * j], n + h), a[2 + h] = unpack(r[2 * j + 1], n + h);
 #pragma unroll
                         for (int b = 0; b < NB; ++b) mma16816(o[b][(c * kPer + n) / 2], a[0], a[1], a[2], a[3], pb[b][2 * j], pb[b][2 * j + 1]);
                     }
             }
         }
         __syncwarp();
-        fetch(i + S::kCount);
+        fetch(slot);
+        if (++slot == S::kCount) slot = 0, phase ^= 1;
         if (now.unit + 1 == now.units || i + 1 == count) {
             close(run.from + i + 1);
             now.next_pair(p, part);
@@ -452,7 +472,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p) {
     }
 }
 
-// A half of the cache as boxes of a page's rows of a head, at most kKeys of them: {bytes of a row, rows of a page, pages}
+// A half of the cache's codes as boxes of a page's rows of a head, at most kKeys of them: {bytes of a row, rows of a page, pages}
 static bool encode_half(CUtensorMap* map, const Half& half, const Cache& cache, int row_bytes) {
     const EncodeTiledFn encode = encode_tiled();
     if (encode == nullptr) return false;
@@ -482,9 +502,9 @@ static cudaError_t attend_form(const bfq_plan* plan, const AttendParams& p, int*
         *ctas = plan->sm_count * occ;
         return cudaSuccess;
     }
-    CUtensorMap k_map, v_map;
-    if (!encode_half(&k_map, p.cache.k, p.cache, S::kRow) || !encode_half(&v_map, p.cache.v, p.cache, S::kRow)) return cudaErrorInvalidValue;
-    return launch_overlapped(k_attend<D, BITS, NB>, dim3(unsigned(plan->sm_count * occ)), dim3(kAttendThreads), S::kSmem, st, p, k_map, v_map);
+    Maps maps;
+    if (!encode_half(&maps.k_codes, p.cache.k, p.cache, S::kRow) || !encode_half(&maps.v_codes, p.cache.v, p.cache, S::kRow)) return cudaErrorInvalidValue;
+    return launch_overlapped(k_attend<D, BITS, NB>, dim3(unsigned(plan->sm_count * occ)), dim3(kAttendThreads), S::kSmem, st, p, maps);
 }
 template <int D, int BITS>
 static cudaError_t attend_rows(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {

@@ -186,15 +186,35 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
 }
 // Codes of a word as exact fp16 pairs (one of the lower half, one of the upper): the code's bits, its top one inverted, lie in the mantissa of
 // 1024 .. 2047.  4 bits: codes i and i + 4, i < 4; the odd ones lie four places up there, 1152 + 16 code.  8 bits: codes i and i + 2, i < 2.
-__device__ __forceinline__ uint32_t pair4(uint32_t w, int i) {
-    if (i >= 2) w >>= 8;
-    return i & 1 ? fma_pair((w & 0x00F000F0u) ^ 0x64806480u, 0x2C002C00u, 0xD480D480u)  // / 16 - 72
-                 : sub_pair((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);             // - 1032
-}
-__device__ __forceinline__ uint32_t pair8(uint32_t w, int i) {
-    if (i) w >>= 8;
-    return sub_pair((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);  // - 1152
-}
+// Masks and bases are kept in registers that the compiler cannot see through: as constants, two of them in one operation, it makes two
+// operations of each (of the kernel for few rows' 850 instructions for 32 keys of 4 bits 130).
+template <int BITS>
+struct Unpack {
+    uint32_t mask, base, mask_up, base_up;
+    __device__ __forceinline__ Unpack() {
+        asm volatile("mov.u32 %0, %1;" : "=r"(mask) : "n"(BITS == 4 ? 0x000F000F : 0x00FF00FF));
+        asm volatile("mov.u32 %0, %1;" : "=r"(base) : "n"(BITS == 4 ? 0x64086408 : 0x64806480));  // 1032, 1152
+        if constexpr (BITS == 4) {
+            asm volatile("mov.u32 %0, %1;" : "=r"(mask_up) : "n"(0x00F000F0));
+            asm volatile("mov.u32 %0, %1;" : "=r"(base_up) : "n"(0x64806480));  // 1152
+        }
+    }
+    __device__ __forceinline__ static uint32_t and_xor(uint32_t a, uint32_t b, uint32_t c) {
+        uint32_t d;
+        asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+        return d;
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t w, int i) const {
+        if constexpr (BITS == 4) {
+            if (i >= 2) w >>= 8;
+            return i & 1 ? fma_pair(and_xor(w, mask_up, base_up), 0x2C002C00u, 0xD480D480u)  // / 16 - 72
+                         : sub_pair(and_xor(w, mask, base), base);
+        } else {
+            if (i) w >>= 8;
+            return sub_pair(and_xor(w, mask, base), base);
+        }
+    }
+};
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     } else if (warp < 12) {
         // ---- codes to operands -------------------------------------------------------------------------------------------------
         const int r = tid - 256, w = r >> 5;
+        const Unpack<BITS> unpack;
         // 16-byte pieces: the eight lanes of a phase of the stores below write chunks of one half to eight different places of 16 bytes
         constexpr int kPer = BITS == 4 ? 2 : 4;          // pieces of 64 elements
         constexpr int kKeys = 32 / (kPer * (D / 64));    // keys of a warp's 32 pieces
@@ -321,11 +322,11 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 if constexpr (BITS == 4) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        store16(row + (((4 * part_of + j) ^ (key & 7)) << 4), pair4(x[j], 0), pair4(x[j], 1), pair4(x[j], 2), pair4(x[j], 3));
+                        store16(row + (((4 * part_of + j) ^ (key & 7)) << 4), unpack(x[j], 0), unpack(x[j], 1), unpack(x[j], 2), unpack(x[j], 3));
                 } else {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        store16(row + (((2 * part_of + j) ^ (key & 7)) << 4), pair8(x[2 * j], 0), pair8(x[2 * j], 1), pair8(x[2 * j + 1], 0), pair8(x[2 * j + 1], 1));
+                        store16(row + (((2 * part_of + j) ^ (key & 7)) << 4), unpack(x[2 * j], 0), unpack(x[2 * j], 1), unpack(x[2 * j + 1], 0), unpack(x[2 * j + 1], 1));
                 }
             }
         };
