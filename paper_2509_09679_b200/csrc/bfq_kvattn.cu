@@ -392,83 +392,88 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     }
 }
 
-// Joins a row's partial results (the shared prefix's, then its sequence's), turns it back by Q^T and rounds it once.  A warp for each
-// (token, query head).
+// Joins a row's partial results (the shared prefix's, then its sequence's), turns it back by Q^T and rounds it once.  A row is a (token, query
+// head); a warp takes `each` consecutive ones.
 template <int D>
-__global__ void __launch_bounds__(128) k_join(const AttendParams p) {
+__global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
     constexpr int kE = D / 32;
     const int lane = threadIdx.x & 31;
     grid_dep_wait();
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    const int q_heads = p.q.heads;
-    if (row >= p.tokens * q_heads) return;
-    const int token = static_cast<int>(row / q_heads), head = static_cast<int>(row % q_heads), h = head / p.group;
-    int b = token, place = 0;
-    if (token < first_token(p, 0) || token >= first_token(p, p.batch)) return;  // rows of no sequence stay as they are
-    if (p.q_starts != nullptr) {                   // the last sequence that starts at or before this token
-        int lo = 0, hi = p.batch;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (first_token(p, mid) <= token) lo = mid;
-            else hi = mid;
-        }
-        b = lo, place = token - first_token(p, b);
-    }
+    const int rows_all = static_cast<int>(p.tokens) * p.q.heads, row0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * each;
+    if (row0 >= rows_all) return;
     Turn<D, kE, true> turn;
     turn.load(p.tw, lane);
-    float m = -INFINITY, l = 0.f, o[kE];
-#pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = 0.f;
-    auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
-        const Part& part = tall ? p.tall : p.few;
-        const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
-        if (tile_of(p, part, entry).keys == 0) return;
-        const int pair = entry * p.cache.heads + h;
-        const int2 ctas = load_plain(part.pairs + pair);
-        const int64_t first = static_cast<int64_t>(ctas.x) + pair;
-        for (int i0 = 0; i0 < ctas.y; i0 += 32) {  // a lane has one of 32 results' m and l
-            const int n = ctas.y - i0 < 32 ? ctas.y - i0 : 32;
-            const float2 ml = lane < n ? load_plain(part.sums + (first + i0 + lane) * rows + r) : make_float2(-INFINITY, 0.f);
-            float top = ml.x;
-#pragma unroll
-            for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-            top = fmaxf(top, m);
-            const float safe = top == -INFINITY ? 0.f : top, old = exp2_fast(m - safe), mine = exp2_fast(ml.x - safe);
-            float sum = mine * ml.y;
-#pragma unroll
-            for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-            m = top, l = l * old + sum;
-#pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] *= old;
-#pragma unroll 8
-            for (int i = 0; i < n; ++i) {
-                const float f = __shfl_sync(0xFFFFFFFFu, mine, i);
-                const float* at = part.parts + ((first + i0 + i) * rows + r) * D + kE * lane;
-                if constexpr (kE == 4) {
-                    const float4 u = load_plain(reinterpret_cast<const float4*>(at));
-                    o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]), o[2] = fmaf(f, u.z, o[2]), o[3] = fmaf(f, u.w, o[3]);
-                } else {
-                    const float2 u = load_plain(reinterpret_cast<const float2*>(at));
-                    o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]);
+    const int q_heads = p.q.heads, begin = first_token(p, 0), end = first_token(p, p.batch);
+    int of = -1, b = 0, place = 0;  // token that b and place are of
+    for (int row = row0; row < row0 + each && row < rows_all; ++row) {
+        const int token = row / q_heads, head = row - token * q_heads, h = head / p.group;
+        if (token < begin || token >= end) continue;  // rows of no sequence stay as they are
+        if (token != of) {
+            of = b = token, place = 0;
+            if (p.q_starts != nullptr) {  // the last sequence that starts at or before this token
+                int lo = 0, hi = p.batch;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (first_token(p, mid) <= token) lo = mid;
+                    else hi = mid;
                 }
+                b = lo, place = token - first_token(p, b);
             }
         }
-    };
-    if (p.prefix_length > 0) join(p.prefix_tall != 0, -1, token * p.group + head % p.group);
-    if (place < p.max_new) join(p.seq_tall != 0, b, place * p.group + head % p.group);
-    else if (lane == 0) atomicExch(p.status, kBadIndex);  // more new tokens than the call was told
-    const float f = l > 0.f || l != l ? 1.f / l : 0.f;
+        float m = -INFINITY, l = 0.f, o[kE];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] *= f;
-    turn.apply(o);
-    uint8_t* out = const_cast<uint8_t*>(p.out.data) + (token * p.out.token + head * p.out.head + kE * lane) * 2;
-    if constexpr (kE == 4) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]));
-    else *reinterpret_cast<uint32_t*>(out) = bf16_pair(o[0], o[1]);
-    if (p.lse != nullptr && lane == 0) p.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-    // a length or a start outside its range was taken as the nearest one inside
-    if (lane == 0 && head == 0 && place == 0) {
-        const int n = load_plain(p.lengths + b);
-        if (n != cached_keys(p, b)) atomicExch(p.status, kBadIndex);
+        for (int e = 0; e < kE; ++e) o[e] = 0.f;
+        auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
+            const Part& part = tall ? p.tall : p.few;
+            const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
+            if (tile_of(p, part, entry).keys == 0) return;
+            const int pair = entry * p.cache.heads + h;
+            const int2 ctas = load_plain(part.pairs + pair);
+            const int64_t first = static_cast<int64_t>(ctas.x) + pair;
+            for (int i0 = 0; i0 < ctas.y; i0 += 32) {  // a lane has one of 32 results' m and l
+                const int n = ctas.y - i0 < 32 ? ctas.y - i0 : 32;
+                const float2 ml = lane < n ? load_plain(part.sums + (first + i0 + lane) * rows + r) : make_float2(-INFINITY, 0.f);
+                float top = ml.x;
+#pragma unroll
+                for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                top = fmaxf(top, m);
+                const float safe = top == -INFINITY ? 0.f : top, old = exp2_fast(m - safe), mine = exp2_fast(ml.x - safe);
+                float sum = mine * ml.y;
+#pragma unroll
+                for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+                m = top, l = l * old + sum;
+#pragma unroll
+                for (int e = 0; e < kE; ++e) o[e] *= old;
+#pragma unroll 8
+                for (int i = 0; i < n; ++i) {
+                    const float f = __shfl_sync(0xFFFFFFFFu, mine, i);
+                    const float* at = part.parts + ((first + i0 + i) * rows + r) * D + kE * lane;
+                    if constexpr (kE == 4) {
+                        const float4 u = load_plain(reinterpret_cast<const float4*>(at));
+                        o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]), o[2] = fmaf(f, u.z, o[2]), o[3] = fmaf(f, u.w, o[3]);
+                    } else {
+                        const float2 u = load_plain(reinterpret_cast<const float2*>(at));
+                        o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]);
+                    }
+                }
+            }
+        };
+        if (p.prefix_length > 0) join(p.prefix_tall != 0, -1, token * p.group + head % p.group);
+        if (place < p.max_new) join(p.seq_tall != 0, b, place * p.group + head % p.group);
+        else if (lane == 0) atomicExch(p.status, kBadIndex);  // more new tokens than the call was told
+        const float f = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[e] *= f;
+        turn.apply(o);
+        uint8_t* out = const_cast<uint8_t*>(p.out.data) + (token * p.out.token + head * p.out.head + kE * lane) * 2;
+        if constexpr (kE == 4) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]));
+        else *reinterpret_cast<uint32_t*>(out) = bf16_pair(o[0], o[1]);
+        if (p.lse != nullptr && lane == 0) p.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        // a length or a start outside its range was taken as the nearest one inside
+        if (lane == 0 && head == 0 && place == 0) {
+            const int n = load_plain(p.lengths + b);
+            if (n != cached_keys(p, b)) atomicExch(p.status, kBadIndex);
+        }
     }
 }
 
@@ -617,8 +622,10 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
         if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, st);
         if (e == cudaSuccess) {
-            const dim3 grid(unsigned((p.tokens * p.q.heads + 3) / 4));
-            e = plan->n == 64 ? launch_overlapped(kv::k_join<64>, grid, dim3(128), 0, st, p) : launch_overlapped(kv::k_join<128>, grid, dim3(128), 0, st, p);
+            // a warp for each row where that is fewer than the chip runs at once; more would only load the butterfly's constants again
+            const int64_t rows = p.tokens * p.q.heads, warps = int64_t(plan->sm_count) * 16, each = (rows + warps - 1) / warps;
+            const dim3 grid(unsigned((rows + 4 * each - 1) / (4 * each)));
+            e = plan->n == 64 ? launch_overlapped(kv::k_join<64>, grid, dim3(128), 0, st, p, int(each)) : launch_overlapped(kv::k_join<128>, grid, dim3(128), 0, st, p, int(each));
         }
     }
     if (e == cudaSuccess) return BFQ_OK;

@@ -162,14 +162,6 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     return run;
 }
 
-// page of a key: -1, and reported, if the block table has none of the cache's
-__device__ __forceinline__ int64_t page_of(const AttendParams& p, const Tile& tile, int key) {
-    const int page = load_plain(tile.pages + (key >> p.cache.page_shift));
-    if (page >= 0 && page < p.cache.pages) return page;
-    atomicExch(p.status, kBadIndex);
-    return -1;
-}
-
 __device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));

@@ -1,15 +1,18 @@
 // Attention of many query rows over the same keys of the paged low-bit cache (a shared prefix for a batch, chunks of a prompt) on the
-// fifth-generation tensor cores: the same formula, references and scales as the kernel for few rows (bfq_kvattn.cu).
+// fifth-generation tensor cores: the same formula and references as the kernel for few rows (bfq_kvattn.cu).
 //
 // A CTA has up to 256 rows, two M = 128 tiles, and takes its keys in units of 128:
 //   warps 0 .. 3, 4 .. 7  softmax of tile 0, 1: a thread owns a row (a lane of tensor memory).  Two walks over the row's 128 scores, the first
 //                         for the largest (a new reference and a pass over the products only where a score passes the old one by more than
-//                         8, as there), the second for exp2, sum, value scales and the rounding to fp16, which goes back to tensor memory over the
-//                         scores;
+//                         8, as there), the second for exp2, sum and the rounding to fp16, which goes back to tensor memory over the scores;
 //   warps 8 .. 11         codes to fp16: a unit's keys and values into one of two stages, loaded one unit ahead into registers;
 //   warp 12, one thread   the MMAs: S = Q K^T (both operands in shared memory), O += P V (P from tensor memory).
 // The order of the MMAs, S0 S1 | O0 S0' O1 S1' | ..., lets the softmax of one tile run beside the products of the other; scores and
 // probabilities share their columns, so tensor memory holds 2 x 128 columns of scores and 2 x D of products.
+// Keys and values are multiplied by their scales on the way into shared memory, over a power of two for all of a pair so far: one rounding to
+// fp16 of each element, 2^-12 on average and independent of its neighbours, a fraction of the output's own rounding.  Applied exactly, to
+// scores and probabilities, the scales would be read from shared memory 256 times by every softmax warp for a unit, which took three times as
+// long as everything else.
 // Shared-memory operands have the 128-byte swizzle: a row of 128 bytes is 64 elements d of one key (or query row), the two halves of
 // D = 128 lie one after the other; K is K-major, V the same bytes read MN-major.  The d within a 16-byte chunk stand in the order in which a
 // code word's pairs come out (0 4 1 5 2 6 3 7, or 0 2 1 3 of each four): Q's rows are stored in that order too, and O's columns are
@@ -20,16 +23,15 @@
 namespace bfq {
 namespace kv {
 
-constexpr int kTallThreads = 13 * 32;
+constexpr int kTallThreads = 16 * 32;  // warps 13 .. 15 only lend their registers
 constexpr int kConvert = 128;  // threads that turn codes into operands
 
 template <int D>
 struct TallSmem {
     static constexpr uint32_t kHalves = D / 64, kTile = kHalves * 128 * 128;  // 128 rows
     static constexpr uint32_t kQ = 0, kStages = 2 * kTile, kStage = 2 * kTile;  // a stage: keys, values
-    static constexpr uint32_t kScales = kStages + 2 * kStage;  // per stage: 128 key scales, 128 value scales (fp32), factor, unit
-    static constexpr uint32_t kScalesBytes = 2 * 128 * 4 + 16;
-    static constexpr uint32_t kBars = kScales + 2 * kScalesBytes;
+    static constexpr uint32_t kFactors = kStages + 2 * kStage;  // per stage: less, unit of the products, unit of the scores
+    static constexpr uint32_t kBars = kFactors + 2 * 16;
     static constexpr uint32_t kBytes = kBars + 16 * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
 enum Bar { kKvFull = 0, kKvEmpty = 2, kSFull = 4, kPFull = 6, kQFull = 8, kOFull = 10, kBarCount = 12 };
@@ -80,12 +82,12 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     __shared__ long long scan[kTallThreads / 32 + 2];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int dead;
-    __shared__ float warp_top[kConvert / 32];
+    __shared__ float2 warp_top[2][kConvert / 32];  // of the keys' scales, the values'
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     auto bar = [&](int b) { return base + M::kBars + 8u * b; };
     auto stage_at = [&](int s) { return base + M::kStages + s * M::kStage; };
-    auto scales_at = [&](int s) { return base + M::kScales + s * M::kScalesBytes; };
+    auto factors_at = [&](int s) { return base + M::kFactors + 16u * s; };
     grid_dep_wait();
     const Part& part = p.tall;
     Walk walk;
@@ -108,7 +110,9 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     auto products = [&](int tile) { return tmem + 256u + D * tile; };
     const int count = run.count;
 
+    // registers: 256 x 168 + 128 x 112 + 128 x 64 = 512 x 128, what the block was launched with
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         // ---- softmax ---------------------------------------------------------------------------------------------------------
         const int tile = warp >> 2, row_of_tile = tid & 127;
         const uint32_t lanes = uint32_t(warp & 3) << 21;  // 32 lanes of tensor memory
@@ -127,7 +131,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             const int token = t.token0 + row / p.group, head = walk.head * p.group + row % p.group;
             const uint4* at = reinterpret_cast<const uint4*>(p.q.data + (there ? (token * p.q.token + head * p.q.head) * 2 : 0));
             float top = 0.f;
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < D / 8; ++c) {
                 const uint4 v = there ? load_plain(at + c) : make_uint4(0, 0, 0, 0);
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -137,7 +141,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             const RowPower power(top);
             const float up = p.scale_log2 < 0.f ? -power.up : power.up;
             row_scale = fabsf(p.scale_log2) * power.down;
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < D / 8; ++c) {
                 const uint4 v = there ? load_plain(at + c) : make_uint4(0, 0, 0, 0);
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -162,7 +166,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 const bool there = r < walk.tile.rows;
                 const long long entry = static_cast<long long>(blockIdx.x) + pair;
                 float* const to = part.parts + (entry * kTallRows + r) * D;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t v[32];
                     tmem_ld32(o_at + 32 * c, v);
@@ -188,83 +192,75 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         open();
         for (int i = 0; i < count; ++i) {
             if (active) {
-                const uint32_t k_scales = scales_at(i & 1), v_scales = k_scales + 512;
                 const int key0 = walk.unit * kUnit;
                 const bool edge = key0 + kUnit > least;  // some row of the warp ends in this unit, or has ended
-                wait_for(bar(kKvFull + (i & 1)), (i >> 1) & 1, &dead, p.status);  // for the scales
+                wait_for(bar(kKvFull + (i & 1)), (i >> 1) & 1, &dead, p.status);  // for the factors
                 wait_for(bar(kSFull + tile), s_phase, &dead, p.status);
                 s_phase ^= 1;
                 tmem_fence_after();
-                const float4 head = load_shared4(k_scales + 1024);
-                const float less = head.x;
-                unit = head.y;
+                const float4 factors = load_shared4(factors_at(i & 1));
+                const float less = factors.x, scale = fmaxf(row_scale * factors.z, 1e-30f);  // -infinity times it is that
+                unit = factors.y;
                 float most = -INFINITY;
-#pragma unroll
+                // compact loops: unrolled over the whole row, with the masks that few units need, the instruction cache missed all the time
+#pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     uint32_t v[32];
                     tmem_ld32(s_at + 32 * c, v);
                     tmem_wait_ld32(v);
+                    if (edge) {
+                        const int n = limit - key0 - 32 * c;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 ks = load_shared4(k_scales + 16 * (8 * c + j));
-                        float x[4];
-                        unpack2(mul2(pack2u(v[4 * j], v[4 * j + 1]), pack2(ks.x, ks.y)), x[0], x[1]);
-                        unpack2(mul2(pack2u(v[4 * j + 2], v[4 * j + 3]), pack2(ks.z, ks.w)), x[2], x[3]);
-                        if (edge) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] = key0 + 32 * c + 4 * j + e < limit ? x[e] : -INFINITY;
-                        }
-                        most = fmaxf(fmaxf(most, fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
+                        for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0xFF800000u;
                     }
+                    float x[4] = {most, most, most, most};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j & 3] = fmaxf(x[j & 3], __uint_as_float(v[j]));
+                    most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
                 }
-                most = most == -INFINITY ? most : most * row_scale;
+                most = most == -INFINITY ? most : most * scale;
                 const bool over = most > m + 8.f;
                 if (first) {
                     m = most;
                 } else if (__any_sync(0xFFFFFFFFu, over) || less != 1.f) {
                     float f = less;
                     if (over) f *= exp2_fast(m - most), l *= exp2_fast(m - most), m = most;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 16; ++c) {
-                        uint32_t v[16];
-                        tmem_ld16(o_at + 16 * c, v);
-                        tmem_wait_ld16(v);
+                        uint32_t w[16];
+                        tmem_ld16(o_at + 16 * c, w);
+                        tmem_wait_ld16(w);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-                        tmem_st16(o_at + 16 * c, v);
+                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+                        tmem_st16(o_at + 16 * c, w);
                     }
                 }
                 first = false;
                 const float ref = m == -INFINITY ? 0.f : m;
-                const u64 scale2 = pack2(row_scale, row_scale), ref2 = pack2(-ref, -ref);
-                u64 sum2 = pack2(0.f, 0.f);
-#pragma unroll
+                const u64 scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
+                u64 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     uint32_t v[32], out[16];
                     tmem_ld32(s_at + 32 * c, v);
                     tmem_wait_ld32(v);
+                    if (edge) {
+                        const int n = limit - key0 - 32 * c;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 ks = load_shared4(k_scales + 16 * (8 * c + j)), us = load_shared4(v_scales + 16 * (8 * c + j));
+                        for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0xFF800000u;
+                    }
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float a, b;
-                            const u64 kk = h ? pack2(ks.z, ks.w) : pack2(ks.x, ks.y);
-                            unpack2(fma2(mul2(pack2u(v[4 * j + 2 * h], v[4 * j + 2 * h + 1]), kk), scale2, ref2), a, b);
-                            if (edge) {
-                                const int key = key0 + 32 * c + 4 * j + 2 * h;
-                                a = key < limit ? a : -INFINITY, b = key + 1 < limit ? b : -INFINITY;
-                            }
-                            const u64 e2 = pack2(exp2_fast(a), exp2_fast(b));
-                            sum2 = add2(sum2, e2);
-                            unpack2(mul2(e2, h ? pack2(us.z, us.w) : pack2(us.x, us.y)), a, b);
-                            out[2 * j + h] = half_pair(a, b);
-                        }
+                    for (int j = 0; j < 16; ++j) {
+                        float a, b;
+                        unpack2(fma2(pack2u(v[2 * j], v[2 * j + 1]), scale2, ref2), a, b);
+                        a = exp2_fast(a), b = exp2_fast(b);
+                        sum2[j & 1] = add2(sum2[j & 1], pack2(a, b));
+                        out[j] = half_pair(a, b);
                     }
                     tmem_st16(s_at + 16 * c, out);
                 }
                 float a, b;
-                unpack2(sum2, a, b);
+                unpack2(add2(sum2[0], sum2[1]), a, b);
                 l += a + b;
                 tmem_wait_st();
                 tmem_fence_before();
@@ -280,91 +276,106 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             }
         }
     } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
         // ---- codes to operands -------------------------------------------------------------------------------------------------
-        const int r = tid - 256, w = r >> 5;
+        const int w = warp - 8;
         const Unpack<BITS> unpack;
         // 16-byte pieces: the eight lanes of a phase of the stores below write chunks of one half to eight different places of 16 bytes
-        constexpr int kPer = BITS == 4 ? 2 : 4;          // pieces of 64 elements
-        constexpr int kKeys = 32 / (kPer * (D / 64));    // keys of a warp's 32 pieces
+        constexpr int kPer = BITS == 4 ? 2 : 4;        // pieces of 64 elements
+        constexpr int kKeys = 32 / (kPer * (D / 64));  // keys of a warp's 32 pieces: of one page
         constexpr int kTurns = kUnit / kKeys / 4;
         const int part_of = lane % kPer, key_low = lane / kPer % (8 / kPer);
         const int half = D == 128 ? lane >> 3 & 1 : 0, key_of = key_low + (8 / kPer) * (D == 128 ? lane >> 4 : lane >> 3);
         uint4 k_raw[kTurns], v_raw[kTurns];
-        uint32_t scale_raw = 0;
+        uint32_t scales[kTurns];  // of the key in the lower half, of the value in the upper
+        constexpr int64_t kNone = -(int64_t(1) << 32);
+        int64_t page = kNone;  // lane c: of turn c; kNone: it has no keys
+        auto look = [&]() {
+            const int key = walk.unit * kUnit + (lane * 4 + w) * kKeys;
+            page = lane < kTurns && key < walk.tile.keys ? load_plain(walk.tile.pages + (key >> p.cache.page_shift)) : kNone;
+        };
         auto load = [&]() {
             const int mask = (1 << p.cache.page_shift) - 1;
+            if (page != kNone && (page < 0 || page >= p.cache.pages)) atomicExch(p.status, kBadIndex), page = kNone;
 #pragma unroll
             for (int c = 0; c < kTurns; ++c) {
                 const int key = walk.unit * kUnit + (c * 4 + w) * kKeys + key_of;
-                const int64_t page = key < walk.tile.keys ? page_of(p, walk.tile, key) : -1;
-                k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0);
-                if (page >= 0) {
-                    const int at = 16 * (half * kPer + part_of);
-                    k_raw[c] = load_plain(reinterpret_cast<const uint4*>(codes_of<kRow>(p.cache.k, p.cache.page_shift, page, walk.head, key & mask) + at));
-                    v_raw[c] = load_plain(reinterpret_cast<const uint4*>(codes_of<kRow>(p.cache.v, p.cache.page_shift, page, walk.head, key & mask) + at));
-                }
-            }
-            const int key = walk.unit * kUnit + r;
-            const int64_t page = key < walk.tile.keys ? page_of(p, walk.tile, key) : -1;
-            scale_raw = 0;
-            if (page >= 0) {
-                const uint32_t a = *static_cast<volatile const uint16_t*>(scale_of(p.cache.k, p.cache.page_shift, page, walk.head, key & mask));
-                const uint32_t b = *static_cast<volatile const uint16_t*>(scale_of(p.cache.v, p.cache.page_shift, page, walk.head, key & mask));
-                scale_raw = a | b << 16;
-            }
-        };
-        auto store = [&](uint32_t to, const uint4 (&raw)[kTurns]) {
-#pragma unroll
-            for (int c = 0; c < kTurns; ++c) {
-                const int key = (c * 4 + w) * kKeys + key_of;
-                const uint32_t row = to + half * 16384 + key * 128;
-                const uint32_t x[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
-                if constexpr (BITS == 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        store16(row + (((4 * part_of + j) ^ (key & 7)) << 4), unpack(x[j], 0), unpack(x[j], 1), unpack(x[j], 2), unpack(x[j], 3));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        store16(row + (((2 * part_of + j) ^ (key & 7)) << 4), unpack(x[2 * j], 0), unpack(x[2 * j], 1), unpack(x[2 * j + 1], 0), unpack(x[2 * j + 1], 1));
+                const int64_t at = __shfl_sync(0xFFFFFFFFu, page, c);
+                k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0), scales[c] = 0;
+                if (at >= 0 && key < walk.tile.keys) {
+                    const int64_t row = (static_cast<int64_t>(walk.head) << p.cache.page_shift) + (key & mask);
+                    const int off = 16 * (half * kPer + part_of);
+                    k_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.k.codes + at * p.cache.k.codes_page + row * kRow + off));
+                    v_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.v.codes + at * p.cache.v.codes_page + row * kRow + off));
+                    const uint32_t a = *static_cast<volatile const uint16_t*>(p.cache.k.scales + at * p.cache.k.scales_page + row);
+                    const uint32_t b = *static_cast<volatile const uint16_t*>(p.cache.v.scales + at * p.cache.v.scales_page + row);
+                    scales[c] = a | b << 16;
                 }
             }
         };
-        float u_top = 0.f;
+        auto times = [](uint32_t a, uint32_t b) {
+            uint32_t d;
+            asm("mul.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+            return d;
+        };
+        auto store = [&](uint32_t to, const uint4& raw, int key, float scale) {
+            const uint32_t row = to + half * 16384 + key * 128, s2 = half_pair(scale, scale);
+            const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
+            if constexpr (BITS == 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    store16(row + (((4 * part_of + j) ^ (key & 7)) << 4), times(unpack(x[j], 0), s2), times(unpack(x[j], 1), s2), times(unpack(x[j], 2), s2),
+                            times(unpack(x[j], 3), s2));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    store16(row + (((2 * part_of + j) ^ (key & 7)) << 4), times(unpack(x[2 * j], 0), s2), times(unpack(x[2 * j], 1), s2),
+                            times(unpack(x[2 * j + 1], 0), s2), times(unpack(x[2 * j + 1], 1), s2));
+            }
+        };
+        // the power of two above all scales of the pair so far, at most that of 65504
+        auto above = [](float top, float most) { return most > top ? __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u) : top; };
+        float k_top = 0.f, v_top = 0.f;
         bool first = true;
+        look();
         load();
         for (int i = 0; i < count; ++i) {
             const int s = i & 1;
-            if (i >= 2) wait_for(bar(kKvEmpty + s), ((i >> 1) - 1) & 1, &dead, p.status);
-            store(stage_at(s), k_raw);
-            store(stage_at(s) + M::kTile, v_raw);
-            const float ks = half_value(static_cast<uint16_t>(scale_raw & 0xFFFFu)), us = half_value(static_cast<uint16_t>(scale_raw >> 16));
-            const bool last_of_pair = walk.unit + 1 == walk.units;
+            float2 most = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < kTurns; ++c)
+                most.x = fmaxf(most.x, half_value(static_cast<uint16_t>(scales[c] & 0xFFFFu))), most.y = fmaxf(most.y, half_value(static_cast<uint16_t>(scales[c] >> 16)));
+            most.x = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.x)));  // not negative: ordered as integers
+            most.y = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.y)));
+            if (lane == 0) warp_top[s][w] = most;
+            bar_sync(1, kConvert);
+#pragma unroll
+            for (int n = 0; n < kConvert / 32; ++n) most.x = fmaxf(most.x, warp_top[s][n].x), most.y = fmaxf(most.y, warp_top[s][n].y);
+            if (first) k_top = v_top = 0x1p-24f;
+            const float v_before = v_top;
+            k_top = above(k_top, most.x), v_top = above(v_top, most.y);
+            const float k_factor = 128.f / k_top, v_factor = 128.f / v_top;  // codes times scales: at most 2^14
+            first = walk.unit + 1 == walk.units;
             walk.next(p, part);
-            if (i + 1 < count) load();
-            // the power of two above all value scales of the pair so far
-            const float top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(us)));  // not negative: ordered as integers
-            if (lane == 0) warp_top[w] = top;
-            bar_sync(1, kConvert);
-            const float most = fmaxf(fmaxf(warp_top[0], warp_top[1]), fmaxf(warp_top[2], warp_top[3]));
-            bar_sync(1, kConvert);
-            float less = 1.f;
-            if (first) u_top = 0x1p-24f, first = false;
-            if (most > u_top) {
-                const float next = __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u);
-                less = u_top / next, u_top = next;
+            if (i + 1 < count) look();
+            if (i >= 2) wait_for(bar(kKvEmpty + s), ((i >> 1) - 1) & 1, &dead, p.status);
+#pragma unroll
+            for (int c = 0; c < kTurns; ++c) {
+                const int key = (c * 4 + w) * kKeys + key_of;
+                store(stage_at(s), k_raw[c], key, k_factor * half_value(static_cast<uint16_t>(scales[c] & 0xFFFFu)));
+                store(stage_at(s) + M::kTile, v_raw[c], key, v_factor * half_value(static_cast<uint16_t>(scales[c] >> 16)));
             }
-            if (last_of_pair) first = true;
-            const uint32_t to = scales_at(s);
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4 * r), "f"(ks) : "memory");
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 512 + 4 * r), "f"(us * (128.f / u_top)) : "memory");
-            if (r == 0) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(to + 1024), "f"(less), "f"(u_top * (1.f / 128.f)) : "memory");
+            if (warp == 8 && lane == 0)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors_at(s)), "f"(v_before / v_top), "f"(v_top * (1.f / 128.f)), "f"(k_top * (1.f / 128.f)), "f"(0.f)
+                             : "memory");
+            if (i + 1 < count) load();
             fence_operands();
             arrive(bar(kKvFull + s));
         }
     } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // ---- MMAs ----------------------------------------------------------------------------------------------------------------
-        if (lane == 0) {
+        if (warp == 12 && lane == 0) {
             uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
             constexpr uint32_t kScoresDesc = instruction(128, 0), kProductsDesc = instruction(D, 1);
             auto issue_scores = [&](int tile, int s) {

@@ -3,10 +3,12 @@
 Tolerances, from the arithmetic (a rounding to bf16 is off by at most 2^-8 of the value, to fp32 by 2^-24):
   * appended rows: the quantizer's rule of tests/parity.py (codes exact but next to a boundary, scales within one fp16 step); queries and rows
     read back: one rounding to the output's type plus fp32 arithmetic, 1e-5 of the row's norm (some thirty operations of 2^-24 each).
-  * attention: with P the probabilities and V the cached values, in the rotated basis each probability is rounded once to bf16 after its value's
-    scale, so |error| <= 2^-8 P |V|.  A score is an fp32 sum of D exact products, off by at most 2^-16 scale |q| |k| (128 additions of 2^-23), which
-    with the exponential's 2^-20 is the relative error of a probability, twice with the sum's; the sums over the keys add 2^-23 a key.  The
-    basis change takes that bound through |Q|, and the result is rounded once: 2^-8 |out|."""
+  * attention: with P the probabilities and V the cached values, in the rotated basis each probability (times its value's scale) is rounded once to
+    fp16, 2^-11, or 2^-32 of the largest where it is that small; where many rows share their keys (tensor-core tiles of 256 rows) keys and values
+    are rounded to fp16 after their scales, 2^-11 of each element.  So |error| <= 2^-10 P |V|, and a score, an fp32 sum of D products,
+    is off by at most (2^-11 where keys are rounded, 2^-16 where not: 128 additions of 2^-23) scale |q| |k|, which with the exponential's
+    2^-20 is the relative error of a probability, twice with the sum's; the sums over the keys add 2^-23 a key.  The basis change takes that
+    bound through |Q|, and the result is rounded once: 2^-8 |out|."""
 import numpy as np
 import pytest
 import torch
@@ -71,12 +73,15 @@ def rope_table(rows, dims):
 
 
 def attention(q, theta, k, v, table, lengths, starts, page, scale, prefix=None, prefix_length=0):
+    # more rows than 16 for one of the key heads' runs of keys: they may go to the tiles of 256 rows
     """-> (out, lse, error bound of out, of lse) [tokens][heads][n]; k, v [pages][heads][page][n], q float64 in the rotated basis."""
     tokens, heads, n = q.shape
     group = heads // k.shape[1]
     out, bound = np.zeros_like(q), np.zeros_like(q)
     lse, lse_bound = np.full((tokens, heads), -np.inf), np.zeros((tokens, heads))
     Q = dense(theta)
+    most = max((starts[b + 1] - starts[b] for b in range(len(lengths))), default=0)
+    rounded = 2.0 ** -11 if group * max(most, (starts[len(lengths)] - starts[0]) if prefix_length else 0) > 16 else 2.0 ** -16
     for b, length in enumerate(lengths):
         first, last = starts[b], starts[b + 1]
         for h in range(heads):
@@ -93,8 +98,9 @@ def attention(q, theta, k, v, table, lengths, starts, page, scale, prefix=None, 
                 e = np.exp(s - s.max())
                 p = e / e.sum()
                 out[t, h] = p @ vs @ Q
-                delta = 2.0 ** -16 * (np.abs(ks) @ np.abs(q[t, h])).max() * abs(scale) + 2.0 ** -20 + 2.0 ** -23 * np.abs(s).max()
-                bound[t, h] = (2.0 ** -8 + 2 * delta + len(ks) * 2.0 ** -23) * (p @ np.abs(vs)) @ np.abs(Q) + (2.0 ** -8 + 1e-6) * np.abs(out[t, h]) + 1e-30
+                delta = rounded * (np.abs(ks) @ np.abs(q[t, h])).max() * abs(scale) + 2.0 ** -20 + 2.0 ** -23 * np.abs(s).max()
+                each = (2.0 ** -10 + 2 * delta + len(ks) * 2.0 ** -23) * (p @ np.abs(vs)) + len(ks) * 2.0 ** -30 * np.abs(vs).max()
+                bound[t, h] = each @ np.abs(Q) + (2.0 ** -8 + 1e-6) * np.abs(out[t, h]) + 1e-30
                 lse[t, h] = s.max() + np.log(e.sum())
                 lse_bound[t, h] = delta + 2.0 ** -22 * abs(lse[t, h]) + len(ks) * 2.0 ** -23
     return out, lse, bound, lse_bound
