@@ -37,6 +37,11 @@ struct TallSmem {
 enum Bar { kKvFull = 0, kKvEmpty = 2, kSFull = 4, kPFull = 6, kQFull = 8, kOFull = 10, kBarCount = 12 };
 
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// the wait of a converged warp
+__device__ __forceinline__ void wait_all(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+    wait_for(bar, parity, dead, status);
+    __syncwarp();
+}
 __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -54,18 +59,28 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
 __host__ __device__ constexpr uint32_t instruction(int n, int v_mn_major) {
     return (1u << 4) | (uint32_t(v_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                 "r"(accumulate)
-                 : "memory");
+// Issued by the one thread of a converged warp whose `lead` is set: a predicate on the instruction and no branch around it, so that the
+// operands can stay in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
-                 "r"(accumulate)
-                 : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+        "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+        : "memory");
 }
-__device__ __forceinline__ void commit_to(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
+        "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void commit_to(uint32_t lead, uint32_t bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead)
+                 : "memory");
 }
 
 // Place i of a 16-byte chunk holds element order(i) of its eight.
@@ -116,7 +131,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         // ---- softmax ---------------------------------------------------------------------------------------------------------
         const int tile = warp >> 2, row_of_tile = tid & 127;
         const uint32_t lanes = uint32_t(warp & 3) << 21;  // 32 lanes of tensor memory
-        const uint32_t s_at = scores(tile) + lanes, o_at = products(tile) + lanes, q_at = base + M::kQ + tile * M::kTile + row_of_tile * 128;
+        const uint32_t s_at = scores(tile) + lanes, o_at = products(tile) + lanes;
         float m = -INFINITY, l = 0.f, row_scale = 0.f, unit = 0.f;
         int limit = 0, least = 0;  // keys of the row; of the warp's rows, at least
         uint32_t s_phase = 0, o_phase = 0;
@@ -126,29 +141,31 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             const Tile& t = walk.tile;
             active = t.rows > 128 * tile;
             if (!active) return;
-            const int r = 128 * tile + row_of_tile, row = t.row0 + r;
-            const bool there = r < t.rows;
-            const int token = t.token0 + row / p.group, head = walk.head * p.group + row % p.group;
-            const uint4* at = reinterpret_cast<const uint4*>(p.q.data + (there ? (token * p.q.token + head * p.q.head) * 2 : 0));
-            float top = 0.f;
+            constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;  // of a row
+            const int first_row = 128 * tile + 32 * (warp & 3), part_of = lane % kLanes;
+            const float sign = p.scale_log2 < 0.f ? -1.f : 1.f;
 #pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                const uint4 v = there ? load_plain(at + c) : make_uint4(0, 0, 0, 0);
+            for (int n = 0; n < 32; n += kRowsAtOnce) {
+                const int r = first_row + n + lane / kLanes, row = t.row0 + r;
+                const int token = t.token0 + row / p.group, head = walk.head * p.group + row % p.group;
+                const uint4 v = r < t.rows ? load_plain(reinterpret_cast<const uint4*>(p.q.data + (token * p.q.token + head * p.q.head + 8 * part_of) * 2)) : make_uint4(0, 0, 0, 0);
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                float top = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
-            }
-            const RowPower power(top);
-            const float up = p.scale_log2 < 0.f ? -power.up : power.up;
-            row_scale = fabsf(p.scale_log2) * power.down;
-#pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                const uint4 v = there ? load_plain(at + c) : make_uint4(0, 0, 0, 0);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int x = 1; x < kLanes; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                const RowPower power(top);
+                const float up = sign * power.up;
                 auto element = [&](int i) { return up * __uint_as_float(order<BITS>(i) & 1 ? w[order<BITS>(i) / 2] & 0xFFFF0000u : w[order<BITS>(i) / 2] << 16); };
-                store16(q_at + (c >> 3) * 16384 + (((c & 7) ^ (row_of_tile & 7)) << 4), half_pair(element(0), element(1)), half_pair(element(2), element(3)),
-                        half_pair(element(4), element(5)), half_pair(element(6), element(7)));
+                const int at = 32 * (warp & 3) + n + lane / kLanes;  // of the tile
+                store16(base + M::kQ + tile * M::kTile + at * 128 + (part_of >> 3) * 16384 + (((part_of & 7) ^ (at & 7)) << 4), half_pair(element(0), element(1)),
+                        half_pair(element(2), element(3)), half_pair(element(4), element(5)), half_pair(element(6), element(7)));
+                const float down = __shfl_sync(0xFFFFFFFFu, power.down, (lane % kRowsAtOnce) * kLanes);
+                if (lane / kRowsAtOnce == n / kRowsAtOnce) row_scale = fabsf(p.scale_log2) * down;  // the lane's own row
             }
+            const int r = 128 * tile + row_of_tile, row = t.row0 + r;
+            const bool there = r < t.rows;
             fence_operands();
             arrive(bar(kQFull + tile));
             m = -INFINITY, l = 0.f;
@@ -165,22 +182,37 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 const int r = 128 * tile + row_of_tile;
                 const bool there = r < walk.tile.rows;
                 const long long entry = static_cast<long long>(blockIdx.x) + pair;
-                float* const to = part.parts + (entry * kTallRows + r) * D;
+                // half of 32 rows at a time through the warp's part of the query tile, which no product reads any more, so that rows are written
+                // whole: 16 bytes at place (chunk ^ row) of a row's half
+                constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
+                const uint32_t own = base + M::kQ + tile * M::kTile + (warp & 3) * (M::kTile / 4);
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t v[32];
-                    tmem_ld32(o_at + 32 * c, v);
-                    tmem_wait_ld32(v);
-                    if (there) {
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32(o_at + (D / 2) * h + 32 * c, v);
+                        tmem_wait_ld32(v);
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             float x[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) x[order<BITS>(i)] = __uint_as_float(v[8 * q + i]) * unit;
-                            reinterpret_cast<float4*>(to + 32 * c + 8 * q)[0] = make_float4(x[0], x[1], x[2], x[3]);
-                            reinterpret_cast<float4*>(to + 32 * c + 8 * q)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                store16(own + lane * 2 * D + (((8 * c + 2 * q + i) ^ (lane & (kLanes - 1))) << 4), __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]),
+                                        __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
                         }
                     }
+                    __syncwarp();
+                    const int chunk = lane % kLanes;
+#pragma unroll 4
+                    for (int n = 0; n < 32; n += kRowsAtOnce) {
+                        const int row = n + lane / kLanes, to = 128 * tile + 32 * (warp & 3) + row;
+                        const float4 x = load_shared4(own + row * 2 * D + ((chunk ^ (row & (kLanes - 1))) << 4));
+                        if (to < walk.tile.rows) *reinterpret_cast<float4*>(part.parts + (entry * kTallRows + to) * D + (D / 2) * h + 4 * chunk) = x;
+                    }
+                    __syncwarp();
                 }
                 tmem_fence_before();
                 if (there) part.sums[entry * kTallRows + r] = make_float2(m, l);
@@ -287,7 +319,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         const int part_of = lane % kPer, key_low = lane / kPer % (8 / kPer);
         const int half = D == 128 ? lane >> 3 & 1 : 0, key_of = key_low + (8 / kPer) * (D == 128 ? lane >> 4 : lane >> 3);
         uint4 k_raw[kTurns], v_raw[kTurns];
-        uint32_t scales[kTurns];  // of the key in the lower half, of the value in the upper
+        uint16_t k_scale[kTurns], v_scale[kTurns];
         constexpr int64_t kNone = -(int64_t(1) << 32);
         int64_t page = kNone;  // lane c: of turn c; kNone: it has no keys
         auto look = [&]() {
@@ -301,15 +333,14 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             for (int c = 0; c < kTurns; ++c) {
                 const int key = walk.unit * kUnit + (c * 4 + w) * kKeys + key_of;
                 const int64_t at = __shfl_sync(0xFFFFFFFFu, page, c);
-                k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0), scales[c] = 0;
+                k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0), k_scale[c] = v_scale[c] = 0;
                 if (at >= 0 && key < walk.tile.keys) {
                     const int64_t row = (static_cast<int64_t>(walk.head) << p.cache.page_shift) + (key & mask);
                     const int off = 16 * (half * kPer + part_of);
                     k_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.k.codes + at * p.cache.k.codes_page + row * kRow + off));
                     v_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.v.codes + at * p.cache.v.codes_page + row * kRow + off));
-                    const uint32_t a = *static_cast<volatile const uint16_t*>(p.cache.k.scales + at * p.cache.k.scales_page + row);
-                    const uint32_t b = *static_cast<volatile const uint16_t*>(p.cache.v.scales + at * p.cache.v.scales_page + row);
-                    scales[c] = a | b << 16;
+                    k_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.k.scales + at * p.cache.k.scales_page + row);
+                    v_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.v.scales + at * p.cache.v.scales_page + row);
                 }
             }
         };
@@ -344,7 +375,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             float2 most = make_float2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < kTurns; ++c)
-                most.x = fmaxf(most.x, half_value(static_cast<uint16_t>(scales[c] & 0xFFFFu))), most.y = fmaxf(most.y, half_value(static_cast<uint16_t>(scales[c] >> 16)));
+                most.x = fmaxf(most.x, half_value(k_scale[c])), most.y = fmaxf(most.y, half_value(v_scale[c]));
             most.x = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.x)));  // not negative: ordered as integers
             most.y = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.y)));
             if (lane == 0) warp_top[s][w] = most;
@@ -362,20 +393,21 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
 #pragma unroll
             for (int c = 0; c < kTurns; ++c) {
                 const int key = (c * 4 + w) * kKeys + key_of;
-                store(stage_at(s), k_raw[c], key, k_factor * half_value(static_cast<uint16_t>(scales[c] & 0xFFFFu)));
-                store(stage_at(s) + M::kTile, v_raw[c], key, v_factor * half_value(static_cast<uint16_t>(scales[c] >> 16)));
+                store(stage_at(s), k_raw[c], key, k_factor * half_value(k_scale[c]));
+                store(stage_at(s) + M::kTile, v_raw[c], key, v_factor * half_value(v_scale[c]));
             }
             if (warp == 8 && lane == 0)
                 asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors_at(s)), "f"(v_before / v_top), "f"(v_top * (1.f / 128.f)), "f"(k_top * (1.f / 128.f)), "f"(0.f)
                              : "memory");
-            if (i + 1 < count) load();
             fence_operands();
             arrive(bar(kKvFull + s));
+            if (i + 1 < count) load();
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // ---- MMAs ----------------------------------------------------------------------------------------------------------------
-        if (warp == 12 && lane == 0) {
+        if (warp == 12) {
+            const uint32_t lead = elect_one();
             uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
             constexpr uint32_t kScoresDesc = instruction(128, 0), kProductsDesc = instruction(D, 1);
             auto issue_scores = [&](int tile, int s) {
@@ -383,45 +415,45 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                    mma_ss(scores(tile), operand(a + off, 0), operand(b + off, 0), kScoresDesc, k > 0);
+                    mma_ss(lead, scores(tile), operand(a + off, 0), operand(b + off, 0), kScoresDesc, k > 0);
                 }
-                commit_to(bar(kSFull + tile));
+                commit_to(lead, bar(kSFull + tile));
             };
             auto issue_products = [&](int tile, int s, bool accumulate) {
                 const uint32_t b = stage_at(s) + M::kTile;
     #pragma unroll
-                for (int k = 0; k < kUnit / 16; ++k) mma_ts(products(tile), scores(tile) + 8 * k, operand(b + 2048 * k, 16384), kProductsDesc, accumulate || k > 0);
+                for (int k = 0; k < kUnit / 16; ++k) mma_ts(lead, products(tile), scores(tile) + 8 * k, operand(b + 2048 * k, 16384), kProductsDesc, accumulate || k > 0);
             };
             bool first = true;
             for (int i = 0; i < count; ++i) {
                 const int s = i & 1, tiles = walk.tile.rows > 128 ? 2 : 1;
                 const bool last = walk.unit + 1 == walk.units || i + 1 == count;
                 if (first) {
-                    wait_for(bar(kKvFull + s), (i >> 1) & 1, &dead, p.status);
+                    wait_all(bar(kKvFull + s), (i >> 1) & 1, &dead, p.status);
                     for (int t = 0; t < tiles; ++t) {
-                        wait_for(bar(kQFull + t), q_phase[t], &dead, p.status);
+                        wait_all(bar(kQFull + t), q_phase[t], &dead, p.status);
                         q_phase[t] ^= 1;
                         tmem_fence_after();
                         issue_scores(t, s);
                     }
                 }
                 for (int t = 0; t < tiles; ++t) {
-                    wait_for(bar(kPFull + t), p_phase[t], &dead, p.status);
+                    wait_all(bar(kPFull + t), p_phase[t], &dead, p.status);
                     p_phase[t] ^= 1;
                     tmem_fence_after();
                     issue_products(t, s, !first);
                     if (last) {
-                        commit_to(bar(kOFull + t));
+                        commit_to(lead, bar(kOFull + t));
                     } else {
-                        if (t == 0) wait_for(bar(kKvFull + (s ^ 1)), ((i + 1) >> 1) & 1, &dead, p.status);
+                        if (t == 0) wait_all(bar(kKvFull + (s ^ 1)), ((i + 1) >> 1) & 1, &dead, p.status);
                         issue_scores(t, s ^ 1);
                     }
                 }
-                commit_to(bar(kKvEmpty + s));
+                commit_to(lead, bar(kKvEmpty + s));
                 first = last;
                 walk.next(p, part);
             }
-            wait_for(bar(kKvEmpty + ((count - 1) & 1)), ((count - 1) >> 1) & 1, &dead, p.status);  // the last arrival has come
+            wait_all(bar(kKvEmpty + ((count - 1) & 1)), ((count - 1) >> 1) & 1, &dead, p.status);  // the last arrival has come
         }
         __syncwarp();
     }
