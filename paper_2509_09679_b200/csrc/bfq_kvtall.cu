@@ -144,25 +144,36 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;  // of a row
             const int first_row = 128 * tile + 32 * (warp & 3), part_of = lane % kLanes;
             const float sign = p.scale_log2 < 0.f ? -1.f : 1.f;
-#pragma unroll 4
-            for (int n = 0; n < 32; n += kRowsAtOnce) {
-                const int r = first_row + n + lane / kLanes, row = t.row0 + r;
-                const int token = t.token0 + row / p.group, head = walk.head * p.group + row % p.group;
-                const uint4 v = r < t.rows ? load_plain(reinterpret_cast<const uint4*>(p.q.data + (token * p.q.token + head * p.q.head + 8 * part_of) * 2)) : make_uint4(0, 0, 0, 0);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                float top = 0.f;
+            // eight loads on their way at a time
+            constexpr int kLoads = 8;
+#pragma unroll 1
+            for (int n0 = 0; n0 < 32; n0 += kLoads * kRowsAtOnce) {
+                uint4 v[kLoads];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+                for (int x = 0; x < kLoads; ++x) {
+                    const int r = first_row + n0 + x * kRowsAtOnce + lane / kLanes, row = t.row0 + r, token = row / p.group;
+                    v[x] = make_uint4(0, 0, 0, 0);
+                    if (r < t.rows)
+                        v[x] = load_plain(reinterpret_cast<const uint4*>(p.q.data + ((t.token0 + token) * p.q.token + (walk.head * p.group + row - token * p.group) * p.q.head + 8 * part_of) * 2));
+                }
 #pragma unroll
-                for (int x = 1; x < kLanes; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-                const RowPower power(top);
-                const float up = sign * power.up;
-                auto element = [&](int i) { return up * __uint_as_float(order<BITS>(i) & 1 ? w[order<BITS>(i) / 2] & 0xFFFF0000u : w[order<BITS>(i) / 2] << 16); };
-                const int at = 32 * (warp & 3) + n + lane / kLanes;  // of the tile
-                store16(base + M::kQ + tile * M::kTile + at * 128 + (part_of >> 3) * 16384 + (((part_of & 7) ^ (at & 7)) << 4), half_pair(element(0), element(1)),
-                        half_pair(element(2), element(3)), half_pair(element(4), element(5)), half_pair(element(6), element(7)));
-                const float down = __shfl_sync(0xFFFFFFFFu, power.down, (lane % kRowsAtOnce) * kLanes);
-                if (lane / kRowsAtOnce == n / kRowsAtOnce) row_scale = fabsf(p.scale_log2) * down;  // the lane's own row
+                for (int x = 0; x < kLoads; ++x) {
+                    const int n = n0 + x * kRowsAtOnce;
+                    const uint32_t w[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+#pragma unroll
+                    for (int y = 1; y < kLanes; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
+                    const RowPower power(top);
+                    const float up = sign * power.up;
+                    auto element = [&](int i) { return up * __uint_as_float(order<BITS>(i) & 1 ? w[order<BITS>(i) / 2] & 0xFFFF0000u : w[order<BITS>(i) / 2] << 16); };
+                    const int at = 32 * (warp & 3) + n + lane / kLanes;  // of the tile
+                    store16(base + M::kQ + tile * M::kTile + at * 128 + (part_of >> 3) * 16384 + (((part_of & 7) ^ (at & 7)) << 4), half_pair(element(0), element(1)),
+                            half_pair(element(2), element(3)), half_pair(element(4), element(5)), half_pair(element(6), element(7)));
+                    const float down = __shfl_sync(0xFFFFFFFFu, power.down, (lane % kRowsAtOnce) * kLanes);
+                    if (lane / kRowsAtOnce == n / kRowsAtOnce) row_scale = fabsf(p.scale_log2) * down;  // the lane's own row
+                }
             }
             const int r = 128 * tile + row_of_tile, row = t.row0 + r;
             const bool there = r < t.rows;
