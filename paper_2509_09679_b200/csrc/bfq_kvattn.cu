@@ -26,7 +26,7 @@ namespace kv {
 
 constexpr int kWarps = 4, kAttendThreads = 32 * kWarps;
 
-constexpr int kKeys = kUnit / kWarps;  // of a warp
+constexpr int kKeys = kFewUnit / kWarps;  // of a warp
 
 // Shared memory: for each warp kCount stages of its 32 keys' and values' codes, the same of their scales, a tile's merged products, sums, barriers.
 template <int D, int BITS, int NB>
@@ -112,13 +112,13 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     int64_t page = kNone;  // of the lane's box; kNone: it has no keys
     int sent = 0;          // units
     auto look = [&]() {
-        const int key = ahead.unit * kUnit + own;
+        const int key = ahead.unit * kFewUnit + own;
         page = sent < count && a_box && key < ahead.tile.keys ? load_plain(ahead.tile.pages + (key >> p.cache.page_shift)) : kNone;
     };
     auto fetch = [&](int slot) {
         if (sent >= count) return;
         ++sent;
-        const int row = (ahead.head << p.cache.page_shift) + ((ahead.unit * kUnit + own) & (page_keys - 1));
+        const int row = (ahead.head << p.cache.page_shift) + ((ahead.unit * kFewUnit + own) & (page_keys - 1));
         const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, page != kNone));
         if (lane == 0) mbar_expect_tx(full(slot), boxes * box * (2 * S::kRow + 4));
         __syncwarp();
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     int slot = 0;
     uint32_t phase = 0;
     for (int i = 0; i < count; ++i) {
-        const int key0 = now.unit * kUnit + kKeys * warp;
+        const int key0 = now.unit * kFewUnit + kKeys * warp;
         const uint32_t stage = stage_at(slot), scales = scales_at(slot);
         wait_for(full(slot), phase, &dead, p.status);
         if (key0 < now.tile.keys) {
@@ -570,7 +570,8 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : in->max_new;
     const int64_t rows = (in->q_starts == nullptr ? in->batch : in->tokens) * int64_t(p->group), rows_seq = int64_t(p->max_new) * p->group;
     p->prefix_tall = use_tall(rows), p->seq_tall = use_tall(rows_seq);
-    p->tall.rows = kTallRows;
+    p->tall.rows = kTallRows, p->tall.unit_shift = 6, p->few.unit_shift = 7;
+    static_assert(kTallUnit == 1 << 6 && kFewUnit == 1 << 7, "shifts");
     p->few.rows = (p->seq_tall || rows_seq <= 8) && (in->prefix_length == 0 || p->prefix_tall || rows <= 8) ? 8 : 16;
     const int tile_prefix = p->prefix_tall ? kTallRows : p->few.rows, tile_seq = p->seq_tall ? kTallRows : p->few.rows;
     const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;

@@ -14,11 +14,12 @@
 namespace bfq {
 namespace kv {
 
-constexpr int kUnit = 128;  // keys
+constexpr int kFewUnit = 128, kTallUnit = 64;  // keys
 constexpr int kTallRows = 256;
 
 struct Part {
     int rows;                     // of a tile
+    int unit_shift;               // keys of a unit: 1 << unit_shift
     int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
     int2* pairs;                  // [pairs] first CTA, CTAs
     float2* sums;                 // [entries][rows] m, l
@@ -97,7 +98,7 @@ struct Walk {
         const int last = p.entries(part);
         for (entry = e, units = 0; entry < last; ++entry) {
             tile = tile_of(p, part, entry);
-            units = (tile.keys + kUnit - 1) / kUnit;
+            units = (tile.keys + (1 << part.unit_shift) - 1) >> part.unit_shift;
             if (units > 0) break;
         }
     }
@@ -124,7 +125,7 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     constexpr int kWarps = THREADS / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, entries = p.entries(part), heads = p.cache.heads;
     const int each = (entries + THREADS - 1) / THREADS;
-    auto units_at = [&](int e) { return (tile_of(p, part, e).keys + kUnit - 1) / kUnit; };
+    auto units_at = [&](int e) { return (tile_of(p, part, e).keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
     long long mine = 0;
     for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_at(e);
     long long before = mine, total = 0;
@@ -224,14 +225,18 @@ struct RowPower {
 
 // Waits for a phase, with a limit.  Once one wait has given up all others of the CTA return at once (what they wait for may never come): the
 // kernel ends with meaningless outputs and the status word says so.
-constexpr int kWaitLimit = 1 << 22;
+constexpr long long kWaitCycles = 1ll << 31;  // about a second
 __device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
-    for (int i = 0; i < kWaitLimit; ++i) {
-        if (mbar_try_wait(bar, parity)) return;
+    if (mbar_try_wait(bar, parity)) return;
+    const long long since = clock64();
+    while (!mbar_try_wait(bar, parity)) {
         if (*dead) return;
+        if (clock64() - since > kWaitCycles) {
+            *dead = 1;
+            atomicExch(status, 3);
+            return;
+        }
     }
-    *dead = 1;
-    atomicExch(status, 3);
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 

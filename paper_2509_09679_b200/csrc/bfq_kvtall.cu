@@ -1,14 +1,15 @@
 // Attention of many query rows over the same keys of the paged low-bit cache (a shared prefix for a batch, chunks of a prompt) on the
 // fifth-generation tensor cores: the same formula and references as the kernel for few rows (bfq_kvattn.cu).
 //
-// A CTA has up to 256 rows, two M = 128 tiles, and takes its keys in units of 128:
-//   warps 0 .. 3, 4 .. 7  softmax of tile 0, 1: a thread owns a row (a lane of tensor memory).  Two walks over the row's 128 scores, the first
-//                         for the largest (a new reference and a pass over the products only where a score passes the old one by more than
-//                         8, as there), the second for exp2, sum and the rounding to fp16, which goes back to tensor memory over the scores;
-//   warps 8 .. 11         codes to fp16: a unit's keys and values into one of two stages, loaded one unit ahead into registers;
-//   warp 12, one thread   the MMAs: S = Q K^T (both operands in shared memory), O += P V (P from tensor memory).
-// The order of the MMAs, S0 S1 | O0 S0' O1 S1' | ..., lets the softmax of one tile run beside the products of the other; scores and
-// probabilities share their columns, so tensor memory holds 2 x 128 columns of scores and 2 x D of products.
+// A CTA has up to 256 rows, two M = 128 tiles, and takes its keys in units of 64:
+//   warps 0 .. 3, 4 .. 7  softmax of tile 0, 1: a thread owns a row (a lane of tensor memory) and has its 64 scores in registers: the largest
+//                         (a new reference and a pass over the products only where a score passes the old one by more than 8, as
+//                         there), exp2, sum and the rounding to fp16, which goes back to tensor memory over the scores;
+//   warps 8 .. 15         codes to fp16: a unit's keys and values into one of four stages, loaded two units ahead into registers;
+//   warp 16               the MMAs: S = Q K^T (both operands in shared memory), O += P V (P from tensor memory).
+// Two buffers of scores for each tile: S of the next unit is there while the products of this one run, so that a tile's softmax waits
+// for nothing but itself.  With one buffer of 128 keys a unit's chain, softmax 2500 cycles and then both products 1600, was the kernel's period.  Tensor
+// memory: 2 x 2 x 64 columns of scores (probabilities in the same place), 2 x D of products.
 // Keys and values are multiplied by their scales on the way into shared memory, over a power of two for all of a pair so far: one rounding to
 // fp16 of each element, 2^-12 on average and independent of its neighbours, a fraction of the output's own rounding.  Applied exactly, to
 // scores and probabilities, the scales would be read from shared memory 256 times by every softmax warp for a unit, which took three times as
@@ -23,18 +24,21 @@
 namespace bfq {
 namespace kv {
 
-constexpr int kTallThreads = 16 * 32;  // warps 13 .. 15 only lend their registers
-constexpr int kConvert = 128;  // threads that turn codes into operands
+constexpr int kTallThreads = 20 * 32;  // warps 17 .. 19 only lend their registers
+constexpr int kConvert = 256;          // threads that turn codes into operands
+constexpr int kStageCount = 4;
 
 template <int D>
 struct TallSmem {
-    static constexpr uint32_t kHalves = D / 64, kTile = kHalves * 128 * 128;  // 128 rows
-    static constexpr uint32_t kQ = 0, kStages = 2 * kTile, kStage = 2 * kTile;  // a stage: keys, values
-    static constexpr uint32_t kFactors = kStages + 2 * kStage;  // per stage: less, unit of the products, unit of the scores
-    static constexpr uint32_t kBars = kFactors + 2 * 16;
-    static constexpr uint32_t kBytes = kBars + 16 * 8 + 1024;  // and what rounding the base up to 1024 takes
+    static constexpr uint32_t kHalves = D / 64, kTile = kHalves * 128 * 128;     // 128 query rows
+    static constexpr uint32_t kKeysHalf = kTallUnit * 128, kKeys = kHalves * kKeysHalf;  // 64 elements of a unit's keys, all of them
+    static constexpr uint32_t kQ = 0, kStages = 2 * kTile, kStage = 2 * kKeys;   // a stage: keys, values
+    static constexpr uint32_t kFactors = kStages + kStageCount * kStage;          // per stage: less, unit of the products, unit of the scores
+    static constexpr uint32_t kBars = kFactors + kStageCount * 16;
+    static constexpr uint32_t kBytes = kBars + 24 * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
-enum Bar { kKvFull = 0, kKvEmpty = 2, kSFull = 4, kPFull = 6, kQFull = 8, kOFull = 10, kBarCount = 12 };
+// per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products up to date
+enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kBarCount = 20 };
 
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // the wait of a converged warp
@@ -109,32 +113,33 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     const Run run = find_run<kTallThreads>(p, part, scan, &walk);
     if (run.count == 0) return;
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 4; ++s) {
             mbar_init(bar(kKvFull + s), kConvert), mbar_init(bar(kKvEmpty + s), 1);
-            mbar_init(bar(kSFull + s), 1), mbar_init(bar(kPFull + s), 128), mbar_init(bar(kQFull + s), 128), mbar_init(bar(kOFull + s), 1);
+            mbar_init(bar(kSFull + s), 1), mbar_init(bar(kPFull + s), 128);
         }
+        for (int t = 0; t < 2; ++t) mbar_init(bar(kQFull + t), 128), mbar_init(bar(kDone + t), 1);
         mbar_init_fence();
         dead = 0;
     }
-    if (warp == 12) tmem_alloc512(smem_u32(&tmem_at));
+    if (warp == 16) tmem_alloc512(smem_u32(&tmem_at));
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = tmem_at;
-    auto scores = [&](int tile) { return tmem + 128u * tile; };
+    auto scores = [&](int tile, int buffer) { return tmem + 128u * tile + 64u * buffer; };
     auto products = [&](int tile) { return tmem + 256u + D * tile; };
     const int count = run.count;
 
-    // registers: 256 x 168 + 128 x 112 + 128 x 64 = 512 x 128, what the block was launched with
+    // registers: 256 x 136 + 256 x 80 + 128 x 48 = 640 x 96, what the block was launched with
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         // ---- softmax ---------------------------------------------------------------------------------------------------------
         const int tile = warp >> 2, row_of_tile = tid & 127;
         const uint32_t lanes = uint32_t(warp & 3) << 21;  // 32 lanes of tensor memory
-        const uint32_t s_at = scores(tile) + lanes, o_at = products(tile) + lanes;
+        const uint32_t o_at = products(tile) + lanes;
         float m = -INFINITY, l = 0.f, row_scale = 0.f, unit = 0.f;
         int limit = 0, least = 0;  // keys of the row; of the warp's rows, at least
-        uint32_t s_phase = 0, o_phase = 0;
+        uint32_t s_phase = 0, done_phase = 0;  // s_phase: a bit for each buffer; done_phase: of the last products that were asked for
         bool active = false;
         long long pair_from = run.from - walk.unit;
         auto open = [&]() {
@@ -144,8 +149,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;  // of a row
             const int first_row = 128 * tile + 32 * (warp & 3), part_of = lane % kLanes;
             const float sign = p.scale_log2 < 0.f ? -1.f : 1.f;
-            // eight loads on their way at a time
-            constexpr int kLoads = 8;
+            // four loads on their way at a time
+            constexpr int kLoads = 4;
 #pragma unroll 1
             for (int n0 = 0; n0 < 32; n0 += kLoads * kRowsAtOnce) {
                 uint4 v[kLoads];
@@ -187,8 +192,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         auto close = [&](long long done) {
             const int pair = walk.pair(p);
             if (active) {
-                wait_for(bar(kOFull + tile), o_phase, &dead, p.status);
-                o_phase ^= 1;
+                wait_for(bar(kDone + tile), done_phase ^ 1, &dead, p.status);
                 tmem_fence_after();
                 const int r = 128 * tile + row_of_tile;
                 const bool there = r < walk.tile.rows;
@@ -235,67 +239,60 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         open();
         for (int i = 0; i < count; ++i) {
             if (active) {
-                const int key0 = walk.unit * kUnit;
-                const bool edge = key0 + kUnit > least;  // some row of the warp ends in this unit, or has ended
-                wait_for(bar(kKvFull + (i & 1)), (i >> 1) & 1, &dead, p.status);  // for the factors
-                wait_for(bar(kSFull + tile), s_phase, &dead, p.status);
-                s_phase ^= 1;
+                const int key0 = walk.unit * kTallUnit, buffer = i & 1;
+                const bool edge = key0 + kTallUnit > least;  // some row of the warp ends in this unit, or has ended
+                const uint32_t s_at = scores(tile, buffer) + lanes;
+                wait_for(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status);  // for the factors
+                wait_for(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1, &dead, p.status);
+                s_phase ^= 1u << buffer;
                 tmem_fence_after();
-                const float4 factors = load_shared4(factors_at(i & 1));
+                uint32_t v[2][32];
+                tmem_ld32(s_at, v[0]);
+                tmem_ld32(s_at + 32, v[1]);
+                const float4 factors = load_shared4(factors_at(i & 3));
                 const float less = factors.x, scale = fmaxf(row_scale * factors.z, 1e-30f);  // -infinity times it is that
                 unit = factors.y;
-                float most = -INFINITY;
-                // compact loops: unrolled over the whole row, with the masks that few units need, the instruction cache missed all the time
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_ld32(s_at + 32 * c, v);
-                    tmem_wait_ld32(v);
-                    if (edge) {
-                        const int n = limit - key0 - 32 * c;
+                tmem_wait_ld32(v[0]);
+                tmem_wait_ld32(v[1]);
+                if (edge) {
+                    const int n = limit - key0;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0xFF800000u;
-                    }
-                    float x[4] = {most, most, most, most};
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j & 3] = fmaxf(x[j & 3], __uint_as_float(v[j]));
-                    most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                    for (int j = 0; j < 64; ++j) v[j >> 5][j & 31] = j < n ? v[j >> 5][j & 31] : 0xFF800000u;
                 }
+                float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int j = 0; j < 64; ++j) x[j & 3] = fmaxf(x[j & 3], __uint_as_float(v[j >> 5][j & 31]));
+                float most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
                 most = most == -INFINITY ? most : most * scale;
                 const bool over = most > m + 8.f;
                 if (first) {
                     m = most;
                 } else if (__any_sync(0xFFFFFFFFu, over) || less != 1.f) {
+                    wait_for(bar(kDone + tile), done_phase ^ 1, &dead, p.status);  // the products of the unit before
+                    tmem_fence_after();
                     float f = less;
                     if (over) f *= exp2_fast(m - most), l *= exp2_fast(m - most), m = most;
 #pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t w[16];
-                        tmem_ld16(o_at + 16 * c, w);
-                        tmem_wait_ld16(w);
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint32_t w[8];
+                        tmem_ld8(o_at + 8 * c, w);
+                        tmem_wait_ld8(w);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
-                        tmem_st16(o_at + 16 * c, w);
+                        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * f);
+                        tmem_st8(o_at + 8 * c, w);
                     }
                 }
                 first = false;
                 const float ref = m == -INFINITY ? 0.f : m;
                 const u64 scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
                 u64 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32], out[16];
-                    tmem_ld32(s_at + 32 * c, v);
-                    tmem_wait_ld32(v);
-                    if (edge) {
-                        const int n = limit - key0 - 32 * c;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0xFF800000u;
-                    }
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t out[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         float a, b;
-                        unpack2(fma2(pack2u(v[2 * j], v[2 * j + 1]), scale2, ref2), a, b);
+                        unpack2(fma2(pack2u(v[c][2 * j], v[c][2 * j + 1]), scale2, ref2), a, b);
                         a = exp2_fast(a), b = exp2_fast(b);
                         sum2[j & 1] = add2(sum2[j & 1], pack2(a, b));
                         out[j] = half_pair(a, b);
@@ -307,7 +304,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 l += a + b;
                 tmem_wait_st();
                 tmem_fence_before();
-                arrive(bar(kPFull + tile));
+                done_phase ^= 1;
+                arrive(bar(kPFull + 2 * tile + buffer));
             }
             if (walk.unit + 1 == walk.units || i + 1 == count) {
                 close(run.from + i + 1);
@@ -318,42 +316,53 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 ++walk.unit;
             }
         }
-    } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+    } else if (warp < 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // ---- codes to operands -------------------------------------------------------------------------------------------------
         const int w = warp - 8;
         const Unpack<BITS> unpack;
         // 16-byte pieces: the eight lanes of a phase of the stores below write chunks of one half to eight different places of 16 bytes
         constexpr int kPer = BITS == 4 ? 2 : 4;        // pieces of 64 elements
         constexpr int kKeys = 32 / (kPer * (D / 64));  // keys of a warp's 32 pieces: of one page
-        constexpr int kTurns = kUnit / kKeys / 4;
+        constexpr int kTurns = kTallUnit / kKeys / 8 > 0 ? kTallUnit / kKeys / 8 : 1;  // D = 64 at 4 bits: half of the warps have all
         const int part_of = lane % kPer, key_low = lane / kPer % (8 / kPer);
         const int half = D == 128 ? lane >> 3 & 1 : 0, key_of = key_low + (8 / kPer) * (D == 128 ? lane >> 4 : lane >> 3);
-        uint4 k_raw[kTurns], v_raw[kTurns];
-        uint16_t k_scale[kTurns], v_scale[kTurns];
+        const bool busy = w * kKeys < kTallUnit;
+        struct Raw {
+            uint4 k[kTurns], v[kTurns];
+            uint16_t k_scale[kTurns], v_scale[kTurns];
+            bool first;  // unit of its pair
+        };
         constexpr int64_t kNone = -(int64_t(1) << 32);
         int64_t page = kNone;  // lane c: of turn c; kNone: it has no keys
-        auto look = [&]() {
-            const int key = walk.unit * kUnit + (lane * 4 + w) * kKeys;
-            page = lane < kTurns && key < walk.tile.keys ? load_plain(walk.tile.pages + (key >> p.cache.page_shift)) : kNone;
+        int sent = 0;          // units loaded
+        bool opens = true;     // the unit ahead is its pair's first here
+        auto look = [&]() {    // pages of the unit ahead, a load earlier than they are needed
+            const int key = walk.unit * kTallUnit + (lane * 8 + w) * kKeys;
+            page = sent < count && busy && lane < kTurns && key < walk.tile.keys ? load_plain(walk.tile.pages + (key >> p.cache.page_shift)) : kNone;
         };
-        auto load = [&]() {
+        auto load = [&](Raw& raw) {
+            if (sent >= count) return;
             const int mask = (1 << p.cache.page_shift) - 1;
             if (page != kNone && (page < 0 || page >= p.cache.pages)) atomicExch(p.status, kBadIndex), page = kNone;
 #pragma unroll
             for (int c = 0; c < kTurns; ++c) {
-                const int key = walk.unit * kUnit + (c * 4 + w) * kKeys + key_of;
+                const int key = walk.unit * kTallUnit + (c * 8 + w) * kKeys + key_of;
                 const int64_t at = __shfl_sync(0xFFFFFFFFu, page, c);
-                k_raw[c] = v_raw[c] = make_uint4(0, 0, 0, 0), k_scale[c] = v_scale[c] = 0;
+                raw.k[c] = raw.v[c] = make_uint4(0, 0, 0, 0), raw.k_scale[c] = raw.v_scale[c] = 0;
                 if (at >= 0 && key < walk.tile.keys) {
-                    const int64_t row = (static_cast<int64_t>(walk.head) << p.cache.page_shift) + (key & mask);
-                    const int off = 16 * (half * kPer + part_of);
-                    k_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.k.codes + at * p.cache.k.codes_page + row * kRow + off));
-                    v_raw[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.v.codes + at * p.cache.v.codes_page + row * kRow + off));
-                    k_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.k.scales + at * p.cache.k.scales_page + row);
-                    v_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.v.scales + at * p.cache.v.scales_page + row);
+                    const int row = (walk.head << p.cache.page_shift) + (key & mask), off = row * kRow + 16 * (half * kPer + part_of);
+                    raw.k[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.k.codes + at * p.cache.k.codes_page + off));
+                    raw.v[c] = load_plain(reinterpret_cast<const uint4*>(p.cache.v.codes + at * p.cache.v.codes_page + off));
+                    raw.k_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.k.scales + at * p.cache.k.scales_page + row);
+                    raw.v_scale[c] = *static_cast<volatile const uint16_t*>(p.cache.v.scales + at * p.cache.v.scales_page + row);
                 }
             }
+            raw.first = opens;
+            opens = walk.unit + 1 == walk.units;
+            ++sent;
+            walk.next(p, part);
+            look();
         };
         auto times = [](uint32_t a, uint32_t b) {
             uint32_t d;
@@ -361,7 +370,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             return d;
         };
         auto store = [&](uint32_t to, const uint4& raw, int key, float scale) {
-            const uint32_t row = to + half * 16384 + key * 128, s2 = half_pair(scale, scale);
+            const uint32_t row = to + half * M::kKeysHalf + key * 128, s2 = half_pair(scale, scale);
             const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
             if constexpr (BITS == 4) {
 #pragma unroll
@@ -378,99 +387,105 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         // the power of two above all scales of the pair so far, at most that of 65504
         auto above = [](float top, float most) { return most > top ? __uint_as_float((__float_as_uint(most) & 0x7F800000u) + 0x00800000u) : top; };
         float k_top = 0.f, v_top = 0.f;
-        bool first = true;
-        look();
-        load();
-        for (int i = 0; i < count; ++i) {
-            const int s = i & 1;
+        auto step = [&](int i, Raw& raw) {
+            const int s = i & 3;
             float2 most = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int c = 0; c < kTurns; ++c)
-                most.x = fmaxf(most.x, half_value(k_scale[c])), most.y = fmaxf(most.y, half_value(v_scale[c]));
+            for (int c = 0; c < kTurns; ++c) most.x = fmaxf(most.x, half_value(raw.k_scale[c])), most.y = fmaxf(most.y, half_value(raw.v_scale[c]));
             most.x = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.x)));  // not negative: ordered as integers
             most.y = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.y)));
-            if (lane == 0) warp_top[s][w] = most;
+            if (lane == 0) warp_top[i & 1][w] = most;
             bar_sync(1, kConvert);
 #pragma unroll
-            for (int n = 0; n < kConvert / 32; ++n) most.x = fmaxf(most.x, warp_top[s][n].x), most.y = fmaxf(most.y, warp_top[s][n].y);
-            if (first) k_top = v_top = 0x1p-24f;
+            for (int n = 0; n < kConvert / 32; ++n) most.x = fmaxf(most.x, warp_top[i & 1][n].x), most.y = fmaxf(most.y, warp_top[i & 1][n].y);
+            if (raw.first) k_top = v_top = 0x1p-24f;
             const float v_before = v_top;
             k_top = above(k_top, most.x), v_top = above(v_top, most.y);
             const float k_factor = 128.f / k_top, v_factor = 128.f / v_top;  // codes times scales: at most 2^14
-            first = walk.unit + 1 == walk.units;
-            walk.next(p, part);
-            if (i + 1 < count) look();
-            if (i >= 2) wait_for(bar(kKvEmpty + s), ((i >> 1) - 1) & 1, &dead, p.status);
+            if (i >= kStageCount) wait_for(bar(kKvEmpty + s), ((i >> 2) - 1) & 1, &dead, p.status);
+            if (busy) {
 #pragma unroll
-            for (int c = 0; c < kTurns; ++c) {
-                const int key = (c * 4 + w) * kKeys + key_of;
-                store(stage_at(s), k_raw[c], key, k_factor * half_value(k_scale[c]));
-                store(stage_at(s) + M::kTile, v_raw[c], key, v_factor * half_value(v_scale[c]));
+                for (int c = 0; c < kTurns; ++c) {
+                    const int key = (c * 8 + w) * kKeys + key_of;
+                    store(stage_at(s), raw.k[c], key, k_factor * half_value(raw.k_scale[c]));
+                    store(stage_at(s) + M::kKeys, raw.v[c], key, v_factor * half_value(raw.v_scale[c]));
+                }
             }
             if (warp == 8 && lane == 0)
                 asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors_at(s)), "f"(v_before / v_top), "f"(v_top * (1.f / 128.f)), "f"(k_top * (1.f / 128.f)), "f"(0.f)
                              : "memory");
             fence_operands();
             arrive(bar(kKvFull + s));
-            if (i + 1 < count) load();
+            load(raw);
+        };
+        Raw even, odd;
+        look();
+        load(even);
+        load(odd);
+        for (int i = 0; i < count; i += 2) {
+            step(i, even);
+            if (i + 1 < count) step(i + 1, odd);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         // ---- MMAs ----------------------------------------------------------------------------------------------------------------
-        if (warp == 12) {
+        if (warp == 16) {
             const uint32_t lead = elect_one();
-            uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
-            constexpr uint32_t kScoresDesc = instruction(128, 0), kProductsDesc = instruction(D, 1);
-            auto issue_scores = [&](int tile, int s) {
-                const uint32_t a = base + M::kQ + tile * M::kTile, b = stage_at(s);
-    #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                    mma_ss(lead, scores(tile), operand(a + off, 0), operand(b + off, 0), kScoresDesc, k > 0);
-                }
-                commit_to(lead, bar(kSFull + tile));
+            uint32_t p_phase = 0, q_phase[2] = {0, 0};  // p_phase: a bit for each tile and buffer
+            constexpr uint32_t kScoresDesc = instruction(kTallUnit, 0), kProductsDesc = instruction(D, 1);
+            auto issue_scores = [&](int tile, int i) {
+                const uint32_t a = base + M::kQ + tile * M::kTile, b = stage_at(i & 3);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_ss(lead, scores(tile, i & 1), operand(a + (k >> 2) * 16384 + (k & 3) * 32, 0), operand(b + (k >> 2) * M::kKeysHalf + (k & 3) * 32, 0), kScoresDesc, k > 0);
+                commit_to(lead, bar(kSFull + 2 * tile + (i & 1)));
             };
-            auto issue_products = [&](int tile, int s, bool accumulate) {
-                const uint32_t b = stage_at(s) + M::kTile;
-    #pragma unroll
-                for (int k = 0; k < kUnit / 16; ++k) mma_ts(lead, products(tile), scores(tile) + 8 * k, operand(b + 2048 * k, 16384), kProductsDesc, accumulate || k > 0);
+            auto issue_products = [&](int tile, int i, bool accumulate) {
+                const uint32_t b = stage_at(i & 3) + M::kKeys;
+#pragma unroll
+                for (int k = 0; k < kTallUnit / 16; ++k)
+                    mma_ts(lead, products(tile), scores(tile, i & 1) + 8 * k, operand(b + 2048 * k, M::kKeysHalf), kProductsDesc, accumulate || k > 0);
+                commit_to(lead, bar(kDone + tile));
             };
-            bool first = true;
-            for (int i = 0; i < count; ++i) {
-                const int s = i & 1, tiles = walk.tile.rows > 128 ? 2 : 1;
-                const bool last = walk.unit + 1 == walk.units || i + 1 == count;
-                if (first) {
-                    wait_all(bar(kKvFull + s), (i >> 1) & 1, &dead, p.status);
-                    for (int t = 0; t < tiles; ++t) {
-                        wait_all(bar(kQFull + t), q_phase[t], &dead, p.status);
-                        q_phase[t] ^= 1;
-                        tmem_fence_after();
-                        issue_scores(t, s);
-                    }
-                }
+            auto operands_there = [&](int i) { wait_all(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status); };
+            for (int i0 = 0; i0 < count;) {  // a pair's units here: i0 .. i1 - 1
+                const int left = walk.units - walk.unit, i1 = i0 + left < count ? i0 + left : count, tiles = walk.tile.rows > 128 ? 2 : 1;
+                operands_there(i0);
                 for (int t = 0; t < tiles; ++t) {
-                    wait_all(bar(kPFull + t), p_phase[t], &dead, p.status);
-                    p_phase[t] ^= 1;
+                    wait_all(bar(kQFull + t), q_phase[t], &dead, p.status);
+                    q_phase[t] ^= 1;
                     tmem_fence_after();
-                    issue_products(t, s, !first);
-                    if (last) {
-                        commit_to(lead, bar(kOFull + t));
-                    } else {
-                        if (t == 0) wait_all(bar(kKvFull + (s ^ 1)), ((i + 1) >> 1) & 1, &dead, p.status);
-                        issue_scores(t, s ^ 1);
-                    }
+                    issue_scores(t, i0);
                 }
-                commit_to(lead, bar(kKvEmpty + s));
-                first = last;
-                walk.next(p, part);
+                if (i0 + 1 < i1) {
+                    operands_there(i0 + 1);
+                    for (int t = 0; t < tiles; ++t) issue_scores(t, i0 + 1);
+                }
+                for (int i = i0; i < i1; ++i) {
+                    for (int t = 0; t < tiles; ++t) {
+                        const int which = 2 * t + (i & 1);
+                        wait_all(bar(kPFull + which), p_phase >> which & 1, &dead, p.status);
+                        p_phase ^= 1u << which;
+                        tmem_fence_after();
+                        issue_products(t, i, i > i0);
+                        if (i + 2 < i1) {
+                            if (t == 0) operands_there(i + 2);
+                            issue_scores(t, i + 2);
+                        }
+                    }
+                    commit_to(lead, bar(kKvEmpty + (i & 3)));
+                }
+                i0 = i1;
+                walk.next_pair(p, part);
             }
-            wait_all(bar(kKvEmpty + ((count - 1) & 1)), ((count - 1) >> 1) & 1, &dead, p.status);  // the last arrival has come
+            for (int i = count > kStageCount ? count - kStageCount : 0; i < count; ++i)  // the last arrivals have come
+                wait_all(bar(kKvEmpty + (i & 3)), (i >> 2) & 1, &dead, p.status);
         }
         __syncwarp();
     }
     tmem_fence_before();
     __syncthreads();
-    if (warp == 12) tmem_dealloc512(tmem);
+    if (warp == 16) tmem_dealloc512(tmem);
 }
 
 template <int D, int BITS>
