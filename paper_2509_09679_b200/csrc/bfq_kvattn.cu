@@ -622,7 +622,9 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
         if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, st);
-        if (e == cudaSuccess) {
+        if (e == cudaSuccess && p.seq_tall && p.prefix_length == 0) {
+            e = kv::join_tall_launch(plan, p, st);
+        } else if (e == cudaSuccess) {
             // a warp for each row where that is fewer than the chip runs at once; more would only load the butterfly's constants again
             const int64_t rows = p.tokens * p.q.heads, warps = int64_t(plan->sm_count) * 16, each = (rows + warps - 1) / warps;
             const dim3 grid(unsigned((rows + 4 * each - 1) / (4 * each)));

@@ -243,6 +243,8 @@ __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.ar
 // the tall kernel (bfq_kvtall.cu): CTAs of a launch, and the launch
 cudaError_t tall_ctas(const bfq_plan* plan, int bits, int* ctas);
 cudaError_t tall_launch(const bfq_plan* plan, const AttendParams& p, int ctas, cudaStream_t st);
+// joins its results where there is no prefix (bfq_kvjoin.cu)
+cudaError_t join_tall_launch(const bfq_plan* plan, const AttendParams& p, cudaStream_t st);
 
 }  // namespace kv
 }  // namespace bfq

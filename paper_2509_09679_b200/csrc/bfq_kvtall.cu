@@ -242,8 +242,10 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 const int key0 = walk.unit * kTallUnit, buffer = i & 1;
                 const bool edge = key0 + kTallUnit > least;  // some row of the warp ends in this unit, or has ended
                 const uint32_t s_at = scores(tile, buffer) + lanes;
-                wait_for(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status);  // for the factors
-                wait_for(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1, &dead, p.status);
+                // the factors and the scores, usually both there: one latency
+                const bool kv_there = mbar_try_wait(bar(kKvFull + (i & 3)), (i >> 2) & 1), s_there = mbar_try_wait(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1);
+                if (!kv_there) wait_for(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status);
+                if (!s_there) wait_for(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1, &dead, p.status);
                 s_phase ^= 1u << buffer;
                 tmem_fence_after();
                 uint32_t v[2][32];
@@ -261,7 +263,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 }
                 float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int j = 0; j < 64; ++j) x[j & 3] = fmaxf(x[j & 3], __uint_as_float(v[j >> 5][j & 31]));
+                for (int j = 0; j < 64; j += 2)
+                    x[j >> 1 & 3] = fmaxf(fmaxf(x[j >> 1 & 3], __uint_as_float(v[j >> 5][j & 31])), __uint_as_float(v[j >> 5][(j & 31) + 1]));
                 float most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
                 most = most == -INFINITY ? most : most * scale;
                 const bool over = most > m + 8.f;
