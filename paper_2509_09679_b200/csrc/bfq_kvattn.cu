@@ -91,11 +91,17 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     auto full = [&](int s) { return base + S::kBars + 8u * (warp * S::kCount + s); };
     auto stage_at = [&](int s) { return base + (warp * S::kCount + s) * S::kBytes; };
     auto scales_at = [&](int s) { return base + S::kScales + (warp * S::kCount + s) * S::kScaleBytes; };
-    grid_dep_wait();
+    // Beside the tall kernel, which has waited for all that came before and shares nothing with this one: it is waited for at the end, so that
+    // this kernel's end is the end of both.
+    if (!p.beside_tall) grid_dep_wait();
+    grid_dep_launch();
     const Part& part = p.few;
     Walk ahead;
     const Run run = find_run<kAttendThreads>(p, part, scan, &ahead);
-    if (run.count == 0) return;
+    if (run.count == 0) {
+        if (p.beside_tall) grid_dep_wait();
+        return;
+    }
     Walk now = ahead;
     const int count = run.count;
     if (tid == 0) {
@@ -390,6 +396,7 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
             ++now.unit;
         }
     }
+    if (p.beside_tall) grid_dep_wait();
 }
 
 // Joins a row's partial results (the shared prefix's, then its sequence's), turns it back by Q^T and rounds it once.  A row is a (token, query
@@ -575,7 +582,7 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     p->few.rows = (p->seq_tall || rows_seq <= 8) && (in->prefix_length == 0 || p->prefix_tall || rows <= 8) ? 8 : 16;
     const int tile_prefix = p->prefix_tall ? kTallRows : p->few.rows, tile_seq = p->seq_tall ? kTallRows : p->few.rows;
     const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;
-    if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 30) return BFQ_ERR_TOO_LARGE;
+    if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 27) return BFQ_ERR_TOO_LARGE;
     (p->prefix_tall ? p->tall : p->few).tiles_prefix = int(tiles_prefix), (p->seq_tall ? p->tall : p->few).tiles_seq = int(tiles_seq);
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;
@@ -620,6 +627,7 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return BFQ_ERR_ALIGN;
         kv::lay_out(&p, plan->n, few, tall, static_cast<uint8_t*>(workspace));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
+        p.beside_tall = tall > 0;
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
         if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, st);
         if (e == cudaSuccess && p.seq_tall && p.prefix_length == 0) {

@@ -43,6 +43,7 @@ struct AttendParams {
     const float2* tw;
     Part few, tall;
     int prefix_tall, seq_tall;  // which of them has the prefix, the sequences
+    int beside_tall;            // the kernel for few rows follows the one for many
     int* status;
     __host__ __device__ int entries(const Part& part) const { return part.tiles_prefix + batch * part.tiles_seq; }
 };

@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     auto stage_at = [&](int s) { return base + M::kStages + s * M::kStage; };
     auto factors_at = [&](int s) { return base + M::kFactors + 16u * s; };
     grid_dep_wait();
+    grid_dep_launch();
     const Part& part = p.tall;
     Walk walk;
     const Run run = find_run<kTallThreads>(p, part, scan, &walk);
