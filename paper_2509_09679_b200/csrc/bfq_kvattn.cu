@@ -433,13 +433,27 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
         auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
             const Part& part = tall ? p.tall : p.few;
             const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
-            if (tile_of(p, part, entry).keys == 0) return;
             const int pair = entry * p.cache.heads + h;
-            const int2 ctas = load_plain(part.pairs + pair);
-            const int64_t first = static_cast<int64_t>(ctas.x) + pair;
-            for (int i0 = 0; i0 < ctas.y; i0 += 32) {  // a lane has one of 32 results' m and l
-                const int n = ctas.y - i0 < 32 ? ctas.y - i0 : 32;
+            const int2 found = load_plain(part.pairs + pair);  // beside the lengths; means something where there are keys
+            if (tile_of(p, part, entry).keys == 0) return;
+            const int64_t first = static_cast<int64_t>(found.x) + pair;
+            constexpr int kAtOnce = 4;  // results on their way
+            float v[kAtOnce][kE];
+            auto load = [&](int i, float (&to)[kE]) {
+                const float* at = part.parts + ((first + i) * rows + r) * D + kE * lane;
+                if constexpr (kE == 4) {
+                    const float4 u = load_plain(reinterpret_cast<const float4*>(at));
+                    to[0] = u.x, to[1] = u.y, to[2] = u.z, to[3] = u.w;
+                } else {
+                    const float2 u = load_plain(reinterpret_cast<const float2*>(at));
+                    to[0] = u.x, to[1] = u.y;
+                }
+            };
+            for (int i0 = 0; i0 < found.y; i0 += 32) {  // a lane has one of 32 results' m and l
+                const int n = found.y - i0 < 32 ? found.y - i0 : 32;
                 const float2 ml = lane < n ? load_plain(part.sums + (first + i0 + lane) * rows + r) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) load(i0 + (k < n ? k : 0), v[k]);
                 float top = ml.x;
 #pragma unroll
                 for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
@@ -451,16 +465,13 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
                 m = top, l = l * old + sum;
 #pragma unroll
                 for (int e = 0; e < kE; ++e) o[e] *= old;
-#pragma unroll 8
-                for (int i = 0; i < n; ++i) {
-                    const float f = __shfl_sync(0xFFFFFFFFu, mine, i);
-                    const float* at = part.parts + ((first + i0 + i) * rows + r) * D + kE * lane;
-                    if constexpr (kE == 4) {
-                        const float4 u = load_plain(reinterpret_cast<const float4*>(at));
-                        o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]), o[2] = fmaf(f, u.z, o[2]), o[3] = fmaf(f, u.w, o[3]);
-                    } else {
-                        const float2 u = load_plain(reinterpret_cast<const float2*>(at));
-                        o[0] = fmaf(f, u.x, o[0]), o[1] = fmaf(f, u.y, o[1]);
+                for (int i = 0; i < n; i += kAtOnce) {
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) {
+                        const float f = __shfl_sync(0xFFFFFFFFu, mine, (i + k) & 31);
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) o[e] = i + k < n ? fmaf(f, v[k][e], o[e]) : o[e];
+                        if (i + kAtOnce + k < n) load(i0 + i + kAtOnce + k, v[k]);
                     }
                 }
             }
