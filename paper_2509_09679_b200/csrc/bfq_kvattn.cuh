@@ -10,6 +10,7 @@
 // tiles to one of them and the sequences' to the same one or the other; each has its own Part of the work.
 #pragma once
 #include "bfq_kv.cuh"
+#include "bfq_kvmma.cuh"
 
 namespace bfq {
 namespace kv {
@@ -163,83 +164,6 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     walk->head = static_cast<int>(scan[kWarps + 1] / walk->units), walk->unit = static_cast<int>(scan[kWarps + 1] % walk->units);
     return run;
 }
-
-__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// Codes of a word as exact fp16 pairs (one of the lower half, one of the upper): the code's bits, its top one inverted, lie in the mantissa of
-// 1024 .. 2047.  4 bits: codes i and i + 4, i < 4; the odd ones lie four places up there, 1152 + 16 code.  8 bits: codes i and i + 2, i < 2.
-// Masks and bases are kept in registers that the compiler cannot see through: as constants, two of them in one operation, it makes two
-// operations of each (of the kernel for few rows' 850 instructions for 32 keys of 4 bits 130).
-template <int BITS>
-struct Unpack {
-    uint32_t mask, base, mask_up, base_up;
-    __device__ __forceinline__ Unpack() {
-        asm volatile("mov.u32 %0, %1;" : "=r"(mask) : "n"(BITS == 4 ? 0x000F000F : 0x00FF00FF));
-        asm volatile("mov.u32 %0, %1;" : "=r"(base) : "n"(BITS == 4 ? 0x64086408 : 0x64806480));  // 1032, 1152
-        if constexpr (BITS == 4) {
-            asm volatile("mov.u32 %0, %1;" : "=r"(mask_up) : "n"(0x00F000F0));
-            asm volatile("mov.u32 %0, %1;" : "=r"(base_up) : "n"(0x64806480));  // 1152
-        }
-    }
-    __device__ __forceinline__ static uint32_t and_xor(uint32_t a, uint32_t b, uint32_t c) {
-        uint32_t d;
-        asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-        return d;
-    }
-    __device__ __forceinline__ uint32_t operator()(uint32_t w, int i) const {
-        if constexpr (BITS == 4) {
-            if (i >= 2) w >>= 8;
-            return i & 1 ? fma_pair(and_xor(w, mask_up, base_up), 0x2C002C00u, 0xD480D480u)  // / 16 - 72
-                         : sub_pair(and_xor(w, mask, base), base);
-        } else {
-            if (i) w >>= 8;
-            return sub_pair(and_xor(w, mask, base), base);
-        }
-    }
-};
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// The power of two that puts a row's largest element `top` in [2^10, 2^11): elements down to 2^-24 of it stay exact in fp16.
-struct RowPower {
-    float up, down;  // 2^e and 2^-e
-    __device__ __forceinline__ explicit RowPower(float top) {
-        const int field = 264 - static_cast<int>(__float_as_uint(top) >> 23), e = field > 253 ? 253 : field;
-        up = __uint_as_float(uint32_t(e) << 23), down = __uint_as_float(uint32_t(254 - e) << 23);
-    }
-};
-
-// Waits for a phase, with a limit.  Once one wait has given up all others of the CTA return at once (what they wait for may never come): the
-// kernel ends with meaningless outputs and the status word says so.
-constexpr long long kWaitCycles = 1ll << 31;  // about a second
-__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
-    if (mbar_try_wait(bar, parity)) return;
-    const long long since = clock64();
-    while (!mbar_try_wait(bar, parity)) {
-        if (*dead) return;
-        if (clock64() - since > kWaitCycles) {
-            *dead = 1;
-            atomicExch(status, 3);
-            return;
-        }
-    }
-}
-__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 // the tall kernel (bfq_kvtall.cu): CTAs of a launch, and the launch
 cudaError_t tall_ctas(const bfq_plan* plan, int bits, int* ctas);

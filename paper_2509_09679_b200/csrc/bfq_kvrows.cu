@@ -6,18 +6,18 @@
 //     keys, values s = fp16(max |y| / qmax), codes = clip(round(y / s)) in the page and place of the token's slot.
 // Values are rotated by Q alone.  bfq_kv_read: x = Q^T (s code), the rows at any slots in the model's basis.
 //
-// A thread owns a row of D = 64 or 128 elements, all of it in registers, so that norms, maxima and the stages of the butterfly need no
-// exchange between lanes; a warp takes 32 consecutive rows (a token's heads share its angles), copied into shared memory 16 bytes a lane, the next
-// 32 while these are worked on, and results go out the same way.  The butterfly's constants are the same for all lanes: they come from
-// shared memory by broadcast.  Its stages run in the scaled form, two FMAs a pair: with z = P w, P the product of the cosines
-// that an element has been through,
-//     lo: w <- w_lo - tan(t) (P_hi / P_lo) w_hi,   hi: w <- w_hi + tan(t) (P_lo / P_hi) w_lo,   P <- P cos(t)
-// and P multiplied in at the end.  Where some |P| is below 2^-40 (an angle close to an odd multiple of pi/2), and for 32 rows of which
-// one is not finite in that form, the plain stages are taken, four operations a pair.  All sums in fp32.
-//
-// What bounds it: fp32 operations, about 14 an element at 128 a cycle and SM, which is what the memory's rate leaves room for, too.  With a row
-// on 16 lanes (exchanges by shuffles, constants in registers, 12 warps on an SM) 16384 tokens of 32 + 2 x 8 heads took 420 us.
+// The kernels below are for many rows (bfq_kvrows_few.cu has those for few): the butterfly as one dense product on the tensor cores, 128
+// rows to a tcgen05.mma.  A thread owns a row of D = 64 or 128 elements, all of it in registers, so that norms and maxima need no exchange; a
+// warp's 32 consecutive rows (a token's heads share its angles) come through shared memory 16 bytes a lane, the next ones while these are worked
+// on.  A row z, times the power of two that puts its largest element in [2^10, 2^11), is split into two fp16 terms, h + l, 22 bits; so is Q, times
+// 2^10, built from the stages' cosines and sines in fp32 by each CTA.  y = h Qh + h Ql + l Qh in fp32: off by at most 2^-20 of |z| (both
+// splits 2^-22 of their elements, l Ql 2^-22, the rest for the sums).  Rows read back are exact in one term: the codes, times their scale
+// afterwards.  The terms go straight into tensor memory as the product's left operand; two groups of four warps take tiles in turn, one
+// working while the other's product runs.
+// What it replaced took, for 16384 tokens of 32 + 2 x 8 heads: a row on 16 lanes, stages by shuffles, 420 us; a row to a thread, stages in
+// registers with their constants broadcast from shared memory, 235 us.
 #include "bfq_generic.cuh"
+#include "bfq_kvmma.cuh"
 #include "bfq_kvrows.cuh"
 #include "bfq_kvturn.cuh"
 #include "bfq_n4096.cuh"
@@ -25,18 +25,22 @@
 namespace bfq {
 namespace kv {
 
-constexpr int kMostWarps = 4;  // of a CTA
+constexpr int kGroups = 2, kRowsThreads = 128 * kGroups;  // groups of four warps
 
-// Which rows a warp has: chunks of 32 rows, a CTA's consecutive, its warps' in turn.
-struct Chunks {
-    int at, end, step;
-    __device__ __forceinline__ explicit Chunks(int rows) {
-        const int chunks = (rows + 31) / 32, per = (chunks + gridDim.x - 1) / gridDim.x, from = per * blockIdx.x;
-        step = blockDim.x >> 5;
-        end = from + per < chunks ? from + per : chunks;
-        at = from + (threadIdx.x >> 5);
+// Which tiles of 128 rows a group has: a CTA's consecutive, its groups' in turn.
+struct Tiles {
+    int at, end;
+    __device__ __forceinline__ explicit Tiles(int rows) {
+        const int tiles = (rows + 127) / 128, per = (tiles + gridDim.x - 1) / gridDim.x, from = per * blockIdx.x;
+        end = from + per < tiles ? from + per : tiles;
+        at = from + (threadIdx.x >> 7);
     }
     __device__ __forceinline__ bool there() const { return at < end; }
+    // the thread's row of a tile; -1: of none
+    __device__ __forceinline__ int row(int tile, int rows) const {
+        const int r = tile * 128 + (threadIdx.x & 127);
+        return tile < end && r < rows ? r : -1;
+    }
 };
 
 // 16 bytes of a row as numbers, in pairs
@@ -60,17 +64,6 @@ __device__ __forceinline__ float largest(const u64 (&x)[D / 2]) {  // NaN elemen
         top[r & 3] = fmaxf(top[r & 3], fmaxf(fabsf(a), fabsf(b)));
     }
     return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-}
-// whether an infinity or a NaN is among them: a sum of zeros otherwise
-template <int D>
-__device__ __forceinline__ bool all_finite(const u64 (&x)[D / 2]) {
-    u64 sum = pack2(0.f, 0.f);
-    const u64 zero = pack2(0.f, 0.f);
-#pragma unroll
-    for (int r = 0; r < D / 2; ++r) sum = fma2(x[r], zero, sum);
-    float a, b;
-    unpack2(sum, a, b);
-    return a + b == 0.f;
 }
 // pairs (i, i + R / 2), R known to the compiler so that the row stays in registers
 template <int D, int R>
@@ -106,69 +99,198 @@ __device__ __forceinline__ void turn_neighbours(int dims, u64 (&x)[D / 2], const
         }
 }
 
-template <int D, bool F32, int BITS>
-struct AppendSmem {
-    static constexpr int kIn = D * (F32 ? 4 : 2), kInPitch = kIn + 16, kOutPitch = 2 * D + 16, kCodes = D * BITS / 8;
-    static constexpr uint32_t kTable = RowTurn<D, false>::kBytes, kNorms = kTable, kProducts = kNorms + 3 * D * 4;  // weights of queries, keys, ones
-    static constexpr uint32_t kWarps = kProducts + D * 4, kWarp = 32 * (kInPitch + kOutPitch);
-    static constexpr uint32_t bytes(int warps) { return kWarps + warps * kWarp; }
+// Place in its eight of element i, for left operands whose elements stand in the order that codes come out in.
+template <int BITS>
+__host__ __device__ constexpr int place_of(int i) {
+    return BITS == 4 ? (i < 4 ? 2 * i : 2 * i - 7) : (i & 4) + ((i >> 1) & 1) + 2 * (i & 1);
+}
+
+// Q (or, for rows read back, Q^T) as right operand, K-major, times 2^10 in two fp16 terms: [2 terms][D / 64 halves of k][D rows n][128 bytes].
+// Entry (i, j) of Q is a product over the stages: when stage s comes, the element that leads from j to i has i's bits below s and j's from s
+// on; its pair gives c if bit s of i and j are the same, else s (i's is 1) or -s.  Products over the stages from s on depend on j's bits from s on
+// alone, so that a thread with half a row of Q makes D / 2 entries with D / 2 multiplications and a few.
+template <int D, bool READ, int BITS>
+__device__ __forceinline__ void build_matrix(uint32_t to, const float2* tw) {
+    constexpr int kStages = D == 64 ? 6 : 7;
+    constexpr uint32_t kTerm = D * D * 2;
+    const int i = threadIdx.x % D, w = threadIdx.x / D;  // row, upper bit of j
+    if (w < 2) {
+        float v[D / 2];
+        v[0] = 1.f;
+        int n = 1;
+#pragma unroll
+        for (int s = kStages - 1; s >= 0; --s) {
+            const bool one = i >> s & 1;
+            if (s == kStages - 1) {
+                const float2 t = load_plain(tw + s * (D / 2) + (i & ((1 << s) - 1)));
+                v[0] = (one == (w == 1)) ? t.x : (one ? t.y : -t.y);
+            } else {
+#pragma unroll
+                for (int k = D / 4 - 1; k >= 0; --k)
+                    if (k < n) {
+                        const float2 t = load_plain(tw + s * (D / 2) + (((w * n + k) << s) | (i & ((1 << s) - 1))));
+                        const float x = v[k];
+                        v[2 * k] = x * (one ? t.y : t.x), v[2 * k + 1] = x * (one ? t.x : -t.y);
+                    }
+                n *= 2;
+            }
+        }
+        auto split = [](float x, uint16_t& hi, uint16_t& lo) {
+            const __half h = __float2half_rn(x);
+            hi = __half_as_ushort(h), lo = __half_as_ushort(__float2half_rn(x - __half2float(h)));
+        };
+        if constexpr (!READ) {  // n = i, k = j
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint16_t h[2], l[2];
+                    split(v[8 * c + 2 * e] * 1024.f, h[0], l[0]), split(v[8 * c + 2 * e + 1] * 1024.f, h[1], l[1]);
+                    hi[e] = h[0] | uint32_t(h[1]) << 16, lo[e] = l[0] | uint32_t(l[1]) << 16;
+                }
+                const int j = w * (D / 2) + 8 * c;
+                const uint32_t at = to + (j >> 6) * (D * 128) + i * 128 + (((j >> 3 & 7) ^ (i & 7)) << 4);
+                store16(at, hi[0], hi[1], hi[2], hi[3]), store16(at + kTerm, lo[0], lo[1], lo[2], lo[3]);
+            }
+        } else {  // n = j, k = the place of i
+            const int k = (i & ~7) + place_of<BITS>(i & 7);
+#pragma unroll
+            for (int c = 0; c < D / 2; ++c) {
+                const int j = w * (D / 2) + c;
+                const uint32_t at = to + (k >> 6) * (D * 128) + j * 128 + (((k >> 3 & 7) ^ (j & 7)) << 4) + 2 * (k & 7);
+                uint16_t hi, lo;
+                split(v[c] * 1024.f, hi, lo);
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(hi) : "memory");
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + kTerm), "h"(lo) : "memory");
+            }
+        }
+    }
+    fence_operands();
+}
+
+// Shared memory: the matrix, weights of queries' and keys' norms and ones, each warp's rows in and out.
+template <int D, int IN, int OUT, bool ONE>  // bytes of a row; ONE: rows go out through the place of those that came in
+struct RowsSmem {
+    static constexpr int kInPitch = IN + 16, kOutPitch = OUT + 16;
+    static constexpr uint32_t kNorms = 4 * D * D, kBars = kNorms + 3 * D * 4, kWarps = kBars + 64, kOut = ONE ? 0 : 32 * kInPitch,
+                              kWarp = ONE ? 32 * (kInPitch > kOutPitch ? kInPitch : kOutPitch) : 32 * (kInPitch + kOutPitch);
+    static constexpr uint32_t kBytes = kWarps + (kRowsThreads / 32) * kWarp + 1024;  // and what rounding the base up to 1024 takes
+    static constexpr int kCtas = kBytes < 110000 ? 2 : 1;                            // on an SM; they share tensor memory
 };
+template <int COLUMNS>
+__device__ __forceinline__ void tensor_memory(uint32_t at) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "n"(COLUMNS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <int COLUMNS>
+__device__ __forceinline__ void tensor_memory_free(uint32_t at) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(COLUMNS) : "memory");
+}
+
+// The product of a group's 128 rows, whose TERMS terms of fp16 are in tensor memory (D / 2 columns each, then the result's D): all threads of the
+// group call it, and have the result in tensor memory when it returns.
+template <int D, int TERMS>
+__device__ __forceinline__ void multiply(uint32_t columns, uint32_t matrix, uint32_t bar, uint32_t& phase, volatile int* dead, int* status) {
+    tmem_wait_st();
+    tmem_fence_before();
+    bar_sync(1 + (threadIdx.x >> 7), 128);
+    if ((threadIdx.x >> 5 & 3) == 0) {
+        tmem_fence_after();
+        const uint32_t lead = elect_one();
+#pragma unroll
+        for (int term = 0; term < TERMS + 1; ++term)  // h Qh, h Ql, l Qh
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                mma_ts(lead, columns + D, columns + (term == 2 ? D / 2 : 0) + 8 * k, operand(matrix + (term == 1 ? D * D * 2 : 0) + (k >> 2) * (D * 128) + (k & 3) * 32, 0),
+                       instruction(D, 0), term > 0 || k > 0);
+        commit_to(lead, bar);
+    }
+    wait_for(bar, phase, dead, status);
+    phase ^= 1;
+    tmem_fence_after();
+}
+// the result's row, times f
+template <int D>
+__device__ __forceinline__ void result_row(uint32_t at, float f, u64 (&x)[D / 2]) {
+    const u64 f2 = pack2(f, f);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        uint32_t v[32];
+        tmem_ld32(at + 32 * c, v);
+        tmem_wait_ld32(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[16 * c + i] = mul2(pack2u(v[2 * i], v[2 * i + 1]), f2);
+    }
+}
+
+template <int D, bool F32>
+using AppendSmem = RowsSmem<D, D*(F32 ? 4 : 2), 2 * D, F32>;
 
 template <int D, bool F32, int BITS>
-__global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_append(const AppendParams p) {
-    using S = AppendSmem<D, F32, BITS>;
-    extern __shared__ __align__(16) uint8_t smem[];
+__global__ void __launch_bounds__(kRowsThreads, AppendSmem<D, F32>::kCtas) k_append(const AppendParams p) {
+    using S = AppendSmem<D, F32>;
+    constexpr int kIn = D * (F32 ? 4 : 2), kCodes = D * BITS / 8;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int dead;
     grid_dep_wait();
-    const int lane = threadIdx.x & 31;
-    const uint32_t table = smem_u32(smem), norms = table + S::kNorms, in = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp, out = in + 32 * S::kInPitch;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, norms = base + S::kNorms, in = base + S::kWarps + warp * S::kWarp, out = in + S::kOut,
+                   bar = base + S::kBars + 8 * (warp >> 2);
     const int heads = p.q.heads + 2 * p.cache.heads, rows = static_cast<int>(p.tokens) * heads;  // rows of a token: queries, keys, values
-    Chunks chunks(rows);
-    // The lane's row of a chunk.  Found anew wherever it is needed, so that it takes no registers while the row is worked on.
+    Tiles tiles(rows);
+    // The thread's row of a tile.  Found anew wherever it is needed, so that it takes no registers while the row is worked on.
     struct Row {
         int token, kind, head;  // 0 query, 1 key, 2 value, -1 none
     };
-    auto find = [&](int chunk) {
-        const int row = chunk * 32 + lane;
+    auto find = [&](int tile) {
+        const int row = tiles.row(tile, rows);
         Row r{row / heads, -1, 0};
-        if (row < 0 || row >= rows) return Row{0, -1, 0};
+        if (row < 0) return Row{0, -1, 0};
         const int i = row - r.token * heads;
         r.kind = i < p.q.heads ? 0 : (i < p.q.heads + p.cache.heads ? 1 : 2);
         r.head = r.kind == 0 ? i : (r.kind == 1 ? i - p.q.heads : i - p.q.heads - p.cache.heads);
         return r;
     };
-    auto data_of = [&](const Row& r) {
+    auto fetch = [&](const Row& r) {
         const Heads& from = r.kind == 0 ? p.q : (r.kind == 1 ? p.k : p.v);
-        return from.data + (r.token * from.token + r.head * from.head) * (F32 ? 4 : 2);
+        each_chunk<kIn, S::kInPitch>(from.data + (r.token * from.token + r.head * from.head) * (F32 ? 4 : 2), r.kind >= 0 ? kIn : 0,
+                                     [&](uint32_t at, uint8_t* data) { copy_in(in + at, data); });
     };
-    auto fetch = [&](const Row& r) { each_chunk<S::kIn, S::kInPitch>(data_of(r), r.kind >= 0 ? S::kIn : 0, [&](uint32_t at, uint8_t* from) { copy_in(in + at, from); }); };
     auto position_of = [&](const Row& r) { return p.positions != nullptr && (r.kind == 0 || r.kind == 1) ? load_plain(p.positions + r.token) : 0; };
     auto angles_of = [&](int position) { return p.rope + (position >= 0 && position < p.rope_rows ? position : 0) * int64_t(p.rope_dims); };
-    auto prefetch = [&](const Row& r, int position) {  // a row's angles, into the cache
-        if (p.positions == nullptr || r.kind < 0 || r.kind > 1) return;
-        const float* at = angles_of(position);
-        for (int i = 0; i < p.rope_dims; i += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(at + i));
-    };
-    {
-        const Row first = find(chunks.there() ? chunks.at : -1);
-        fetch(first);
-        prefetch(first, position_of(first));
+    fetch(find(tiles.at));
+    if (threadIdx.x == 0) {
+        for (int g = 0; g < kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);
+        mbar_init_fence();
+        dead = 0;
     }
-    for (int i = threadIdx.x; i < D; i += blockDim.x) {
-        float* w = reinterpret_cast<float*>(smem + S::kNorms);
+    if (warp == 0) tensor_memory<4 * D>(smem_u32(&tmem_at));
+    for (int i = threadIdx.x; i < D; i += kRowsThreads) {
+        float* w = reinterpret_cast<float*>(smem_raw + (norms - smem_u32(smem_raw)));
         w[i] = p.q_norm != nullptr ? load_plain(p.q_norm + i) : 1.f, w[D + i] = p.k_norm != nullptr ? load_plain(p.k_norm + i) : 1.f, w[2 * D + i] = 1.f;
     }
-    const bool scaled = RowTurn<D, false>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
+    build_matrix<D, false, BITS>(base, p.tw);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t columns = tmem_at + 2 * D * (warp >> 2), mine = columns + (uint32_t(warp & 3) << 21);  // the group's; the warp's 32 lanes of them
     const bool normed = p.q_norm != nullptr || p.k_norm != nullptr;
-    for (; chunks.there(); chunks.at += chunks.step) {
-        u64 x[D / 2];
-        copies_done();
-        __syncwarp();
-        const Row now = find(chunks.at), next = find(chunks.at + chunks.step < chunks.end ? chunks.at + chunks.step : -1);
+    uint32_t phase = 0;
+    for (; tiles.there(); tiles.at += kGroups) {
+        const Row now = find(tiles.at), next = find(tiles.at + kGroups);
         const bool turned = p.positions != nullptr && (now.kind == 0 || now.kind == 1);
-        const int position = position_of(now), position_next = position_of(next);
-        if (turned && (position < 0 || position >= p.rope_rows)) atomicExch(p.status, kBadIndex);
-        const float* const angles = angles_of(position);
-        auto prepare = [&]() {  // norm and position
+        const int position = position_of(now);
+        float down;
+        {
+            u64 x[D / 2];
+            copies_done();
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < kIn / 16; ++c) unpack_chunk<F32>(shared_load(in + lane * S::kInPitch + 16 * c), x + (F32 ? 2 : 4) * c);
+            __syncwarp();
+            if (!F32) fetch(next);  // fp32: the place is for the rows out first
             if (normed) {
                 u64 sum = pack2(0.f, 0.f);
 #pragma unroll
@@ -186,29 +308,34 @@ __global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_append(co
                 }
             }
             if (turned) {
+                if (position < 0 || position >= p.rope_rows) atomicExch(p.status, kBadIndex);
+                const float* const angles = angles_of(position);
                 if (p.interleaved) turn_neighbours<D>(p.rope_dims, x, angles);
                 else turn_halves_of<D>(p.rope_dims, x, angles);
             }
-        };
-        constexpr int kPairs = F32 ? 2 : 4;  // of 16 bytes
-        for (bool plain = !scaled, again = false;; plain = again = true) {  // once, or again from memory in the plain form
+            const RowPower power(largest<D>(x));
+            down = power.down * (1.f / 1024.f);
+            const u64 up2 = pack2(power.up, power.up);
 #pragma unroll
-            for (int c = 0; c < S::kIn / 16; ++c) {
-                uint4 v;
-                if (!again) v = shared_load(in + lane * S::kInPitch + 16 * c);
-                else v = now.kind >= 0 ? load_plain(reinterpret_cast<const uint4*>(data_of(now)) + c) : make_uint4(0, 0, 0, 0);
-                unpack_chunk<F32>(v, x + kPairs * c);
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t h[16], l[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const u64 y = mul2(x[16 * c + i], up2);
+                    float a, b;
+                    unpack2(y, a, b);
+                    h[i] = half_pair(a, b);
+                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+                    unpack2(sub2(y, pack2(back.x, back.y)), a, b);
+                    l[i] = half_pair(a, b);
+                }
+                tmem_st16(mine + 16 * c, h);
+                tmem_st16(mine + D / 2 + 16 * c, l);
             }
-            if (!again) {
-                __syncwarp();
-                fetch(next);
-            }
-            prepare();
-            if (!again) prefetch(next, position_next);
-            if (plain) RowTurn<D, false>::plain(x, p.tw);
-            else RowTurn<D, false>::scaled(x, table);
-            if (plain || __all_sync(0xFFFFFFFFu, now.kind < 0 || all_finite<D>(x))) break;
         }
+        multiply<D, 2>(columns, base, bar, phase, &dead, p.status);
+        u64 x[D / 2];
+        result_row<D>(mine + D, down, x);
         uint8_t* to = nullptr;
         int bytes = 0;
         if (now.kind == 0) {
@@ -222,7 +349,7 @@ __global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_append(co
             const u64 inv2 = pack2(inv, inv), magic = pack2(12582912.f, 12582912.f);  // the sum's low bits are the nearest integer
             const bool clip = !(top * inv < kTop + 0.499f);                           // a scale that was rounded down far, or cut
 #pragma unroll
-            for (int c = 0; c < S::kCodes / 16; ++c) {
+            for (int c = 0; c < kCodes / 16; ++c) {
                 uint32_t w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -254,39 +381,44 @@ __global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_append(co
             if (slot >= 0 && page < p.cache.pages) {
                 const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
                 const Half& half = now.kind == 1 ? p.cache.k : p.cache.v;
-                to = codes_of<S::kCodes>(half, p.cache.page_shift, page, now.head, place), bytes = S::kCodes;
+                to = codes_of<kCodes>(half, p.cache.page_shift, page, now.head, place), bytes = kCodes;
                 *scale_of(half, p.cache.page_shift, page, now.head, place) = stored;
             }
         }
         __syncwarp();
         each_chunk<2 * D, S::kOutPitch>(to, bytes, [&](uint32_t at, uint8_t* dst) { *reinterpret_cast<uint4*>(dst) = shared_load(out + at); });
+        __syncwarp();
+        if (F32) fetch(next);
     }
+    copies_done();
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 0) tensor_memory_free<4 * D>(tmem_at);
 }
 
 template <int D, bool F32, int BITS>
-struct ReadSmem {
-    static constexpr int kIn = D * BITS / 8, kInPitch = kIn + 16, kOut = D * (F32 ? 4 : 2), kOutPitch = kOut + 16;
-    static constexpr uint32_t kTable = RowTurn<D, true>::kBytes, kProducts = kTable, kWarps = kProducts + D * 4, kWarp = 32 * (kInPitch + kOutPitch);
-    static constexpr uint32_t bytes(int warps) { return kWarps + warps * kWarp; }
-};
+using ReadSmem = RowsSmem<D, D * BITS / 8, D*(F32 ? 4 : 2), F32>;
 
 template <int D, bool F32, int BITS>
-__global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_read(const ReadParams p) {
+__global__ void __launch_bounds__(kRowsThreads, ReadSmem<D, F32, BITS>::kCtas) k_read(const ReadParams p) {
     using S = ReadSmem<D, F32, BITS>;
-    extern __shared__ __align__(16) uint8_t smem[];
+    constexpr int kIn = D * BITS / 8, kOut = D * (F32 ? 4 : 2);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int dead;
     grid_dep_wait();
-    const int lane = threadIdx.x & 31;
-    const uint32_t table = smem_u32(smem), in = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp, out = in + 32 * S::kInPitch;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, in = base + S::kWarps + warp * S::kWarp, out = in + S::kOut, bar = base + S::kBars + 8 * (warp >> 2);
     const int heads = 2 * p.cache.heads, rows = static_cast<int>(p.tokens) * heads;  // rows of a token: keys, values
-    Chunks chunks(rows);
+    Tiles tiles(rows);
     struct Row {
         const uint8_t* data;  // null: zeros
         uint16_t scale;
     };
-    auto find = [&](int chunk) {
+    auto find = [&](int tile) {
         Row r{};
-        const int row = chunk * 32 + lane;
-        if (row < 0 || row >= rows) return r;
+        const int row = tiles.row(tile, rows);
+        if (row < 0) return r;
         const int token = row / heads, i = row - token * heads, head = i < p.cache.heads ? i : i - p.cache.heads;
         const int64_t slot = load_plain(p.slots + token), page = slot >> p.cache.page_shift;
         if (slot < 0) return r;
@@ -296,48 +428,51 @@ __global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_read(cons
         }
         const int place = static_cast<int>(slot) & ((1 << p.cache.page_shift) - 1);
         const Half& half = i < p.cache.heads ? p.cache.k : p.cache.v;
-        r.data = codes_of<S::kIn>(half, p.cache.page_shift, page, head, place);
+        r.data = codes_of<kIn>(half, p.cache.page_shift, page, head, place);
         r.scale = *static_cast<volatile const uint16_t*>(scale_of(half, p.cache.page_shift, page, head, place));
         return r;
     };
-    auto to_of = [&](int chunk) -> uint8_t* {
-        const int row = chunk * 32 + lane, token = row / heads, i = row - token * heads;
-        if (row >= rows) return nullptr;
-        return (i < p.cache.heads ? p.k : p.v) + (int64_t(token) * p.cache.heads + (i < p.cache.heads ? i : i - p.cache.heads)) * S::kOut;
-    };
-    auto fetch = [&](const Row& r) { each_chunk<S::kIn, S::kInPitch>(r.data, r.data != nullptr ? S::kIn : 0, [&](uint32_t at, uint8_t* from) { copy_in(in + at, from); }); };
-    Row now = find(chunks.there() ? chunks.at : -1);
+    auto fetch = [&](const Row& r) { each_chunk<kIn, S::kInPitch>(r.data, r.data != nullptr ? kIn : 0, [&](uint32_t at, uint8_t* from) { copy_in(in + at, from); }); };
+    Row now = find(tiles.at);
     fetch(now);
-    const bool scaled = RowTurn<D, true>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
-    for (; chunks.there(); chunks.at += chunks.step) {
+    if (threadIdx.x == 0) {
+        for (int g = 0; g < kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);
+        mbar_init_fence();
+        dead = 0;
+    }
+    if (warp == 0) tensor_memory<4 * D>(smem_u32(&tmem_at));
+    build_matrix<D, true, BITS>(base, p.tw);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t columns = tmem_at + 2 * D * (warp >> 2), mine = columns + (uint32_t(warp & 3) << 21);
+    const Unpack<BITS> unpack;
+    uint32_t phase = 0;
+    for (; tiles.there(); tiles.at += kGroups) {
         copies_done();
         __syncwarp();
-        uint4 raw[S::kIn / 16];
+        uint4 raw[kIn / 16];
 #pragma unroll
-        for (int c = 0; c < S::kIn / 16; ++c) raw[c] = now.data != nullptr ? shared_load(in + lane * S::kInPitch + 16 * c) : make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < kIn / 16; ++c) raw[c] = now.data != nullptr ? shared_load(in + lane * S::kInPitch + 16 * c) : make_uint4(0, 0, 0, 0);
         __syncwarp();
-        const Row next = find(chunks.at + chunks.step < chunks.end ? chunks.at + chunks.step : -1);
-        fetch(next);
-        // codes are at most 128 and scales at most 65504: the scaled form, at most 2^40 times that, stays finite
-        const float s = half_value(now.scale);
-        const u64 s2 = pack2(s, s), base = pack2(-8388608.f - (1 << (BITS - 1)), -8388608.f - (1 << (BITS - 1)));
-        u64 x[D / 2];
+        const Row next = find(tiles.at + kGroups);
+        if (!F32) fetch(next);  // fp32: the place is for the rows out first
+        constexpr int kWords = D * BITS / 32, kPairs = 16 / BITS;  // of a row; of a word
 #pragma unroll
-        for (int c = 0; c < S::kIn / 16; ++c) {
-            const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t h[16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                constexpr int kCodesOfWord = 32 / BITS;
-                const uint32_t v = w[i] ^ (BITS == 4 ? 0x88888888u : 0x80808080u);  // code + 2^(bits - 1): low bits on top of 2^23
-#pragma unroll
-                for (int e = 0; e < kCodesOfWord; e += 2) {
-                    const uint32_t lo = (v >> (e * BITS)) & ((1u << BITS) - 1), hi = (v >> (e * BITS + BITS)) & ((1u << BITS) - 1);
-                    x[((4 * c + i) * kCodesOfWord + e) / 2] = mul2(s2, add2(pack2u(lo | 0x4B000000u, hi | 0x4B000000u), base));
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int pair = 16 * c + i, word = pair / kPairs;
+                static_assert(kWords * kPairs == D / 2, "a row");
+                const uint32_t w = (word & 3) == 0 ? raw[word / 4].x : ((word & 3) == 1 ? raw[word / 4].y : ((word & 3) == 2 ? raw[word / 4].z : raw[word / 4].w));
+                h[i] = unpack(w, pair % kPairs);
             }
+            tmem_st16(mine + 16 * c, h);
         }
-        if (scaled) RowTurn<D, true>::scaled(x, table);
-        else RowTurn<D, true>::plain(x, p.tw);
+        multiply<D, 1>(columns, base, bar, phase, &dead, p.status);
+        u64 x[D / 2];
+        result_row<D>(mine + D, half_value(now.scale) * (1.f / 1024.f), x);
         if constexpr (F32) {
 #pragma unroll
             for (int c = 0; c < D / 4; ++c) {
@@ -349,31 +484,39 @@ __global__ void __launch_bounds__(32 * kMostWarps, D == 128 ? 3 : 5) k_read(cons
             store_bf16<D>(out + lane * S::kOutPitch, x);
         }
         __syncwarp();
-        uint8_t* const to = to_of(chunks.at);
-        each_chunk<S::kOut, S::kOutPitch>(to, to != nullptr ? S::kOut : 0, [&](uint32_t at, uint8_t* dst) { *reinterpret_cast<uint4*>(dst) = shared_load(out + at); });
+        const int row = tiles.row(tiles.at, rows), token = row / heads, i = row - token * heads;
+        uint8_t* const to = (i < p.cache.heads ? p.k : p.v) + (int64_t(token) * p.cache.heads + (i < p.cache.heads ? i : i - p.cache.heads)) * kOut;
+        each_chunk<kOut, S::kOutPitch>(to, row >= 0 ? kOut : 0, [&](uint32_t at, uint8_t* dst) { *reinterpret_cast<uint4*>(dst) = shared_load(out + at); });
+        __syncwarp();
+        if (F32) fetch(next);
         now = next;
     }
+    copies_done();
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 0) tensor_memory_free<4 * D>(tmem_at);
 }
 
+// as many CTAs as their shared memory lets run at once
 template <class S, class Kernel, class Params>
-static cudaError_t launch_rows(const bfq_plan* plan, Kernel kern, int* per_sm, int64_t rows, const Params& p, cudaStream_t st) {
-    int& occ = per_sm[plan->device];
-    if (occ == 0) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::bytes(kMostWarps)));
-        int n = 0;
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * kMostWarps, S::bytes(kMostWarps));
+static cudaError_t launch_rows(const bfq_plan* plan, Kernel kern, bool* ready, int64_t rows, const Params& p, cudaStream_t st) {
+    if (!ready[plan->device]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::kBytes));
         if (e != cudaSuccess) return e;
-        occ = n > 0 ? n : 1;
+        ready[plan->device] = true;
     }
-    const int64_t want = (rows + 32 * kMostWarps - 1) / (32 * kMostWarps), most = int64_t(plan->sm_count) * occ;
-    return launch_overlapped(kern, dim3(unsigned(want < most ? want : most)), dim3(32 * kMostWarps), S::bytes(kMostWarps), st, p);
+    const int64_t want = (rows + 128 * kGroups - 1) / (128 * kGroups), most = int64_t(plan->sm_count) * S::kCtas;
+    return launch_overlapped(kern, dim3(unsigned(want < most ? want : most)), dim3(kRowsThreads), S::kBytes, st, p);
 }
-static bool few_rows(int64_t rows) { return rows < 65536; }
+// Measured either side (us; bf16, 32 + 2 x 8 heads appended with norms and positions / read, few : many): n = 128, 6144 rows 6.7 : 12.1 / 6.2 : 7.6,
+// 12288 13.8 : 12.3 / 7.2 : 7.6, 24576 20.8 : 12.5 / 9.5 : 7.9, 65280 37.7 : 21.8 / 16.0 : 11.7; n = 64, 6144 4.2 : 7.3 / 3.4 : 4.7,
+// 12288 5.3 : 7.4 / 4.5 : 4.6, 24576 11.0 : 7.4 / 5.4 : 4.8, 65280 19.5 : 10.4 / 8.5 : 6.9.
+static bool few_rows(int64_t rows) { return rows < 16384; }
 
 template <int D, bool F32, int BITS>
 static cudaError_t launch_append_bits(const bfq_plan* plan, const AppendParams& p, cudaStream_t st) {
-    static int per_sm[kMaxDevices] = {0};
-    return launch_rows<AppendSmem<D, F32, BITS>>(plan, k_append<D, F32, BITS>, per_sm, p.tokens * (p.q.heads + 2 * p.cache.heads), p, st);
+    static bool ready[kMaxDevices] = {false};
+    return launch_rows<AppendSmem<D, F32>>(plan, k_append<D, F32, BITS>, ready, p.tokens * (p.q.heads + 2 * p.cache.heads), p, st);
 }
 template <int D, bool F32>
 static cudaError_t launch_append(const bfq_plan* plan, const AppendParams& p, cudaStream_t st) {
@@ -382,8 +525,8 @@ static cudaError_t launch_append(const bfq_plan* plan, const AppendParams& p, cu
 }
 template <int D, bool F32, int BITS>
 static cudaError_t launch_read_bits(const bfq_plan* plan, const ReadParams& p, cudaStream_t st) {
-    static int per_sm[kMaxDevices] = {0};
-    return launch_rows<ReadSmem<D, F32, BITS>>(plan, k_read<D, F32, BITS>, per_sm, p.tokens * 2 * p.cache.heads, p, st);
+    static bool ready[kMaxDevices] = {false};
+    return launch_rows<ReadSmem<D, F32, BITS>>(plan, k_read<D, F32, BITS>, ready, p.tokens * 2 * p.cache.heads, p, st);
 }
 template <int D, bool F32>
 static cudaError_t launch_read(const bfq_plan* plan, const ReadParams& p, cudaStream_t st) {

@@ -40,59 +40,6 @@ struct TallSmem {
 // per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products up to date
 enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kBarCount = 20 };
 
-__device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// the wait of a converged warp
-__device__ __forceinline__ void wait_all(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
-    wait_for(bar, parity, dead, status);
-    __syncwarp();
-}
-__device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ float4 load_shared4(uint32_t at) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
-}
-// 128-byte swizzle, 8-row groups 1024 bytes apart; MN-major operands: blocks of 64 elements `leading` bytes apart
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(leading >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
-           (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
-}
-// fp16 x fp16 -> fp32, M = 128
-__host__ __device__ constexpr uint32_t instruction(int n, int v_mn_major) {
-    return (1u << 4) | (uint32_t(v_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(128 >> 4) << 24);
-}
-// Issued by the one thread of a converged warp whose `lead` is set: a predicate on the instruction and no branch around it, so that the
-// operands can stay in uniform registers.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
-__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
-        "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
-        "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ void commit_to(uint32_t lead, uint32_t bar) {
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead)
-                 : "memory");
-}
-
-// Place i of a 16-byte chunk holds element order(i) of its eight.
-template <int BITS>
-__host__ __device__ constexpr int order(int i) {
-    return BITS == 4 ? (i >> 1) + 4 * (i & 1) : (i & 4) + ((i >> 1) & 1) + 2 * (i & 1);
-}
-
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendParams p) {
     using M = TallSmem<D>;

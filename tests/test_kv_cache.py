@@ -175,15 +175,16 @@ def test_append(n, bits, page, dtype, hq, hkv, tokens, norm, dims, interleaved):
 
 
 def check_nearest(codes, scales, y, bits):
-    """Every code is a nearest one, up to 1e-4 of a step, on a scale within one fp16 step: check_quant without its count of codes next to a
-    boundary.  Angles that are multiples of pi / 2 in fp32 have cosines of some 4e-8, so a rotated bf16 row is its elements to that part, and those
-    lie on exact ties k + 1/2 of the fp16 scale in bulk: which side they fall on is below fp32's 2^-24 = 6e-8, and both are right."""
+    """Every code is a nearest one on a scale within one fp16 step: check_quant without its count of codes next to a boundary, and up to the error of
+    rows that are rotated on the tensor cores, 2^-20 of the row's norm (22 bits of row and rotation), which is at most sqrt(n) times its largest
+    element, top steps.  No count: angles that are multiples of pi / 2 in fp32 have cosines of some 4e-8, so a rotated bf16 row is its elements
+    to that part, and those lie on exact ties k + 1/2 of the fp16 scale in bulk: which side they fall on is below any of these roundings."""
     got, s = oracle.unpack(codes.cpu().numpy(), bits).astype(np.float64), to_f64(scales)
     top = 2.0 ** (bits - 1) - 1
     want = np.minimum(np.abs(y).max(1) / top, 65504)
     assert (np.abs(s - want) <= 2.0 ** -10 * want + 2.0 ** -25).all()
     pre = np.clip(y / np.where(s > 0, s, np.inf)[:, None], -top - 1, top)
-    assert (np.abs(got - pre) <= 0.5 + 1e-4).all()
+    assert (np.abs(got - pre) <= 0.5 + max(1e-4, 2.0 ** -20 * np.sqrt(y.shape[1]) * top)).all()
 
 
 MANY = [(128, 4, 64, torch.bfloat16, 8, 4), (128, 8, 32, torch.float32, 5, 1), (64, 8, 16, torch.bfloat16, 3, 1), (64, 4, 128, torch.float32, 30, 5)]
@@ -226,7 +227,7 @@ def test_append_and_read_many(n, bits, page, dtype, hq, hkv, angles, size):
     for i, (which, ref) in enumerate((("k", turn(x[:, hq:hq + hkv], w[1])), ("v", x[:, hq + hkv:]))):
         codes, scales = rows_at(cache, which, at)
         y = oracle.forward(theta, ref[keep].reshape(-1, n))
-        (check_quant if angles != "right" else check_nearest)(codes.reshape(-1, codes.shape[-1]), scales.reshape(-1), y, bits)
+        check_nearest(codes.reshape(-1, codes.shape[-1]), scales.reshape(-1), y, bits)
         rows = np.zeros((tokens, hkv, n))
         rows[keep] = oracle.dequantize(oracle.unpack(codes.reshape(-1, codes.shape[-1]).cpu().numpy(), bits),
                                        scales.reshape(-1).cpu().view(torch.int16).numpy().view(np.uint16)).reshape(-1, hkv, n)
