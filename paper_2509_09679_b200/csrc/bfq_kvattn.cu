@@ -508,9 +508,9 @@ static bool encode_half(CUtensorMap* map, const Half& half, const Cache& cache, 
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// One of the kernel's forms: CTAs of a launch, all that the chip runs at once (ctas), or the launch (st).
+// One of the kernel's forms: all CTAs that the chip runs at once (ctas), or a launch of `grid` on st.
 template <int D, int BITS, int NB>
-static cudaError_t attend_form(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
+static cudaError_t attend_form(const bfq_plan* plan, const AttendParams& p, int* ctas, int grid, cudaStream_t st) {
     using S = Stage<D, BITS, NB>;
     static int per_sm[kMaxDevices] = {0};
     int& occ = per_sm[plan->device];
@@ -527,15 +527,15 @@ static cudaError_t attend_form(const bfq_plan* plan, const AttendParams& p, int*
     }
     Maps maps;
     if (!encode_half(&maps.k_codes, p.cache.k, p.cache, S::kRow) || !encode_half(&maps.v_codes, p.cache.v, p.cache, S::kRow)) return cudaErrorInvalidValue;
-    return launch_overlapped(k_attend<D, BITS, NB>, dim3(unsigned(plan->sm_count * occ)), dim3(kAttendThreads), S::kSmem, st, p, maps);
+    return launch_overlapped(k_attend<D, BITS, NB>, dim3(unsigned(grid)), dim3(kAttendThreads), S::kSmem, st, p, maps);
 }
 template <int D, int BITS>
-static cudaError_t attend_rows(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
-    return p.few.rows == 8 ? attend_form<D, BITS, 1>(plan, p, ctas, st) : attend_form<D, BITS, 2>(plan, p, ctas, st);
+static cudaError_t attend_rows(const bfq_plan* plan, const AttendParams& p, int* ctas, int grid, cudaStream_t st) {
+    return p.few.rows == 8 ? attend_form<D, BITS, 1>(plan, p, ctas, grid, st) : attend_form<D, BITS, 2>(plan, p, ctas, grid, st);
 }
-static cudaError_t attend(const bfq_plan* plan, const AttendParams& p, int* ctas, cudaStream_t st) {
-    return plan->n == 64 ? (p.cache.bits == 4 ? attend_rows<64, 4>(plan, p, ctas, st) : attend_rows<64, 8>(plan, p, ctas, st))
-                         : (p.cache.bits == 4 ? attend_rows<128, 4>(plan, p, ctas, st) : attend_rows<128, 8>(plan, p, ctas, st));
+static cudaError_t attend(const bfq_plan* plan, const AttendParams& p, int* ctas, int grid = 0, cudaStream_t st = nullptr) {
+    return plan->n == 64 ? (p.cache.bits == 4 ? attend_rows<64, 4>(plan, p, ctas, grid, st) : attend_rows<64, 8>(plan, p, ctas, grid, st))
+                         : (p.cache.bits == 4 ? attend_rows<128, 4>(plan, p, ctas, grid, st) : attend_rows<128, 8>(plan, p, ctas, grid, st));
 }
 
 // Tiles of 256 rows where there are rows enough to pay for them.
@@ -606,12 +606,17 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
 using namespace bfq;
 
 namespace {
-// CTAs of the two launches; a kernel that has no work: 0
+// CTAs of the two launches, no more than there can be units; a kernel that has no work: 0
 cudaError_t ctas_of_both(const bfq_plan* plan, const kv::AttendParams& p, int* few, int* tall) {
     *few = *tall = 0;
+    auto least = [&](const kv::Part& part, int ctas) {
+        auto units = [&](int64_t keys) { return (keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
+        const int64_t most = (part.tiles_prefix * units(p.prefix_length) + int64_t(p.batch) * part.tiles_seq * units(int64_t(p.table_width) << p.cache.page_shift)) * p.cache.heads;
+        return most < ctas ? (most > 1 ? int(most) : 1) : ctas;
+    };
     cudaError_t e = cudaSuccess;
-    if (p.entries(p.few) > 0) e = kv::attend(plan, p, few, nullptr);
-    if (e == cudaSuccess && p.entries(p.tall) > 0) e = kv::tall_ctas(plan, p.cache.bits, tall);
+    if (p.entries(p.few) > 0) e = kv::attend(plan, p, few), *few = least(p.few, *few);
+    if (e == cudaSuccess && p.entries(p.tall) > 0) e = kv::tall_ctas(plan, p.cache.bits, tall), *tall = least(p.tall, *tall);
     return e;
 }
 }  // namespace
@@ -640,7 +645,7 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         p.beside_tall = tall > 0;
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
-        if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, st);
+        if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, few, st);
         if (e == cudaSuccess && p.seq_tall && p.prefix_length == 0) {
             e = kv::join_tall_launch(plan, p, st);
         } else if (e == cudaSuccess) {

@@ -37,8 +37,8 @@ struct TallSmem {
     static constexpr uint32_t kBars = kFactors + kStageCount * 16;
     static constexpr uint32_t kBytes = kBars + 24 * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
-// per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products up to date
-enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kBarCount = 20 };
+// per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products of a unit done, of a pair
+enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kOFull = 20, kBarCount = 22 };
 
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendParams p) {
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             mbar_init(bar(kKvFull + s), kConvert), mbar_init(bar(kKvEmpty + s), 1);
             mbar_init(bar(kSFull + s), 1), mbar_init(bar(kPFull + s), 128);
         }
-        for (int t = 0; t < 2; ++t) mbar_init(bar(kQFull + t), 128), mbar_init(bar(kDone + t), 1);
+        for (int t = 0; t < 2; ++t) mbar_init(bar(kQFull + t), 128), mbar_init(bar(kDone + t), 1), mbar_init(bar(kOFull + t), 1);
         mbar_init_fence();
         dead = 0;
     }
@@ -87,7 +87,9 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         const uint32_t o_at = products(tile) + lanes;
         float m = -INFINITY, l = 0.f, row_scale = 0.f, unit = 0.f;
         int limit = 0, least = 0;  // keys of the row; of the warp's rows, at least
-        uint32_t s_phase = 0, done_phase = 0;  // s_phase: a bit for each buffer; done_phase: of the last products that were asked for
+        // s_phase: a bit for each buffer; done_phase: of the last products that were asked for.  When a unit's scores are there, the products of the
+        // unit before the last are done, so that a wait for the last one's parity means that one; at a pair's end they may not be
+        uint32_t s_phase = 0, done_phase = 0, o_phase = 0;
         bool active = false;
         long long pair_from = run.from - walk.unit;
         auto open = [&]() {
@@ -140,7 +142,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         auto close = [&](long long done) {
             const int pair = walk.pair(p);
             if (active) {
-                wait_for(bar(kDone + tile), done_phase ^ 1, &dead, p.status);
+                wait_for(bar(kOFull + tile), o_phase, &dead, p.status);
+                o_phase ^= 1;
                 tmem_fence_after();
                 const int r = 128 * tile + row_of_tile;
                 const bool there = r < walk.tile.rows;
@@ -382,7 +385,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         // ---- MMAs ----------------------------------------------------------------------------------------------------------------
         if (warp == 16) {
             const uint32_t lead = elect_one();
-            uint32_t p_phase = 0, q_phase[2] = {0, 0};  // p_phase: a bit for each tile and buffer
+            uint32_t p_phase = 0, done_phase = 0, q_phase[2] = {0, 0};  // a bit for each tile and buffer, for each tile
             constexpr uint32_t kScoresDesc = instruction(kTallUnit, 0), kProductsDesc = instruction(D, 1);
             auto issue_scores = [&](int tile, int i) {
                 const uint32_t a = base + M::kQ + tile * M::kTile, b = stage_at(i & 3);
@@ -419,12 +422,19 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                         p_phase ^= 1u << which;
                         tmem_fence_after();
                         issue_products(t, i, i > i0);
+                        if (i + 1 == i1) commit_to(lead, bar(kOFull + t));
+                    }
+                    commit_to(lead, bar(kKvEmpty + (i & 3)));
+                    if (i + 2 < i1) operands_there(i + 2);
+                    for (int t = 0; t < tiles; ++t) {
+                        // scores of another shape in the place of probabilities: products of different shapes are not ordered by themselves
+                        wait_all(bar(kDone + t), done_phase >> t & 1, &dead, p.status);
+                        done_phase ^= 1u << t;
                         if (i + 2 < i1) {
-                            if (t == 0) operands_there(i + 2);
+                            tmem_fence_after();
                             issue_scores(t, i + 2);
                         }
                     }
-                    commit_to(lead, bar(kKvEmpty + (i & 3)));
                 }
                 i0 = i1;
                 walk.next_pair(p, part);

@@ -82,16 +82,17 @@ def attention(q, theta, k, v, table, lengths, starts, page, scale, prefix=None, 
     Q = dense(theta)
     most = max((starts[b + 1] - starts[b] for b in range(len(lengths))), default=0)
     rounded = 2.0 ** -11 if group * max(most, (starts[len(lengths)] - starts[0]) if prefix_length else 0) > 16 else 2.0 ** -16
+    flat = lambda x, pages, h, count: x[pages, h].reshape(-1, n)[:count]
+    front = [(flat(k, prefix, h, prefix_length), flat(v, prefix, h, prefix_length)) for h in range(k.shape[1])] if prefix_length else None
     for b, length in enumerate(lengths):
         first, last = starts[b], starts[b + 1]
         for h in range(heads):
-            flat = lambda x, pages, count: x[pages, h // group].reshape(-1, n)[:count]
-            kk, vv = flat(k, table[b], length), flat(v, table[b], length)
+            kk, vv = flat(k, table[b], h // group, length), flat(v, table[b], h // group, length)
             for t in range(first, last):
                 own = max(0, length - (last - first) + (t - first) + 1)
                 ks, vs = kk[:own], vv[:own]
                 if prefix_length:
-                    ks, vs = np.concatenate([flat(k, prefix, prefix_length), ks]), np.concatenate([flat(v, prefix, prefix_length), vs])
+                    ks, vs = np.concatenate([front[h // group][0], ks]), np.concatenate([front[h // group][1], vs])
                 if not len(ks):
                     continue
                 s = ks @ q[t, h] * scale
@@ -365,6 +366,34 @@ def test_attend_shared_prefix(n, bits, page, hq, hkv, prefix_length, news, lengt
     out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), prefix=i32(prefix), prefix_length=prefix_length, want_lse=True, **some)
     assert p.device_status() == 0
     check_attention(out, lse, attention(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
+
+
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (64, 8), (128, 8), (64, 4)])
+@pytest.mark.parametrize("news,lengths,prefix_length", [([1] * 7, [9, 0, 70, 1, 33, 5, 200], 16384), ([40, 3, 60], [40, 90, 2000], 9000), ([300], [9000], 0)])
+def test_attend_many_units(n, bits, news, lengths, prefix_length):
+    """Runs of units that go many times through every ring and buffer of the kernels."""
+    page, hkv, hq = 64, 8, 56
+    if prefix_length == 0 or max(news) > 1:
+        hkv, hq = 4, 8
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 2, 45, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 46)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = (2 * torch.randn((starts[-1], hq, n), generator=torch.Generator().manual_seed(47))).to(torch.bfloat16)
+    some = dict(prefix=i32(prefix), prefix_length=prefix_length) if prefix_length else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
+    assert p.device_status() == 0
+    rows = np.unique(np.linspace(0, starts[-1] - 1, 24).astype(int))  # of so many tokens these are looked at, the first and last among them
+    first = np.searchsorted(starts, rows, side="right") - 1
+    wants = [attention(to_f64(q[t:t + 1]), theta, k, v, table[b:b + 1], [max(0, lengths[b] - (starts[b + 1] - 1 - t))], [0, 1], page, n ** -0.5, prefix, prefix_length)
+             for t, b in zip(rows, first)]
+    for t, want in zip(rows, wants):
+        ref, ref_lse, bound, lse_bound = want
+        scores = 2.0 ** -11 * n ** -0.5 * np.linalg.norm(to_f64(q[t]), axis=-1).max() * max(np.linalg.norm(x, axis=-1).max() for x in k)  # keys rounded to fp16
+        check_attention(out[t:t + 1], lse[t:t + 1], (ref, ref_lse, bound + 2 * scores * np.abs(v).max(), lse_bound + scores))
+    again = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), **some)
+    assert torch.equal(out, again)
 
 
 @gpu
