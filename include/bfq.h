@@ -396,7 +396,8 @@ typedef struct {
  * and values quantized (bfq_forward_quant's quantizer, a row is a head) into the cache at slots[token], queries to q_out in bf16.
  * slots: int64 [tokens]; a negative slot: the token's keys and values go nowhere (padding).  The other slots must differ from one another:
  * of two tokens with one slot, parts of either may stay.  q and q_out may both be NULL, and q_out may be q in place where q is bf16.
- * k, v and q are of type xt.  A slot or position outside its range is reported by bfq_device_status (BFQ_ERR_INDEX): that slot is not
+ * k, v and q are of type xt.  Calls with many rows run other kernels than calls with few and round differently: rows are off by at most 2^-20 of
+ * their norm before they are rounded or quantized.  A slot or position outside its range is reported by bfq_device_status (BFQ_ERR_INDEX): that slot is not
  * written, that position counts as 0.  Allocates nothing.
  */
 int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots, int64_t tokens, bfq_dtype xt, const bfq_heads* k, const bfq_heads* v,
@@ -417,6 +418,7 @@ int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots,
  *               last of which is key lengths[b] - 1; each sees the keys up to its own.  NULL: token b is sequence b's only one.
  *   prefix      pages of a prefix that all sequences share, int32 [prefix_pages], of which prefix_length keys are read, once for the
  *               whole batch; every token sees all of them.  lengths and block_table do not count them.  prefix_length 0: none.
+ * Probabilities (and, where more than 48 rows share their keys, the dequantized keys and values) are rounded to fp16, 2^-11 of each; all sums are fp32.
  * A row without keys (no length, or a token in front of its sequence's first key) is zero.  Rows of out and lse of tokens that no
  * sequence has stay as they were.  A page, length or number of tokens outside its range is reported by bfq_device_status
  * (BFQ_ERR_INDEX) and the outputs of that call mean nothing; memory outside the arrays is not touched.  workspace: device,

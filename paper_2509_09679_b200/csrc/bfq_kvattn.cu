@@ -34,7 +34,7 @@ struct Stage {
     static constexpr int kRow = D * BITS / 8;  // bytes of a row's codes
     static constexpr int kCount = kRow == 128 ? 2 : 3;
     static constexpr uint32_t kBytes = 2 * kKeys * kRow, kScaleBytes = 4 * kKeys;
-    static constexpr int kPitch = D + 4;  // of a merged row, floats
+    static constexpr int kPitch = D + (BITS == 4 ? 1 : 8);  // of a merged row, floats: lanes are kPer g + 2 t rows apart, two to a bank
     static constexpr uint32_t kScales = kWarps * kCount * kBytes, kMerge = kScales + kWarps * kCount * kScaleBytes, kSums = kMerge + 8 * NB * kPitch * 4,
                               kBars = kSums + kWarps * 8 * NB * 8;
     static constexpr uint32_t kSmem = kBars + kWarps * kCount * 8 + 1024;  // and what rounding the base up to 1024 takes
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     using S = Stage<D, BITS, NB>;
     constexpr int kSteps = D / 16, kRows = 8 * NB;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ long long scan[kWarps + 2];
+    __shared__ int scan[kWarps + 2];
     __shared__ volatile int dead;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     float* const merge = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + S::kMerge);  // [rows][pitch]
@@ -206,8 +206,8 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
         for (int b = 0; b < NB; ++b) least = min(least, 8 * b + g < tl.rows ? tl.last0 + (tl.row0 + 8 * b + g) / p.group + 1 : least);
         least = __reduce_min_sync(0xFFFFFFFFu, least);
     };
-    long long pair_from = run.from - now.unit;  // number of the pair's unit 0
-    auto close = [&](long long done) {          // after unit `done` (exclusive) of the numbering
+    int pair_from = run.from - now.unit;  // number of the pair's unit 0
+    auto close = [&](int done) {          // after unit `done` (exclusive) of the numbering
         const int pair = now.pair(p);
         const long long entry = blockIdx.x + pair;
 #pragma unroll
@@ -241,27 +241,25 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
             const int n = 2 * i + j;         // chunk n / kPer, unit g, code n % kPer of the unit
             return (n / kPer) * 8 * kPer + kPer * g + n % kPer;
         };
-        auto put = [&](float* to, bool add) {
+        // a quarter of the elements from each warp at a time, all four in turn: an element's sum starts with another warp, but always the same
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+        for (int turn = 0; turn < kWarps; ++turn) {
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i)
+            for (int i = 0; i < kSteps; ++i)
+                if (i / (kSteps / kWarps) == ((warp + turn) & (kWarps - 1))) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float* at = to + (8 * b + 2 * t + (j & 1)) * S::kPitch + element_of(i, j >> 1);
-                        const float v = o[b][i][j] * f[b][j & 1];
-                        *at = add ? *at + v : v;
-                    }
-        };
-        for (int w = 0; w < kWarps; ++w) {  // in this order, so that the sums are the same each time
-            if (warp == w) put(merge, w > 0);
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float* at = merge + (8 * b + 2 * t + (j & 1)) * S::kPitch + element_of(i, j >> 1);
+                            const float v = o[b][i][j] * f[b][j & 1];
+                            *at = turn > 0 ? *at + v : v;
+                        }
+                }
             __syncthreads();
         }
-        for (int i = tid; i < now.tile.rows * (D / 4); i += kAttendThreads) {
-            const int r = i / (D / 4), c = 4 * (i % (D / 4));
-            *reinterpret_cast<float4*>(part.parts + (entry * kRows + r) * D + c) = *reinterpret_cast<const float4*>(merge + r * S::kPitch + c);
-        }
-        if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + now.units - 1) / run.per - blockIdx.x + 1));
+        for (int i = tid; i < now.tile.rows * D; i += kAttendThreads) part.parts[(entry * kRows) * D + i] = merge[(i / D) * S::kPitch + i % D];
+        if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, (pair_from + now.units - 1) / run.per - static_cast<int>(blockIdx.x) + 1);
         pair_from = done;
     };
 
@@ -405,11 +403,16 @@ template <int D>
 __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
     constexpr int kE = D / 32;
     const int lane = threadIdx.x & 31;
-    grid_dep_wait();
+    // The kernel before has let this one start after it had waited for all that came before itself: constants, lengths and starts can be read
+    // while it still works.
     const int rows_all = static_cast<int>(p.tokens) * p.q.heads, row0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * each;
-    if (row0 >= rows_all) return;
+    if (row0 >= rows_all) {
+        grid_dep_wait();
+        return;
+    }
     Turn<D, kE, true> turn;
     turn.load(p.tw, lane);
+    bool waited = false;
     const int q_heads = p.q.heads, begin = first_token(p, 0), end = first_token(p, p.batch);
     int of = -1, b = 0, place = 0;  // token that b and place are of
     for (int row = row0; row < row0 + each && row < rows_all; ++row) {
@@ -434,8 +437,9 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
             const Part& part = tall ? p.tall : p.few;
             const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
             const int pair = entry * p.cache.heads + h;
-            const int2 found = load_plain(part.pairs + pair);  // beside the lengths; means something where there are keys
             if (tile_of(p, part, entry).keys == 0) return;
+            if (!waited) grid_dep_wait(), waited = true;
+            const int2 found = load_plain(part.pairs + pair);
             const int64_t first = static_cast<int64_t>(found.x) + pair;
             constexpr int kAtOnce = 4;  // results on their way
             float v[kAtOnce][kE];
@@ -483,6 +487,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
 #pragma unroll
         for (int e = 0; e < kE; ++e) o[e] *= f;
         turn.apply(o);
+        if (!waited) grid_dep_wait(), waited = true;  // what came before may still read where this is written
         uint8_t* out = const_cast<uint8_t*>(p.out.data) + (token * p.out.token + head * p.out.head + kE * lane) * 2;
         if constexpr (kE == 4) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]));
         else *reinterpret_cast<uint32_t*>(out) = bf16_pair(o[0], o[1]);
@@ -493,6 +498,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
             if (n != cached_keys(p, b)) atomicExch(p.status, kBadIndex);
         }
     }
+    if (!waited) grid_dep_wait();
 }
 
 // A half of the cache's codes as boxes of a page's rows of a head, at most kKeys of them: {bytes of a row, rows of a page, pages}
@@ -594,6 +600,10 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     const int tile_prefix = p->prefix_tall ? kTallRows : p->few.rows, tile_seq = p->seq_tall ? kTallRows : p->few.rows;
     const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;
     if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 27) return BFQ_ERR_TOO_LARGE;
+    // units are numbered in 32 bits, those of 64 keys at most
+    if (double(tiles_prefix) * (double(in->prefix_length) / kTallUnit + 1) * cache->heads +
+            double(tiles_seq) * in->batch * (double(int64_t(in->table_width) << p->cache.page_shift) / kTallUnit + 1) * cache->heads >= double(1 << 30))
+        return BFQ_ERR_TOO_LARGE;
     (p->prefix_tall ? p->tall : p->few).tiles_prefix = int(tiles_prefix), (p->seq_tall ? p->tall : p->few).tiles_seq = int(tiles_seq);
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;

@@ -116,28 +116,29 @@ struct Walk {
     __device__ __forceinline__ int pair(const AttendParams& p) const { return entry * p.cache.heads + head; }
 };
 
-// A CTA's run of units, found by all its threads together from the lengths.
+// A CTA's run of units, found by all its threads together from the lengths.  All numbers are below 2^31: the host has seen to that.
 struct Run {
-    long long from;  // the first one's number
-    long long per;   // units of every CTA but the last
-    int count;       // 0: none
+    int from;   // the first one's number
+    int per;    // units of every CTA but the last
+    int count;  // 0: none
 };
 template <int THREADS>
-__device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part, long long* scan, Walk* walk) {  // scan: shared, THREADS / 32 + 2
+__device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part, int* scan, Walk* walk) {  // scan: shared, THREADS / 32 + 2
     constexpr int kWarps = THREADS / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, entries = p.entries(part), heads = p.cache.heads;
     const int each = (entries + THREADS - 1) / THREADS;
     auto units_at = [&](int e) { return (tile_of(p, part, e).keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
-    long long mine = 0;
+    int mine = 0;
     for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_at(e);
-    long long before = mine, total = 0;
+    int before = mine, total = 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        const int v = __shfl_up_sync(0xFFFFFFFFu, before, o);
         if (lane >= o) before += v;
     }
     if (lane == 31) scan[warp] = before;
     __syncthreads();
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += scan[w];
         total += scan[w];
@@ -145,23 +146,23 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     before -= mine;
     total *= heads;
     Run run;
-    run.per = total > 0 ? (total + gridDim.x - 1) / gridDim.x : 1;
-    run.from = run.per * blockIdx.x;
-    const long long to = run.from + run.per < total ? run.from + run.per : total;
-    run.count = run.from < to ? static_cast<int>(to - run.from) : 0;
+    run.per = total > 0 ? (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x) : 1;
+    run.from = run.per * static_cast<int>(blockIdx.x);
+    run.count = run.from < total ? (run.per < total - run.from ? run.per : total - run.from) : 0;
     if (run.count == 0) return run;
     if (run.from >= before * heads && run.from < (before + mine) * heads) {  // one thread: the entry that holds `from` is one of its own
         int e = tid * each;
-        for (;; ++e) {
-            const int u = units_at(e);
-            if (run.from < (before + u) * heads) break;
-            before += u;
-        }
+        if (each > 1)
+            for (;; ++e) {
+                const int u = units_at(e);
+                if (run.from < (before + u) * heads) break;
+                before += u;
+            }
         scan[kWarps] = e, scan[kWarps + 1] = run.from - before * heads;
     }
     __syncthreads();
-    walk->enter(p, part, static_cast<int>(scan[kWarps]));
-    walk->head = static_cast<int>(scan[kWarps + 1] / walk->units), walk->unit = static_cast<int>(scan[kWarps + 1] % walk->units);
+    walk->enter(p, part, scan[kWarps]);
+    walk->head = scan[kWarps + 1] / walk->units, walk->unit = scan[kWarps + 1] - walk->head * walk->units;
     return run;
 }
 

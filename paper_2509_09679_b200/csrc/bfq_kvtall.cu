@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
     using M = TallSmem<D>;
     constexpr int kRow = D * BITS / 8;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ long long scan[kTallThreads / 32 + 2];
+    __shared__ int scan[kTallThreads / 32 + 2];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int dead;
     __shared__ float2 warp_top[2][kConvert / 32];  // of the keys' scales, the values'
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         // unit before the last are done, so that a wait for the last one's parity means that one; at a pair's end they may not be
         uint32_t s_phase = 0, done_phase = 0, o_phase = 0;
         bool active = false;
-        long long pair_from = run.from - walk.unit;
+        int pair_from = run.from - walk.unit;
         auto open = [&]() {
             const Tile& t = walk.tile;
             active = t.rows > 128 * tile;
@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;  // of a row
             const int first_row = 128 * tile + 32 * (warp & 3), part_of = lane % kLanes;
             const float sign = p.scale_log2 < 0.f ? -1.f : 1.f;
-            // four loads on their way at a time
-            constexpr int kLoads = 4;
+            // eight loads on their way at a time
+            constexpr int kLoads = 8;
 #pragma unroll 1
             for (int n0 = 0; n0 < 32; n0 += kLoads * kRowsAtOnce) {
                 uint4 v[kLoads];
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             limit = there ? (own < t.keys ? (own > 0 ? own : 0) : t.keys) : 0;
             least = __reduce_min_sync(0xFFFFFFFFu, there ? limit : 1 << 30);
         };
-        auto close = [&](long long done) {
+        auto close = [&](int done) {
             const int pair = walk.pair(p);
             if (active) {
                 wait_for(bar(kOFull + tile), o_phase, &dead, p.status);
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 tmem_fence_before();
                 if (there) part.sums[entry * kTallRows + r] = make_float2(m, l);
             }
-            if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, static_cast<int>((pair_from + walk.units - 1) / run.per - blockIdx.x + 1));
+            if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, (pair_from + walk.units - 1) / run.per - static_cast<int>(blockIdx.x) + 1);
             pair_from = done;
         };
         bool first = true;
