@@ -420,7 +420,8 @@ int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots,
  *               whole batch; every token sees all of them.  lengths and block_table do not count them.  prefix_length 0: none.
  * Probabilities (and, where more than 48 rows share their keys, the dequantized keys and values) are rounded to fp16, 2^-11 of each; all sums are fp32.
  * A row without keys (no length, or a token in front of its sequence's first key) is zero.  Rows of out and lse of tokens that no
- * sequence has stay as they were.  A page, length or number of tokens outside its range is reported by bfq_device_status
+ * sequence has stay as they were.  A row that sees a key whose scales are not finite may be NaN (bfq_kv_append
+ * writes no such scale), other rows are not.  A page, length, start or number of tokens outside its range is reported by bfq_device_status
  * (BFQ_ERR_INDEX) and the outputs of that call mean nothing; memory outside the arrays is not touched.  workspace: device,
  * 256-byte aligned, the caller's until the call's work on `stream` is done, at least bfq_kv_attend_workspace bytes (0 on
  * bad arguments; does not look at the data pointers' contents), BFQ_ERR_WORKSPACE otherwise.  Allocates nothing.

@@ -320,11 +320,17 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
                 for (int b = 0; b < NB; ++b) s[b][x >> 1][2 * (x & 1)] *= f, s[b][x >> 1][2 * (x & 1) + 1] *= f;
                 if (edge) {
                     const int key = key0 + 8 * x + g;
-                    u[x] = key < now.tile.keys ? u[x] : 0.f;
+                    // of a key that some rows do not see: a value's scale that is not finite (append_kv writes none) becomes a score of NaN for those
+                    // that do; where all rows see it, it makes NaN of their products below
+                    const bool fine = u[x] <= 65504.f;
+                    u[x] = fine && key < now.tile.keys ? u[x] : 0.f;
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) s[b][x >> 1][2 * (x & 1) + c] = key < limit[b][c] ? s[b][x >> 1][2 * (x & 1) + c] : -INFINITY;
+                        for (int c = 0; c < 2; ++c) {
+                            float& e = s[b][x >> 1][2 * (x & 1) + c];
+                            e = key < limit[b][c] ? (fine ? e : NAN) : -INFINITY;
+                        }
                 }
                 over |= u[x] > u_top;
 #pragma unroll
@@ -406,15 +412,12 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
     // The kernel before has let this one start after it had waited for all that came before itself: constants, lengths and starts can be read
     // while it still works.
     const int rows_all = static_cast<int>(p.tokens) * p.q.heads, row0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * each;
-    if (row0 >= rows_all) {
-        grid_dep_wait();
-        return;
-    }
     Turn<D, kE, true> turn;
     turn.load(p.tw, lane);
     bool waited = false;
     const int q_heads = p.q.heads, begin = first_token(p, 0), end = first_token(p, p.batch);
-    int of = -1, b = 0, place = 0;  // token that b and place are of
+    int of = -1, b = 0, place = 0, news = 0;  // token that b, its place in it, the sequence's tokens and tall are of
+    bool tall = false;
     for (int row = row0; row < row0 + each && row < rows_all; ++row) {
         const int token = row / q_heads, head = row - token * q_heads, h = head / p.group;
         if (token < begin || token >= end) continue;  // rows of no sequence stay as they are
@@ -429,6 +432,12 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
                 }
                 b = lo, place = token - first_token(p, b);
             }
+            news = first_token(p, b + 1) - first_token(p, b);
+            tall = p.seq_tall && news * p.group > kFewMost;
+        }
+        if (tall && p.join_tall) {  // k_join_tall has these
+            row += q_heads - 1 - head;
+            continue;
         }
         float m = -INFINITY, l = 0.f, o[kE];
 #pragma unroll
@@ -481,8 +490,8 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
             }
         };
         if (p.prefix_length > 0) join(p.prefix_tall != 0, -1, token * p.group + head % p.group);
-        if (place < p.max_new) join(p.seq_tall != 0, b, place * p.group + head % p.group);
-        else if (lane == 0) atomicExch(p.status, kBadIndex);  // more new tokens than the call was told
+        // rows that have no tile: of tokens beyond max_new, or of starts that fall
+        if (place < p.max_new && place < news) join(tall, b, place * p.group + head % p.group);
         const float f = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
         for (int e = 0; e < kE; ++e) o[e] *= f;
@@ -492,12 +501,10 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
         if constexpr (kE == 4) *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3]));
         else *reinterpret_cast<uint32_t*>(out) = bf16_pair(o[0], o[1]);
         if (p.lse != nullptr && lane == 0) p.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-        // a length or a start outside its range was taken as the nearest one inside
-        if (lane == 0 && head == 0 && place == 0) {
-            const int n = load_plain(p.lengths + b);
-            if (n != cached_keys(p, b)) atomicExch(p.status, kBadIndex);
-        }
     }
+    // from the last CTA on, which has no rows
+    for (int b = (gridDim.x - 1 - blockIdx.x) * blockDim.x + threadIdx.x; b < p.batch; b += gridDim.x * blockDim.x)
+        if (out_of_range(p, b)) atomicExch(p.status, kBadIndex);
     if (!waited) grid_dep_wait();
 }
 
@@ -544,8 +551,19 @@ static cudaError_t attend(const bfq_plan* plan, const AttendParams& p, int* ctas
                          : (p.cache.bits == 4 ? attend_rows<128, 4>(plan, p, ctas, grid, st) : attend_rows<128, 8>(plan, p, ctas, grid, st));
 }
 
-// Tiles of 256 rows where there are rows enough to pay for them.
-static bool use_tall(int64_t rows) { return rows > 48; }
+// Tiles of 256 rows where there are rows enough to pay for them.  The kernel for few rows against the one for many, us (4-bit cache, n = 128, 8 key
+// heads): 16 sequences of 4096 keys, 32 rows each 63 / 88, 48 rows 91 / 91, 64 rows 114 / 95, 256 rows 422 / 137; 64 of 2048 keys, 48 rows
+// 193 / 221, 64 rows 251 / 226.  One sequence of 2048 keys alone fills no more than the start of either: 64 rows 14 / 18, 256 rows 27 / 23.
+static bool use_tall(int64_t rows) { return rows > kFewMost; }
+// A prefix too, but where the sequences do not need that kernel's launch beside theirs only from five units of 16 rows and 128 keys to an SM on:
+// 8192 keys, 32 rows 28 / 30, 64 rows 48 / 31; 1024 keys, 64 rows 17 / 23, 128 rows (3.5 units) 23 / 25, 256 rows (7) 38 / 27.
+static bool prefix_use_tall(int64_t rows, bool seq_tall, int64_t keys, int heads, int sm_count) {
+    return use_tall(rows) && (seq_tall || ((rows + 15) / 16) * ((keys + kFewUnit - 1) / kFewUnit) * heads > 5 * sm_count);
+}
+// A row to a thread in the join where the rows fill the chip so; else a row to a warp, whose lanes have the results' weights at once.  Whole calls
+// with k_join_tall against k_join, us (as above): 16 sequences, 8192 rows of results 101 / 95, 16384 rows 118 / 114 (n = 64: 87 / 91), 32768 rows
+// 137 / 152; one sequence, 512 rows 46 / 18.
+constexpr int64_t kJoinTallRows = 16384;
 
 // The workspace: for each of the two kernels pairs, sums and parts.  Lays them out from `at` on (null: only counts); returns the bytes.
 static size_t lay_out(AttendParams* p, int n, int ctas_few, int ctas_tall, uint8_t* at) {
@@ -593,18 +611,24 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     p->q_starts = in->q_starts, p->prefix = in->prefix, p->prefix_pages = in->prefix_pages, p->prefix_length = cache->pages > 0 ? int(in->prefix_length) : 0;
     p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : in->max_new;
     const int64_t rows = (in->q_starts == nullptr ? in->batch : in->tokens) * int64_t(p->group), rows_seq = int64_t(p->max_new) * p->group;
-    p->prefix_tall = use_tall(rows), p->seq_tall = use_tall(rows_seq);
+    p->seq_tall = use_tall(rows_seq), p->prefix_tall = prefix_use_tall(rows, p->seq_tall, in->prefix_length, cache->heads, plan->sm_count);
+    p->join_tall = p->seq_tall && p->prefix_length == 0 && in->tokens * in->q.heads > kJoinTallRows;
     p->tall.rows = kTallRows, p->tall.unit_shift = 6, p->few.unit_shift = 7;
     static_assert(kTallUnit == 1 << 6 && kFewUnit == 1 << 7, "shifts");
-    p->few.rows = (p->seq_tall || rows_seq <= 8) && (in->prefix_length == 0 || p->prefix_tall || rows <= 8) ? 8 : 16;
-    const int tile_prefix = p->prefix_tall ? kTallRows : p->few.rows, tile_seq = p->seq_tall ? kTallRows : p->few.rows;
-    const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + tile_prefix - 1) / tile_prefix : 0, tiles_seq = (rows_seq + tile_seq - 1) / tile_seq;
+    // sequences of the kernel for few rows: all of them, or those up to kFewMost rows of a batch with larger ones, mostly single tokens
+    const int64_t rows_few = p->seq_tall ? kFewMost : rows_seq;
+    // a tile of 8 rows where they fit, against 16 (us, as above): 16 sequences of 4096 keys 30 / 37, 64 of 2048 keys 51 / 69, one 10.9 / 11.9
+    p->few.rows = (p->seq_tall ? p->group : rows_few) <= 8 && (in->prefix_length == 0 || p->prefix_tall || rows <= 8) ? 8 : 16;
+    p->few.seq_from = 1, p->few.seq_to = p->seq_tall ? kFewMost : INT32_MAX, p->tall.seq_from = kFewMost + 1, p->tall.seq_to = INT32_MAX;
+    Part& front = p->prefix_tall ? p->tall : p->few;
+    const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + front.rows - 1) / front.rows : 0, tiles_few = (rows_few + p->few.rows - 1) / p->few.rows,
+                  tiles_seq = (p->seq_tall ? (rows_seq + kTallRows - 1) / kTallRows : 0) + tiles_few;
     if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 27) return BFQ_ERR_TOO_LARGE;
     // units are numbered in 32 bits, those of 64 keys at most
     if (double(tiles_prefix) * (double(in->prefix_length) / kTallUnit + 1) * cache->heads +
             double(tiles_seq) * in->batch * (double(int64_t(in->table_width) << p->cache.page_shift) / kTallUnit + 1) * cache->heads >= double(1 << 30))
         return BFQ_ERR_TOO_LARGE;
-    (p->prefix_tall ? p->tall : p->few).tiles_prefix = int(tiles_prefix), (p->seq_tall ? p->tall : p->few).tiles_seq = int(tiles_seq);
+    front.tiles_prefix = int(tiles_prefix), p->few.tiles_seq = int(tiles_few), p->tall.tiles_seq = int(tiles_seq - tiles_few);
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;
     return BFQ_OK;
@@ -656,12 +680,11 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         p.beside_tall = tall > 0;
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
         if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, few, st);
-        if (e == cudaSuccess && p.seq_tall && p.prefix_length == 0) {
-            e = kv::join_tall_launch(plan, p, st);
-        } else if (e == cudaSuccess) {
+        if (e == cudaSuccess && p.join_tall) e = kv::join_tall_launch(plan, p, st);
+        if (e == cudaSuccess) {
             // a warp for each row where that is fewer than the chip runs at once; more would only load the butterfly's constants again
             const int64_t rows = p.tokens * p.q.heads, warps = int64_t(plan->sm_count) * 16, each = (rows + warps - 1) / warps;
-            const dim3 grid(unsigned((rows + 4 * each - 1) / (4 * each)));
+            const dim3 grid(unsigned((rows + 4 * each - 1) / (4 * each)) + 1);
             e = plan->n == 64 ? launch_overlapped(kv::k_join<64>, grid, dim3(128), 0, st, p, int(each)) : launch_overlapped(kv::k_join<128>, grid, dim3(128), 0, st, p, int(each));
         }
     }

@@ -6,8 +6,8 @@
 // What a CTA has of a pair is a partial result: per row the reference m, the sum l of exp2(s - m) and the sum of exp2(s - m) V.  It is
 // entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.
 //
-// Two kernels do this: one for few rows (tiles of 8 or 16 rows), one for many (256 rows).  A call gives the prefix's
-// tiles to one of them and the sequences' to the same one or the other; each has its own Part of the work.
+// Two kernels do this: one for few rows (tiles of 8 or 16 rows), one for many (256 rows); each has its own Part of the work.  A call gives the
+// prefix's tiles to one of them, and each sequence goes by its own rows, seen on the device: a batch may hold chunks of prompts beside single tokens.
 #pragma once
 #include "bfq_kv.cuh"
 #include "bfq_kvmma.cuh"
@@ -17,11 +17,13 @@ namespace kv {
 
 constexpr int kFewUnit = 128, kTallUnit = 64;  // keys
 constexpr int kTallRows = 256;
+constexpr int kFewMost = 48;  // rows that share their keys: more go to the kernel for many
 
 struct Part {
     int rows;                     // of a tile
     int unit_shift;               // keys of a unit: 1 << unit_shift
     int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
+    int seq_from, seq_to;         // rows of the sequences that are this part's
     int2* pairs;                  // [pairs] first CTA, CTAs
     float2* sums;                 // [entries][rows] m, l
     float* parts;                 // [entries][rows][D]
@@ -43,7 +45,8 @@ struct AttendParams {
     float scale_log2;  // softmax scale * log2 e
     const float2* tw;
     Part few, tall;
-    int prefix_tall, seq_tall;  // which of them has the prefix, the sequences
+    int prefix_tall, seq_tall;  // the kernel for many rows has the prefix; has sequences (those of more than kFewMost rows)
+    int join_tall;              // k_join_tall joins the sequences of the kernel for many rows
     int beside_tall;            // the kernel for few rows follows the one for many
     int* status;
     __host__ __device__ int entries(const Part& part) const { return part.tiles_prefix + batch * part.tiles_seq; }
@@ -57,6 +60,16 @@ __device__ __forceinline__ int first_token(const AttendParams& p, int b) {
 __device__ __forceinline__ int cached_keys(const AttendParams& p, int b) {
     const int n = load_plain(p.lengths + b), most = p.cache.pages > 0 ? p.table_width << p.cache.page_shift : 0;
     return n < 0 ? 0 : (n > most ? most : n);
+}
+// Starts that do not rise from 0 to the tokens, more new tokens than the call was told, a length outside its range: the kernels take the nearest one
+// inside, or rows are left out
+__device__ __forceinline__ bool out_of_range(const AttendParams& p, int b) {
+    if (p.q_starts != nullptr) {
+        const int64_t from = load_plain(p.q_starts + b), to = load_plain(p.q_starts + b + 1);
+        if (from < 0 || to < from || to > p.tokens || to - from > p.max_new) return true;
+        if (to == from) return false;  // its length does not matter
+    }
+    return load_plain(p.lengths + b) != cached_keys(p, b);
 }
 
 // One row tile: its rows and the keys that any of them has.
@@ -83,7 +96,7 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     const int b = (e - part.tiles_prefix) / part.tiles_seq, rt = (e - part.tiles_prefix) % part.tiles_seq;
     const int t0 = first_token(p, b), news = first_token(p, b + 1) - t0, n = cached_keys(p, b);
     t.row0 = rt * rows, t.token0 = t0;
-    const int left = news * p.group - t.row0;
+    const int all = news * p.group, left = all >= part.seq_from && all <= part.seq_to ? all - t.row0 : 0;
     t.rows = left < 0 ? 0 : (left < rows ? left : rows);
     t.last0 = n - news;
     const int need = t.rows > 0 ? t.last0 + (t.row0 + t.rows - 1) / p.group + 1 : 0;
@@ -92,13 +105,19 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     return t;
 }
 
+// the entry to look at after e: a sequence's tiles without rows are its last ones
+__device__ __forceinline__ int after(const Part& part, int e, const Tile& t) {
+    if (t.rows > 0 || e < part.tiles_prefix) return e + 1;
+    return part.tiles_prefix + ((e - part.tiles_prefix) / part.tiles_seq + 1) * part.tiles_seq;
+}
+
 // Where in the numbering of units a role of a CTA is.
 struct Walk {
     int entry, head, unit, units;  // unit of units within the pair
     Tile tile;
     __device__ __forceinline__ void enter(const AttendParams& p, const Part& part, int e) {  // the first entry from e on that has units
         const int last = p.entries(part);
-        for (entry = e, units = 0; entry < last; ++entry) {
+        for (entry = e, units = 0; entry < last; entry = after(part, entry, tile)) {
             tile = tile_of(p, part, entry);
             units = (tile.keys + (1 << part.unit_shift) - 1) >> part.unit_shift;
             if (units > 0) break;
@@ -127,9 +146,12 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     constexpr int kWarps = THREADS / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, entries = p.entries(part), heads = p.cache.heads;
     const int each = (entries + THREADS - 1) / THREADS;
-    auto units_at = [&](int e) { return (tile_of(p, part, e).keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
+    auto units_of = [&](const Tile& t) { return (t.keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
     int mine = 0;
-    for (int e = tid * each; e < entries && e < (tid + 1) * each; ++e) mine += units_at(e);
+    for (int e = tid * each; e < entries && e < (tid + 1) * each;) {
+        const Tile t = tile_of(p, part, e);
+        mine += units_of(t), e = after(part, e, t);
+    }
     int before = mine, total = 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -153,10 +175,11 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     if (run.from >= before * heads && run.from < (before + mine) * heads) {  // one thread: the entry that holds `from` is one of its own
         int e = tid * each;
         if (each > 1)
-            for (;; ++e) {
-                const int u = units_at(e);
+            for (;;) {
+                const Tile t = tile_of(p, part, e);
+                const int u = units_of(t);
                 if (run.from < (before + u) * heads) break;
-                before += u;
+                before += u, e = after(part, e, t);
             }
         scan[kWarps] = e, scan[kWarps + 1] = run.from - before * heads;
     }

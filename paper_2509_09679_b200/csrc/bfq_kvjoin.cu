@@ -13,7 +13,7 @@ constexpr int kJoinWarps = 4;
 template <int D>
 struct JoinSmem {
     static constexpr int kIn = 4 * D, kInPitch = kIn + 16, kOut = 2 * D, kOutPitch = kOut + 16;
-    static constexpr uint32_t kProducts = RowTurn<D, true>::kBytes, kWarps = kProducts + D * 4, kWarp = 32 * kInPitch;  // rows out: in the place of rows in
+    static constexpr uint32_t kProducts = RowTurn<D>::kBytes, kWarps = kProducts + D * 4, kWarp = 32 * kInPitch;  // rows out: in the place of rows in
     static constexpr uint32_t kBytes = kWarps + kJoinWarps * kWarp;
 };
 
@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall
     const int lane = threadIdx.x & 31, heads = p.cache.heads;
     const uint32_t table = smem_u32(smem), rows_at = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp;
     const Part& part = p.tall;
-    const bool scaled = RowTurn<D, true>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
+    const bool scaled = RowTurn<D>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
     const int chunks = part.tiles_seq * p.batch * heads * (kTallRows / 32);
     int of = -1;
     Tile tile{};
@@ -61,8 +61,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall
 #pragma unroll
         for (int i = 0; i < D / 2; ++i) x[i] = mul2(x[i], f2);
         // an average of cached rows: at most 128 x 65504, which the scaled form leaves finite
-        if (scaled) RowTurn<D, true>::scaled(x, table);
-        else RowTurn<D, true>::plain(x, p.tw);
+        if (scaled) RowTurn<D>::scaled(x, table);
+        else RowTurn<D>::plain(x, p.tw);
         const int row = tile.row0 + r, token = tile.token0 + row / p.group, q_head = head * p.group + row % p.group;
         store_bf16<D>(rows_at + lane * S::kOutPitch, x);
         __syncwarp();
@@ -71,9 +71,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall
         if (p.lse != nullptr && there) p.lse[static_cast<int64_t>(token) * p.q.heads + q_head] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         __syncwarp();
     }
-    // a length outside its range was taken as the nearest one inside; tokens beyond max_new have no tile
-    for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < p.batch; b += gridDim.x * blockDim.x)
-        if (load_plain(p.lengths + b) != cached_keys(p, b) || first_token(p, b + 1) - first_token(p, b) > p.max_new) atomicExch(p.status, kBadIndex);
 }
 
 template <int D>

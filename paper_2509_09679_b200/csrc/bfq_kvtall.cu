@@ -344,6 +344,10 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
         auto step = [&](int i, Raw& raw) {
             const int s = i & 3;
             float2 most = make_float2(0.f, 0.f);
+            // a scale that is not finite (append_kv writes none): a key of NaN, for the rows that see it
+#pragma unroll
+            for (int c = 0; c < kTurns; ++c)
+                if ((raw.k_scale[c] & 0x7C00) == 0x7C00 || (raw.v_scale[c] & 0x7C00) == 0x7C00) raw.k_scale[c] = 0x7FFF, raw.v_scale[c] = 0;
 #pragma unroll
             for (int c = 0; c < kTurns; ++c) most.x = fmaxf(most.x, half_value(raw.k_scale[c])), most.y = fmaxf(most.y, half_value(raw.v_scale[c]));
             most.x = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most.x)));  // not negative: ordered as integers

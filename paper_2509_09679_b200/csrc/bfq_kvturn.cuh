@@ -1,5 +1,4 @@
-// A row of a head in the registers of one thread: the butterfly on it, and the way of a warp's 32 rows in and out through shared memory.
-// See bfq_kvrows.cu for the scaled form of the stages.
+// A row of a head in the registers of one thread: the inverse butterfly on it, and the way of a warp's 32 rows in and out through shared memory.
 #pragma once
 #include "bfq_kv.cuh"
 
@@ -19,10 +18,14 @@ __device__ __forceinline__ void copy_in(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// The butterfly on a row in a thread's registers, elements 2 r and 2 r + 1 in register r.  Table in shared memory, 16 bytes an entry: stage 0:
-// (a, b) of registers 2 k and 2 k + 1, with lo <- lo + a hi, hi <- hi + b lo; the other stages: (a, a', b, b') of the k-th pair of registers;
-// then P, four elements an entry.
-template <int D, bool BACK>
+// Q^T on a row in a thread's registers, elements 2 r and 2 r + 1 in register r.  A stage's lo <- c lo + s hi, hi <- c hi - s lo is four
+// operations a pair.  With each element kept as x / p, p the product of the cosines that it has met, it is two: lo' <- lo' + a hi',
+// hi' <- hi' + b lo' with a = (s / c) (q / p), b = -(s / c) (p / q) for the factors p of lo and q of hi before the stage, and one
+// multiplication by P, the products of all stages, at the end.  Every rounding is relative to what the plain stage would have there times 1 / p, so that the
+// error is the same; the form is taken while all |P| >= 2^-40, which no row of the cache can bring past fp32's range.
+// Table in shared memory, 16 bytes an entry: stage 0: (a, b) of registers 2 k and 2 k + 1; the other stages: (a, a', b, b') of the k-th pair of
+// registers; then P, four elements an entry.
+template <int D>
 struct RowTurn {
     static constexpr int kStages = D == 64 ? 6 : 7, kPerStage = D / 4;
     static constexpr uint32_t kBytes = 16 * (kStages * kPerStage + D / 4);
@@ -33,11 +36,11 @@ struct RowTurn {
         for (int i = threadIdx.x; i < D; i += blockDim.x) products[i] = 1.f;
         __syncthreads();
         for (int n = 0; n < kStages; ++n) {
-            const int st = BACK ? kStages - 1 - n : n;
+            const int st = kStages - 1 - n;
             for (int j = threadIdx.x; j < D / 2; j += blockDim.x) {
                 const float2 t = load_plain(tw + st * (D / 2) + j);
                 const int lo = ((j >> st) << (st + 1)) | (j & ((1 << st) - 1)), hi = lo + (1 << st);
-                const float tangent = (BACK ? -t.y : t.y) / t.x, p = products[lo], q = products[hi], a = -tangent * (q / p), b = tangent * (p / q);
+                const float tangent = -t.y / t.x, p = products[lo], q = products[hi], a = -tangent * (q / p), b = tangent * (p / q);
                 if (st == 0) {
                     table[2 * j] = a, table[2 * j + 1] = b;
                 } else {  // pair j is half j & 1 of the registers' pair j / 2
@@ -58,7 +61,7 @@ struct RowTurn {
     __device__ __forceinline__ static void scaled(u64 (&x)[D / 2], uint32_t table) {
 #pragma unroll
         for (int n = 0; n < kStages; ++n) {
-            const int st = BACK ? kStages - 1 - n : n;
+            const int st = kStages - 1 - n;
             if (st == 0) {
 #pragma unroll
                 for (int k = 0; k < D / 4; ++k) {
@@ -89,14 +92,14 @@ struct RowTurn {
     __device__ __forceinline__ static void plain(u64 (&x)[D / 2], const float2* tw) {
 #pragma unroll
         for (int n = 0; n < kStages; ++n) {
-            const int st = BACK ? kStages - 1 - n : n;
+            const int st = kStages - 1 - n;
 #pragma unroll
             for (int j = 0; j < D / 2; ++j) {
                 const float2 t = load_plain(tw + st * (D / 2) + j);
                 const int lo = ((j >> st) << (st + 1)) | (j & ((1 << st) - 1)), hi = lo + (1 << st);
                 float v[2], w[2];
                 unpack2(x[lo / 2], v[0], v[1]), unpack2(x[hi / 2], w[0], w[1]);
-                const float s = BACK ? -t.y : t.y, a = v[lo & 1], b = st == 0 ? v[1] : w[hi & 1];
+                const float s = -t.y, a = v[lo & 1], b = st == 0 ? v[1] : w[hi & 1];
                 const float na = fmaf(t.x, a, -s * b), nb = fmaf(s, a, t.x * b);
                 if (st == 0) {
                     x[lo / 2] = pack2(na, nb);

@@ -370,7 +370,7 @@ def test_attend_shared_prefix(n, bits, page, hq, hkv, prefix_length, news, lengt
 
 @gpu
 @pytest.mark.parametrize("n,bits", [(128, 4), (64, 8), (128, 8), (64, 4)])
-@pytest.mark.parametrize("news,lengths,prefix_length", [([1] * 7, [9, 0, 70, 1, 33, 5, 200], 16384), ([40, 3, 60], [40, 90, 2000], 9000), ([300], [9000], 0)])
+@pytest.mark.parametrize("news,lengths,prefix_length", [([1] * 7, [9, 0, 70, 1, 33, 5, 200], 16384), ([40, 3, 60], [40, 90, 2000], 9000), ([300], [9000], 0), ([1, 500, 1, 24, 25, 0, 1], [3000, 4000, 1, 700, 25, 9, 77], 0)])
 def test_attend_many_units(n, bits, news, lengths, prefix_length):
     """Runs of units that go many times through every ring and buffer of the kernels."""
     page, hkv, hq = 64, 8, 56
@@ -662,3 +662,131 @@ def test_what_the_c_entries_refuse():
     with pytest.raises(ValueError):
         small.attend_kv(cache, q, i32([[0]]), i32([1]))
     assert p.attend_kv(cache, q[:0], i32(np.zeros((0, 1))), i32([])).shape == (0, 1, 64)
+
+
+# ---- calls that batches, callers and graphs come to ------------------------------------------------------------------------------
+MIXED = [([1, 500, 0, 24, 25, 1, 7], [3000, 900, 5, 700, 25, 0, 77], 64), ([5, 20, 13], [5, 100, 12], 8), ([1, 13], [0, 0], 4)]
+
+
+def ragged(n, page, news, lengths, hq, hkv, bits=4, seed=101):
+    table, _, pages = tables(lengths, page, 2, seed)
+    cache, values = make_cache(pages, hkv, n, page, bits, seed + 1)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = (2 * torch.randn((starts[-1], hq, n), generator=torch.Generator().manual_seed(seed + 2))).to(torch.bfloat16)
+    return cache, values, table, starts, q
+
+
+@gpu
+@pytest.mark.parametrize("n", [64, 128])
+@pytest.mark.parametrize("angles", ["uniform", "right"])
+@pytest.mark.parametrize("news,lengths,hq", MIXED)
+def test_a_batch_of_chunks_and_single_tokens(n, angles, news, lengths, hq):
+    """Sequences on both sides of the rows from which they go to the tiles of 256, results in a wider tensor, tokens behind the last."""
+    page, hkv = 32, 2
+    p, theta = make_plan(n, "uniform", 9)
+    if angles == "right":  # cosines of nothing: no form with their quotients
+        theta[::2] = np.float32(np.pi / 2)
+        p.set_angles(torch.from_numpy(theta.astype(np.float32)).to(DEV))
+        theta = theta.astype(np.float32).astype(np.float64)
+    cache, (k, v), table, starts, q = ragged(n, page, news, lengths, hq, hkv)
+    q = torch.cat([q, torch.full((3, hq, n), float("nan"), dtype=torch.bfloat16)])
+    wide = torch.full((q.shape[0], hq + 1, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), out=wide[:, :hq], want_lse=True)
+    assert p.device_status() == 0 and (wide[:, hq] == 7).all() and (wide[starts[-1]:] == 7).all()
+    rows = np.unique(np.concatenate([starts[:-1], starts[1:] - 1, np.linspace(0, starts[-1] - 1, 9).astype(int)]))
+    rows = rows[rows >= 0]
+    first = np.searchsorted(starts, rows, side="right") - 1
+    for t, b in zip(rows, first):
+        own = max(0, lengths[b] - (starts[b + 1] - 1 - t))
+        ref, ref_lse, bound, lse_bound = attention(to_f64(q[t:t + 1]), theta, k, v, table[b:b + 1], [own], [0, 1], page, n ** -0.5)
+        scores = 2.0 ** -11 * n ** -0.5 * np.linalg.norm(to_f64(q[t]), axis=-1).max() * max(np.linalg.norm(x, axis=-1).max() for x in k)  # keys rounded to fp16
+        check_attention(out[t:t + 1], lse[t:t + 1], (ref, ref_lse, bound + 2 * scores * np.abs(v).max(), lse_bound + scores))
+
+
+@gpu
+@pytest.mark.parametrize("n,bits,group", [(128, 4, 4), (64, 8, 16), (128, 8, 128)])
+@pytest.mark.parametrize("news", [[1, 1, 1], [3, 1, 2], [40, 1, 33]])
+def test_what_a_row_does_not_see_leaves_it_alone(n, bits, group, news):
+    """NaN and infinities: in scales behind a sequence's keys and in keys of later tokens, in page numbers behind its pages, in other rows of q."""
+    page, lengths = 16, [40, 17, 90]
+    p, _ = make_plan(n)
+    cache, _, table, starts, q = ragged(n, page, news, lengths, group, 1, bits)
+    q, some = q.to(DEV), dict(q_starts=i32(starts), max_new=max(news), want_lse=True)
+    good, good_lse = p.attend_kv(cache, q, i32(table), i32(lengths), **some)
+    bad_table = table.copy()
+    for b, m in enumerate(lengths):
+        for scales, worst in ((cache.k_scales, float("nan")), (cache.v_scales, float("inf"))):
+            for key in range(m, table.shape[1] * page):
+                scales[table[b][key // page], :, key % page] = worst
+        bad_table[b, -(-m // page):] = 1 << 30
+    out, lse = p.attend_kv(cache, q, i32(bad_table), i32(lengths), **some)
+    assert torch.equal(out, good) and torch.equal(lse, good_lse) and p.device_status() == 0
+    # one head of a token
+    token = int(starts[1]) - 1
+    for value in (float("nan"), float("inf")):
+        strange = q.clone()
+        strange[token, group // 2, 5] = value
+        out, lse = p.attend_kv(cache, strange, i32(table), i32(lengths), **some)
+        same = torch.ones_like(lse, dtype=torch.bool)
+        same[token, group // 2] = False
+        assert torch.equal(out[same], good[same]) and torch.equal(lse[same], good_lse[same]) and out[token, group // 2].isnan().all()
+    # the last key of a sequence: only its last token sees it
+    for scales, value in ((cache.v_scales, float("inf")), (cache.v_scales, float("nan")), (cache.k_scales, float("nan"))):
+        at = (table[0][(lengths[0] - 1) // page], slice(None), (lengths[0] - 1) % page)
+        kept = scales[at].clone()
+        scales[at] = value
+        out, lse = p.attend_kv(cache, q, i32(table), i32(lengths), **some)
+        scales[at] = kept
+        assert out[token].isnan().all()
+        # the others: the same keys and values, but powers of two that do not follow this key's scales
+        rest = torch.arange(len(q), device=DEV) != token
+        assert out[rest].isfinite().all()
+        assert (out[rest].double() - good[rest].double()).abs().max() <= 2.0 ** -6 * good.double().abs().max()
+
+
+@gpu
+def test_starts_that_fall_are_reported():
+    n, page = 64, 16
+    p, _ = make_plan(n)
+    cache, _, table, starts, q = ragged(n, page, [40, 30, 50], [40, 90, 60], 8, 2)
+    q, t, lens = q.to(DEV), i32(table), i32([40, 90, 60])
+    good = p.attend_kv(cache, q, t, lens, q_starts=i32(starts), max_new=50)
+    assert p.device_status() == 0
+    for bad in ([0, 70, 40, 120], [0, 1, 0, 120], [-5, 40, 70, 120], [0, 40, 70, 121], [120, 70, 40, 0], [0, 0, 119, 120], [0, 1 << 30, -1 << 30, 120]):
+        for prefix_length in (0, 20):
+            p.attend_kv(cache, q, t, lens, q_starts=i32(bad), max_new=50, prefix=i32([0, 1]), prefix_length=prefix_length)
+            assert p.device_status() == -11, bad
+    assert torch.equal(p.attend_kv(cache, q, t, lens, q_starts=i32(starts), max_new=50), good) and p.device_status() == 0
+
+
+@gpu
+def test_starts_that_change_between_replays():
+    """A captured call whose sequences change sides of the rows from which the tiles of 256 have them; two plans' calls at once."""
+    n, page, hq = 128, 32, 8
+    lengths = [200, 150, 90, 300]
+    p, _ = make_plan(n)
+    cache, _, table, starts, q = ragged(n, page, [60, 1, 3, 56], lengths, hq, 2)
+    q, t, lens, at = q.to(DEV), i32(table), i32(lengths), i32(starts)
+    call = lambda plan: plan.attend_kv(cache, q, t, lens, q_starts=at, max_new=100)
+    call(p)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call(p)
+    for news in ([60, 1, 3, 56], [1, 1, 18, 100], [12, 13, 12, 13], [0, 100, 0, 20]):
+        at.copy_(i32(np.concatenate([[0], np.cumsum(news)])))
+        graph.replay()
+        torch.cuda.synchronize()
+        used = sum(news)
+        assert torch.equal(out[:used], call(p)[:used]) and out[:used].isfinite().all() and p.device_status() == 0
+    other, _ = make_plan(n)
+    want = call(p)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(10):
+        for plan, stream in zip((p, other), streams):
+            with torch.cuda.stream(stream):
+                outs.append(call(plan))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[:120], want[:120]) for o in outs) and p.device_status() == 0 and other.device_status() == 0
