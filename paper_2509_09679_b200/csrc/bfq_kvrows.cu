@@ -498,6 +498,9 @@ __global__ void __launch_bounds__(kRowsThreads, ReadSmem<D, F32, BITS>::kCtas) k
     if (warp == 0) tensor_memory_free<4 * D>(tmem_at);
 }
 
+// Rows of a call: below what a whole tile more for each group can bring past 31 bits.
+constexpr int64_t kMostRows = (int64_t(1) << 31) - 128 * (kGroups + 1);
+
 // as many CTAs as their shared memory lets run at once
 template <class S, class Kernel, class Params>
 static cudaError_t launch_rows(const bfq_plan* plan, Kernel kern, bool* ready, int64_t rows, const Params& p, cudaStream_t st) {
@@ -555,7 +558,7 @@ extern "C" int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const in
     if (rc == BFQ_OK && q != nullptr) rc = kv::check_heads(q, n, esize, &p.q);
     if (rc == BFQ_OK && q != nullptr) rc = kv::check_heads(q_out, n, 2, &p.q_out);
     if (rc != BFQ_OK) return rc;
-    if (tokens * (p.q.heads + 2 * int64_t(cache->heads)) >= (int64_t(1) << 31) - 64) return BFQ_ERR_STRIDE;
+    if (tokens * (p.q.heads + 2 * int64_t(cache->heads)) > kv::kMostRows) return BFQ_ERR_STRIDE;
     if (k->heads != cache->heads || v->heads != cache->heads || (q != nullptr && q_out->heads != q->heads)) return BFQ_ERR_STRIDE;
     if ((reinterpret_cast<uintptr_t>(slots) & 7u) != 0) return BFQ_ERR_ALIGN;
     if (at != nullptr) {
@@ -584,7 +587,7 @@ extern "C" int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int6
     const int rc = kv::check_cache(plan, cache, &p.cache);
     if (rc != BFQ_OK) return rc;
     if (t != BFQ_F32 && t != BFQ_BF16) return BFQ_ERR_DTYPE;
-    if (tokens < 0 || tokens >= int64_t(1) << 31 || tokens * cache->heads >= int64_t(1) << 30) return BFQ_ERR_STRIDE;
+    if (tokens < 0 || tokens >= int64_t(1) << 31 || tokens * 2 * cache->heads > kv::kMostRows) return BFQ_ERR_STRIDE;
     if (tokens == 0) return BFQ_OK;
     if (slots == nullptr || k == nullptr || v == nullptr) return BFQ_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(slots) & 7u) != 0 || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) != 0) return BFQ_ERR_ALIGN;

@@ -790,3 +790,17 @@ def test_starts_that_change_between_replays():
                 outs.append(call(plan))
     torch.cuda.synchronize()
     assert all(torch.equal(o[:120], want[:120]) for o in outs) and p.device_status() == 0 and other.device_status() == 0
+
+
+@gpu
+def test_more_rows_than_can_be_numbered_are_refused():
+    """Counts at which rows, rounded up to whole tiles, would pass 31 bits: refused before anything is read."""
+    p, _ = make_plan(64)
+    cache, _ = make_cache(1, 1, 64, 16, 4, 1)
+    x = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device=DEV)
+    slots = torch.full((1,), -1, dtype=torch.int64, device=DEV)
+    c, rows, L, ref = p._cache(cache), p._head_rows(x, 1, 1, None, "x"), binding.lib(), binding.ctypes.byref
+    for tokens in (2 ** 30 - 1, 2 ** 30 - 100, 2 ** 30, 2 ** 31 - 1, 2 ** 31, 2 ** 62, -1):  # two rows to a token
+        assert L.bfq_kv_read(p._h, c, slots.data_ptr(), tokens, 1, x.data_ptr(), x.data_ptr(), None) == -5
+        assert L.bfq_kv_append(p._h, c, slots.data_ptr(), tokens, 1, ref(rows), ref(rows), None, None, None, None) == -5
+    assert p.device_status() == 0
