@@ -445,8 +445,9 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
         auto join = [&](bool tall, int b, int row) {  // b < 0: the prefix
             const Part& part = tall ? p.tall : p.few;
             const int rows = part.rows, r = row % rows, entry = (b < 0 ? 0 : part.tiles_prefix + b * part.tiles_seq) + row / rows;
-            const int pair = entry * p.cache.heads + h;
-            if (tile_of(p, part, entry).keys == 0) return;
+            const Tile tile = tile_of(p, part, entry);
+            const int pair = tile.place * p.cache.heads + h;
+            if (tile.keys == 0) return;
             if (!waited) grid_dep_wait(), waited = true;
             const int2 found = load_plain(part.pairs + pair);
             const int64_t first = static_cast<int64_t>(found.x) + pair;
@@ -575,7 +576,7 @@ static size_t lay_out(AttendParams* p, int n, int ctas_few, int ctas_tall, uint8
     };
     for (const bool tall : {false, true}) {
         Part& part = tall ? p->tall : p->few;
-        const size_t pairs = size_t(p->entries(part)) * p->cache.heads, rows = (pairs + (tall ? ctas_tall : ctas_few)) * part.rows;
+        const size_t pairs = size_t(p->places(part)) * p->cache.heads, rows = (pairs + (tall ? ctas_tall : ctas_few)) * part.rows;
         if (pairs == 0) continue;
         part.pairs = reinterpret_cast<int2*>(take(pairs * sizeof(int2)));
         part.sums = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
@@ -629,6 +630,11 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
             double(tiles_seq) * in->batch * (double(int64_t(in->table_width) << p->cache.page_shift) / kTallUnit + 1) * cache->heads >= double(1 << 30))
         return BFQ_ERR_TOO_LARGE;
     front.tiles_prefix = int(tiles_prefix), p->few.tiles_seq = int(tiles_few), p->tall.tiles_seq = int(tiles_seq - tiles_few);
+    for (Part* part : {&p->few, &p->tall}) {
+        part->rows_shift = part->rows == 8 ? 3 : (part->rows == 16 ? 4 : 8);
+        part->by_tokens = in->q_starts != nullptr && part->tiles_seq > 0 && p->places_by_tokens(*part) < p->entries(*part);
+    }
+    static_assert(kTallRows == 1 << 8, "shift");
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;
     return BFQ_OK;

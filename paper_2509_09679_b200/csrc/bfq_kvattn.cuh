@@ -4,7 +4,9 @@
 // outermost.  Row tiles of the shared prefix come first (their rows are those of all tokens), then those of each sequence.  A pair's
 // keys are cut into units; units are numbered pair by pair and every CTA takes an equal run of them, wherever sequences end.
 // What a CTA has of a pair is a partial result: per row the reference m, the sum l of exp2(s - m) and the sum of exp2(s - m) V.  It is
-// entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.
+// entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.  Pairs have their numbers there
+// from the places of their tiles: row tiles counted for each sequence alike, or, where most sequences have far fewer tokens than the most that
+// one may have, by the tokens in front of them, (first row of the sequence) / rows + sequence + tile, which rises from tile to tile too.
 //
 // Two kernels do this: one for few rows (tiles of 8 or 16 rows), one for many (256 rows); each has its own Part of the work.  A call gives the
 // prefix's tiles to one of them, and each sequence goes by its own rows, seen on the device: a batch may hold chunks of prompts beside single tokens.
@@ -20,10 +22,11 @@ constexpr int kTallRows = 256;
 constexpr int kFewMost = 48;  // rows that share their keys: more go to the kernel for many
 
 struct Part {
-    int rows;                     // of a tile
+    int rows, rows_shift;         // of a tile, 1 << rows_shift
     int unit_shift;               // keys of a unit: 1 << unit_shift
     int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
     int seq_from, seq_to;         // rows of the sequences that are this part's
+    int by_tokens;                // how tiles are placed in the workspace
     int2* pairs;                  // [pairs] first CTA, CTAs
     float2* sums;                 // [entries][rows] m, l
     float* parts;                 // [entries][rows][D]
@@ -50,6 +53,8 @@ struct AttendParams {
     int beside_tall;            // the kernel for few rows follows the one for many
     int* status;
     __host__ __device__ int entries(const Part& part) const { return part.tiles_prefix + batch * part.tiles_seq; }
+    int64_t places_by_tokens(const Part& part) const { return part.tiles_prefix + (tokens * group >> part.rows_shift) + batch; }
+    int64_t places(const Part& part) const { return part.by_tokens ? places_by_tokens(part) : entries(part); }
 };
 
 __device__ __forceinline__ int first_token(const AttendParams& p, int b) {
@@ -74,6 +79,7 @@ __device__ __forceinline__ bool out_of_range(const AttendParams& p, int b) {
 
 // One row tile: its rows and the keys that any of them has.
 struct Tile {
+    int place;           // in the workspace
     int row0, rows;      // of the sequence's rows (prefix: of all rows)
     int token0;          // token of the sequence's row 0
     int keys;            // keys 0 .. keys - 1
@@ -85,7 +91,7 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     const int rows = part.rows;
     if (e < part.tiles_prefix) {
         const int tokens = first_token(p, p.batch);
-        t.row0 = e * rows, t.token0 = 0;
+        t.place = e, t.row0 = e * rows, t.token0 = 0;
         const int left = tokens * p.group - t.row0;
         t.rows = left < 0 ? 0 : (left < rows ? left : rows);
         t.keys = t.rows > 0 ? p.prefix_length : 0;
@@ -95,6 +101,7 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     }
     const int b = (e - part.tiles_prefix) / part.tiles_seq, rt = (e - part.tiles_prefix) % part.tiles_seq;
     const int t0 = first_token(p, b), news = first_token(p, b + 1) - t0, n = cached_keys(p, b);
+    t.place = part.by_tokens ? part.tiles_prefix + (t0 * p.group >> part.rows_shift) + b + rt : e;
     t.row0 = rt * rows, t.token0 = t0;
     const int all = news * p.group, left = all >= part.seq_from && all <= part.seq_to ? all - t.row0 : 0;
     t.rows = left < 0 ? 0 : (left < rows ? left : rows);
@@ -132,7 +139,7 @@ struct Walk {
     __device__ __forceinline__ void next(const AttendParams& p, const Part& part) {
         if (++unit == units) next_pair(p, part);
     }
-    __device__ __forceinline__ int pair(const AttendParams& p) const { return entry * p.cache.heads + head; }
+    __device__ __forceinline__ int pair(const AttendParams& p) const { return tile.place * p.cache.heads + head; }
 };
 
 // A CTA's run of units, found by all its threads together from the lengths.  All numbers are below 2^31: the host has seen to that.

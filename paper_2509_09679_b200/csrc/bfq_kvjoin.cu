@@ -30,10 +30,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall
     int of = -1;
     Tile tile{};
     for (int c = blockIdx.x * kJoinWarps + (threadIdx.x >> 5); c < chunks; c += gridDim.x * kJoinWarps) {
-        const int pair = c / (kTallRows / 32), entry = pair / heads, head = pair - entry * heads, r = c % (kTallRows / 32) * 32 + lane;
+        const int numbered = c / (kTallRows / 32), entry = numbered / heads, head = numbered - entry * heads, r = c % (kTallRows / 32) * 32 + lane;
         if (entry != of) tile = tile_of(p, part, entry), of = entry;
         if (r - lane >= tile.rows) continue;
         const bool there = r < tile.rows;
+        const int pair = tile.place * heads + head;
         const int2 ctas = tile.keys > 0 ? load_plain(part.pairs + pair) : make_int2(0, 0);
         const int64_t first = (static_cast<int64_t>(ctas.x) + pair) * kTallRows + r;
         u64 x[D / 2];

@@ -804,3 +804,30 @@ def test_more_rows_than_can_be_numbered_are_refused():
         assert L.bfq_kv_read(p._h, c, slots.data_ptr(), tokens, 1, x.data_ptr(), x.data_ptr(), None) == -5
         assert L.bfq_kv_append(p._h, c, slots.data_ptr(), tokens, 1, ref(rows), ref(rows), None, None, None, None) == -5
     assert p.device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("prefix_length", [0, 600])
+def test_the_workspace_follows_the_tokens(prefix_length):
+    """A captured call told of many new tokens for every sequence of a large batch, of which most have one."""
+    n, page, hq, hkv, batch = 64, 16, 16, 2, 64
+    p, _ = make_plan(n)
+    news = [1] * 20 + [0, 700] + [1] * 20 + [50, 2, 6, 7] + [1] * 18
+    lengths = [max(1, (37 * b) % 90) + m for b, m in enumerate(news)]
+    cache, _, table, starts, q = ragged(n, page, news, lengths, hq, hkv)
+    q, t, lens, at = q.to(DEV), i32(table), i32(lengths), i32(starts)
+    some = dict(prefix=i32(range(-(-prefix_length // page))), prefix_length=prefix_length) if prefix_length else {}
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    out = p.attend_kv(cache, q, t, lens, q_starts=at, max_new=800, **some)
+    # a partial result has n + 2 floats; rows: tiles of 256 for the tokens (of prefix and sequences), one more for each sequence and each CTA of the kernel for
+    # many rows; up to 48, in tiles of 8, for each sequence and a tile for each of four CTAs to an SM of the one for few
+    sms, group = torch.cuda.get_device_properties(0).multi_processor_count, hq // hkv
+    rows = 256 * (hkv * (2 * (len(q) * group // 256 + 1) + batch) + sms) + 48 * hkv * batch + 8 * 4 * sms
+    assert torch.cuda.max_memory_allocated() - before < 4 * (n + 2) * rows + 2 * q.numel() + (1 << 20)
+    assert p.device_status() == 0
+    for b in (0, 19, 21, 22, 42, 43, 44, 45, 46, 63):  # each sequence alone gives the same, up to the roundings of other tiles
+        rows = slice(int(starts[b]), int(starts[b + 1]))
+        alone = p.attend_kv(cache, q[rows].contiguous(), t[b:b + 1], lens[b:b + 1], q_starts=i32([0, news[b]]), max_new=news[b], **some)
+        assert (out[rows].double() - alone.double()).abs().max() <= 2.0 ** -6 * alone.double().abs().max(), b
