@@ -148,10 +148,15 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 const int r = 128 * tile + row_of_tile;
                 const bool there = r < walk.tile.rows;
                 const long long entry = static_cast<long long>(blockIdx.x) + pair;
-                // half of 32 rows at a time through the warp's part of the query tile, which no product reads any more, so that rows are written
-                // whole: 16 bytes at place (chunk ^ row) of a row's half
-                constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
-                const uint32_t own = base + M::kQ + tile * M::kTile + (warp & 3) * (M::kTile / 4);
+                // half of 32 rows at a time through the places of the warp's own query rows, which no product reads any more, so that rows are written
+                // whole: 16 bytes at place (chunk ^ row) of a row's half.  Those places are, as open writes them, 4096 bytes at 4096 (warp & 3) of
+                // each half of D: one block of 32 rows at 64 elements, two blocks of 16 rows 16384 apart at 128.  Other warps may still
+                // be here, or write their rows of the next pair already: nothing orders the four of a tile between close and open.
+                constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kBlockRows = 4096 / (2 * D);
+                const uint32_t own = base + M::kQ + tile * M::kTile + (warp & 3) * 4096;
+                auto staged = [&](int row, int chunk) {
+                    return own + (row / kBlockRows) * 16384 + (row % kBlockRows) * 2 * D + ((chunk ^ (row & (kLanes - 1))) << 4);
+                };
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -166,8 +171,8 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                             for (int i = 0; i < 8; ++i) x[order<BITS>(i)] = __uint_as_float(v[8 * q + i]) * unit;
 #pragma unroll
                             for (int i = 0; i < 2; ++i)
-                                store16(own + lane * 2 * D + (((8 * c + 2 * q + i) ^ (lane & (kLanes - 1))) << 4), __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]),
-                                        __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+                                store16(staged(lane, 8 * c + 2 * q + i), __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
+                                        __float_as_uint(x[4 * i + 3]));
                         }
                     }
                     __syncwarp();
@@ -175,7 +180,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
 #pragma unroll 4
                     for (int n = 0; n < 32; n += kRowsAtOnce) {
                         const int row = n + lane / kLanes, to = 128 * tile + 32 * (warp & 3) + row;
-                        const float4 x = load_shared4(own + row * 2 * D + ((chunk ^ (row & (kLanes - 1))) << 4));
+                        const float4 x = load_shared4(staged(row, chunk));
                         if (to < walk.tile.rows) *reinterpret_cast<float4*>(part.parts + (entry * kTallRows + to) * D + (D / 2) * h + 4 * chunk) = x;
                     }
                     __syncwarp();

@@ -1,0 +1,163 @@
+"""Attention over the paged low-bit cache: every row against plain float64, with a bound of its own that a lost unit of keys, another row's result
+or zeros in its place go beyond.
+
+The bound of a row (a token's head), in the 2-norm over its n elements, which the basis change keeps.  u = 2^-11 is fp16's half step, p_j the row's
+probabilities, v_j the cached values, o the result, s_j the scores:
+  * independent roundings, one for each key or element: probabilities, u of each; where keys and values are rounded after their scales (the kernel for
+    many rows, more than 48 to a key head) u of each element, so that a score is off by some  e_j = scale u |q . k_j|_2  (the 2-norm of the products'
+    terms) and the result by  p_j e_j (v_j - o).  Their variances add:  sum p_j^2 (e_j^2 |v_j - o|^2 + 2 u^2 |v_j|^2); six standard deviations, of
+    roundings that are taken as large as they can be (a uniform one's deviation is u / sqrt 3);
+  * what may have one sign for all keys: a score is an fp32 sum of n products, 2^-16 of their absolute sum, and its exponential is off by 2^-20 and by
+    2^-22 of the largest |s|: g_j, for  sum p_j g_j |v_j - o|; probabilities (times scales) that small lose 2^-32 of the row's largest, times the largest |v|, a key;
+    sums over the keys: 2^-22 for every 16 of them, of sum p_j |v_j|, and 2^-24 a key in the sum of the exponentials;
+  * the result's own rounding: 2^-8 |o|, and 2^-19 for the basis change.
+lse: the same score errors, weighted by p_j, and the sum's."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_09679_b200 import synth
+from parity import to_f64
+from test_kv_cache import DEV, dense, i32, make_cache, make_plan, tables
+
+gpu = pytest.mark.gpu
+
+
+def expected(q, theta, k, v, table, lengths, starts, page, scale, prefix=(), prefix_length=0, rounded=True, drop=None):
+    """-> out [tokens][heads][n], lse, bound of |error| of each row of out, of lse.  q, k, v float64; drop: keys of each sequence that are left out."""
+    q, k, v, Q = (torch.as_tensor(np.asarray(x)) for x in (q, k, v, dense(theta)))
+    tokens, heads, n = q.shape
+    group = heads // k.shape[1]
+    out, lse = torch.zeros_like(q), torch.full((tokens, heads), -torch.inf, dtype=torch.float64)
+    tol, lse_tol = torch.zeros(tokens, heads, dtype=torch.float64), torch.zeros(tokens, heads, dtype=torch.float64)
+    flat = lambda x, pages, h, count: x[torch.as_tensor(np.asarray(pages, dtype=np.int64)), h].reshape(-1, n)[:count]
+    u = 2.0 ** -11
+    for b, length in enumerate(lengths):
+        first, last = int(starts[b]), int(starts[b + 1])
+        if first == last:
+            continue
+        own = length - (last - first) + torch.arange(last - first)  # a token's last key
+        for h in range(k.shape[1]):
+            kk, vv = (torch.cat([flat(x, prefix, h, prefix_length), flat(x, table[b], h, length)]) for x in (k, v))
+            seen = torch.arange(len(kk)) <= prefix_length + own[:, None].clamp(min=-1)  # [tokens][keys]
+            if drop is not None:
+                seen[:, prefix_length + drop.start:prefix_length + drop.stop] = False
+            seen = seen.repeat_interleave(group, 0)
+            x = q[first:last, h * group:(h + 1) * group].reshape(-1, n)
+            s = torch.where(seen, x @ kk.T * scale, -torch.inf)
+            if not len(kk):
+                continue
+            top = s.amax(1, keepdim=True)
+            e = torch.exp(s - torch.where(top > -torch.inf, top, 0.0))
+            total = e.sum(1, keepdim=True)
+            p = torch.where(total > 0, e / total, 0.0)
+            o = p @ vv
+            size = vv.square().sum(1)
+            apart = (size - 2 * o @ vv.T + o.square().sum(1, keepdim=True)).clamp(min=0)
+            terms = (u * scale) ** 2 * x.square() @ kk.square().T if rounded else torch.zeros(())
+            g = 2.0 ** -16 * abs(scale) * x.abs() @ kk.abs().T + 2.0 ** -20 + 2.0 ** -22 * torch.where(seen, s, 0.0).abs().amax(1, keepdim=True)
+            many = 2.0 ** -22 * (len(kk) / 16 + 16)
+            random = (p.square() * (terms * apart + (2 if rounded else 1) * u * u * size)).sum(1).sqrt()
+            signed = (p * g * apart.sqrt()).sum(1) + len(kk) * 2.0 ** -32 * size.max().sqrt() + many * (p @ size.sqrt()) + len(kk) * 2.0 ** -24 * o.norm(dim=1)
+            put = lambda to, what: to[first:last, h * group:(h + 1) * group].copy_(what.reshape(last - first, group, *what.shape[1:]))
+            put(out, o @ Q)
+            put(tol, 6 * random + signed + (2.0 ** -8 + 2.0 ** -19) * o.norm(dim=1) + 1e-30)
+            put(lse, (top + total.log())[:, 0])
+            put(lse_tol, 6 * (p.square() * terms).sum(1).sqrt() + (p * g).sum(1) + len(kk) * 2.0 ** -24 + 2.0 ** -22 * (top + total.log())[:, 0].abs().nan_to_num(posinf=0.0))
+    return out, lse, tol, lse_tol
+
+
+def beyond(out, lse, want):
+    """[tokens][heads]: rows whose result is further from the expected one than their bound."""
+    ref, ref_lse, tol, lse_tol = want
+    bad = ~((torch.as_tensor(to_f64(out)) - ref).norm(dim=-1) <= tol)
+    if lse is not None:
+        l = torch.as_tensor(to_f64(lse))
+        bad |= ~torch.where(ref_lse > -torch.inf, (l - ref_lse).abs() <= lse_tol, l == ref_lse)
+    return bad
+
+
+def check_rows(out, lse, want):
+    bad = beyond(out, lse, want)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} rows, first (token, head) {bad.nonzero()[0].tolist()}"
+
+
+def queries(tokens, heads, n, seed, size=2.0):
+    return (size * torch.randn((tokens, heads, n), generator=torch.Generator().manual_seed(seed))).to(torch.bfloat16)
+
+
+def host_cache_values(pages, heads, n, page, bits, seed, monkeypatch):
+    """A cache's values without a GPU."""
+    import test_kv_cache
+
+    monkeypatch.setattr(test_kv_cache, "DEV", "cpu")
+    return make_cache(pages, heads, n, page, bits, seed)[1]
+
+
+@pytest.mark.parametrize("rounded", [True, False])
+def test_the_bound_finds_what_is_wrong(rounded, monkeypatch):
+    """Mistakes planted in the oracle: zeros, a lost unit of 64 keys that has 3 % of a row's weight, a neighbour's row."""
+    n, page, lengths, news = 128, 16, [300, 2000, 4000], [20, 3, 2]
+    theta = to_f64(synth.angles(n, "normal", 3))
+    table, _, pages = tables(lengths, page, 0, 1)
+    k, v = host_cache_values(pages, 2, n, page, 4, 2, monkeypatch)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = to_f64(queries(int(starts[-1]), 4, n, 3))
+    args = (q, theta, k, v, table, lengths, starts, page, n ** -0.5)
+    want = expected(*args, rounded=rounded)
+    as_bf16 = want[0].to(torch.bfloat16)
+    assert not beyond(as_bf16, want[1].float(), want).any()
+    assert beyond(torch.zeros_like(as_bf16), None, want).all()
+    found = 0
+    for first in range(0, max(lengths), 64):
+        lost, lost_lse = expected(*args, rounded=rounded, drop=range(first, first + 64))[:2]
+        weight = 1 - (lost_lse - want[1]).exp()
+        assert (beyond(lost, lost_lse, want) | (weight < 0.03)).all()
+        found += int((weight >= 0.03).sum())
+    assert found > 4 * want[1].numel()
+    assert beyond(as_bf16.roll(1, 0), None, want).all()
+
+
+# ---- the kernel for many rows: pairs that follow one another in a CTA ---------------------------------------------------------------
+SHORT_PAIRS = [  # news, group: tiles of all 256 rows; of 129 to 200; two tiles a sequence of which the second is nearly empty; a second tile of 128 rows of nothing
+    ([64] * 40, 4), ([33 + 17 * (i % 2) for i in range(60)], 4), ([65] * 36, 4), ([70 + 3 * (i % 10) for i in range(44)], 2), ([13 + i % 20 for i in range(100)], 8)]
+
+
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (128, 8), (64, 4), (64, 8)])
+@pytest.mark.parametrize("news,group", SHORT_PAIRS)
+def test_many_short_pairs_to_a_cta(n, bits, news, group):
+    """Runs of some units that hold several pairs: what one pair leaves in shared memory is next to what the following one brings there."""
+    page, hkv = 64, 8
+    lengths = [max(m, 64 + (37 * b) % 237) for b, m in enumerate(news)]
+    p, theta = make_plan(n)
+    table, _, pages = tables(lengths, page, 0, 111)
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 112)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = queries(int(starts[-1]), hkv * group, n, 113)
+    call = lambda **some: p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), **some)
+    out, lse = call(want_lse=True)
+    again = [call() for _ in range(12)]
+    assert p.device_status() == 0
+    check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5))
+    assert all(torch.equal(out, o) for o in again)
+
+
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (128, 8)])
+def test_many_short_pairs_behind_a_prefix(n, bits):
+    """The prefix's pairs and the sequences' in one CTA's run."""
+    page, hkv, group, shared = 32, 8, 4, 200
+    news = [20 + 7 * (i % 5) for i in range(60)]
+    lengths = [m + (29 * b) % 150 for b, m in enumerate(news)]
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 0, 121, -(-shared // page))
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 122)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = queries(int(starts[-1]), hkv * group, n, 123)
+    call = lambda **some: p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), prefix=i32(prefix), prefix_length=shared, **some)
+    out, lse = call(want_lse=True)
+    again = [call() for _ in range(8)]
+    assert p.device_status() == 0
+    check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, shared))
+    assert all(torch.equal(out, o) for o in again)
