@@ -418,7 +418,9 @@ int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots,
  *               last of which is key lengths[b] - 1; each sees the keys up to its own.  NULL: token b is sequence b's only one.
  *   prefix      pages of a prefix that all sequences share, int32 [prefix_pages], of which prefix_length keys are read, once for the
  *               whole batch; every token sees all of them.  lengths and block_table do not count them.  prefix_length 0: none.
- * Probabilities (and, where more than 48 rows share their keys, the dequantized keys and values) are rounded to fp16, 2^-11 of each; all sums are fp32.
+ * Sums are fp32; those of products, on the tensor cores, lose up to 2^-24 of the running sum a key.  Rounded to fp16 are a row's probabilities, times
+ * their values' scales where up to 48 rows share their keys; where more do, the probabilities, and the keys and values times their scales.  Each is
+ * off by 2^-11 of itself, or by 2^-31 of the largest such number of the row (of the keys or values that the row's sequence has), whichever is more.
  * A row without keys (no length, or a token in front of its sequence's first key) is zero.  Rows of out and lse of tokens that no
  * sequence has stay as they were.  A row that sees a key whose scales are not finite may be NaN (bfq_kv_append
  * writes no such scale), other rows are not.  A page, length, start or number of tokens outside its range is reported by bfq_device_status

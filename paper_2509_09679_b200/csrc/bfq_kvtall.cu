@@ -14,6 +14,9 @@
 // fp16 of each element, 2^-12 on average and independent of its neighbours, a fraction of the output's own rounding.  Applied exactly, to
 // scores and probabilities, the scales would be read from shared memory 256 times by every softmax warp for a unit, which took three times as
 // long as everything else.
+// Probabilities go to fp16 times 2^7: the reference is at most 2^8 below the largest, so that they stay below 2^15, and one of 2^-32 of the row's
+// largest is still half a step there.  Without it what is below 2^-25 of the reference counted in the sum of the exponentials alone: beside a
+// large score whose value is near zero, as a prompt's first token has it, nothing was left of the result.
 // Shared-memory operands have the 128-byte swizzle: a row of 128 bytes is 64 elements d of one key (or query row), the two halves of
 // D = 128 lie one after the other; K is K-major, V the same bytes read MN-major.  The d within a 16-byte chunk stand in the order in which a
 // code word's pairs come out (0 4 1 5 2 6 3 7, or 0 2 1 3 of each four): Q's rows are stored in that order too, and O's columns are
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                     __syncwarp();
                 }
                 tmem_fence_before();
-                if (there) part.sums[entry * kTallRows + r] = make_float2(m, l);
+                if (there) part.sums[entry * kTallRows + r] = make_float2(m, l * 0x1p-7f);
             }
             if (tid == 0 && pair_from >= run.from) part.pairs[pair] = make_int2(blockIdx.x, (pair_from + walk.units - 1) / run.per - static_cast<int>(blockIdx.x) + 1);
             pair_from = done;
@@ -243,7 +246,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 }
                 first = false;
                 const float ref = m == -INFINITY ? 0.f : m;
-                const u64 scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
+                const u64 scale2 = pack2(scale, scale), ref2 = pack2(7.f - ref, 7.f - ref);
                 u64 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -375,7 +378,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 }
             }
             if (warp == 8 && lane == 0)
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors_at(s)), "f"(v_before / v_top), "f"(v_top * (1.f / 128.f)), "f"(k_top * (1.f / 128.f)), "f"(0.f)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors_at(s)), "f"(v_before / v_top), "f"(v_top * 0x1p-14f), "f"(k_top * 0x1p-7f), "f"(0.f)
                              : "memory");
             fence_operands();
             arrive(bar(kKvFull + s));

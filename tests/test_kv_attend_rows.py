@@ -8,15 +8,16 @@ probabilities, v_j the cached values, o the result, s_j the scores:
     terms) and the result by  p_j e_j (v_j - o).  Their variances add:  sum p_j^2 (e_j^2 |v_j - o|^2 + 2 u^2 |v_j|^2); six standard deviations, of
     roundings that are taken as large as they can be (a uniform one's deviation is u / sqrt 3);
   * what may have one sign for all keys: a score is an fp32 sum of n products, 2^-16 of their absolute sum, and its exponential is off by 2^-20 and by
-    2^-22 of the largest |s|: g_j, for  sum p_j g_j |v_j - o|; probabilities (times scales) that small lose 2^-32 of the row's largest, times the largest |v|, a key;
-    sums over the keys: 2^-22 for every 16 of them, of sum p_j |v_j|, and 2^-24 a key in the sum of the exponentials;
+    2^-22 of the largest |s|: g_j, for  sum p_j g_j |v_j - o|; probabilities (times scales) that small lose 2^-31 of the row's largest, times the largest |v|, a key;
+    sums over the keys: 2^-24 of the running sum a key, where the tensor cores cut what they add at some 2^-25 of it (a running sum is the difference
+    of two of the sums from the first key on, up to a part of a unit of 64 keys), and 2^-24 a key in the sum of the exponentials;
   * the result's own rounding: 2^-8 |o|, and 2^-19 for the basis change.
 lse: the same score errors, weighted by p_j, and the sum's."""
 import numpy as np
 import pytest
 import torch
 
-from paper_2509_09679_b200 import synth
+from paper_2509_09679_b200 import KVCache, synth
 from parity import to_f64
 from test_kv_cache import DEV, dense, i32, make_cache, make_plan, tables
 
@@ -56,9 +57,10 @@ def expected(q, theta, k, v, table, lengths, starts, page, scale, prefix=(), pre
             apart = (size - 2 * o @ vv.T + o.square().sum(1, keepdim=True)).clamp(min=0)
             terms = (u * scale) ** 2 * x.square() @ kk.square().T if rounded else torch.zeros(())
             g = 2.0 ** -16 * abs(scale) * x.abs() @ kk.abs().T + 2.0 ** -20 + 2.0 ** -22 * torch.where(seen, s, 0.0).abs().amax(1, keepdim=True)
-            many = 2.0 ** -22 * (len(kk) / 16 + 16)
+            units = torch.stack([a @ c for a, c in zip(p.split(64, 1), vv.split(64))], 1)  # [rows][units][n]
+            reach = 2 * units.cumsum(1).norm(dim=2).amax(1) + torch.stack([a @ c.sqrt() for a, c in zip(p.split(64, 1), size.split(64))], 1).amax(1)
             random = (p.square() * (terms * apart + (2 if rounded else 1) * u * u * size)).sum(1).sqrt()
-            signed = (p * g * apart.sqrt()).sum(1) + len(kk) * 2.0 ** -32 * size.max().sqrt() + many * (p @ size.sqrt()) + len(kk) * 2.0 ** -24 * o.norm(dim=1)
+            signed = (p * g * apart.sqrt()).sum(1) + len(kk) * (2.0 ** -31 * size.max().sqrt() + 2.0 ** -24 * (reach + o.norm(dim=1)))
             put = lambda to, what: to[first:last, h * group:(h + 1) * group].copy_(what.reshape(last - first, group, *what.shape[1:]))
             put(out, o @ Q)
             put(tol, 6 * random + signed + (2.0 ** -8 + 2.0 ** -19) * o.norm(dim=1) + 1e-30)
@@ -161,3 +163,58 @@ def test_many_short_pairs_behind_a_prefix(n, bits):
     assert p.device_status() == 0
     check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, shared))
     assert all(torch.equal(out, o) for o in again)
+
+
+# ---- small probabilities --------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("group", [64, 8])  # either kernel
+@pytest.mark.parametrize("sink", [True, False])
+def test_one_large_score_beside_many_small_ones(group, sink):
+    """A key whose probability is 2^18 to 2^31 times that of each of the 10^5 others, all in one CTA's run; its value is zero, so that the result is what
+    the others weigh together, or the same as theirs.  All other values are one row v: the result is a multiple of v, T v / (1 + T) or v, T the others'
+    weight.  It is off by 2^-8 for its own rounding, 2^-11 for the probabilities' (a scale's product with it: another), 2^-31 a key for those below it, 2^-24 of
+    the sum a key for either sum; and e^s by what the score is off, 2^-16 of it.  Rotated elements are off each by a part of its own, so that the bound holds for
+    a row's norm (and for no element of the model's basis)."""
+    n, page, bits, keys = 64, 256, 8, 100000
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    batch = sms if group > 48 else 4 * sms
+    p, theta = make_plan(n)
+    pages = -(-keys // page)
+    cache = KVCache.empty(pages, 1, n, page, bits, DEV)
+    code = torch.arange(n, device=DEV) * 37 % 255 - 127
+    code[3] = 127
+    cache.v_codes[:] = code.to(torch.int8).view(torch.uint8)
+    cache.v_scales[:] = 0.0123
+    if sink:
+        cache.v_codes[0, 0, 0] = 0
+    cache.k_codes[0, 0, 0, 5] = 127
+    cache.k_scales[0, 0, 0] = 1.0
+    q = torch.zeros((batch, group, n))
+    q[:, :, 5] = torch.linspace(18, 31, group) * np.log(2.0) / 127
+    q = q.to(torch.bfloat16).to(DEV)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).repeat(batch, 1)
+    out, lse = p.attend_kv(cache, q, table, i32([keys] * batch), scale=1.0, want_lse=True)
+    assert p.device_status() == 0
+    s, v = to_f64(q[:, :, 5]) * 127, to_f64(code) * float(cache.v_scales[0, 0, 1])
+    T = (keys - 1) * np.exp(-s)
+    gain = T / (1 + T) if sink else np.ones_like(T)
+    tol = gain * (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -18 + 2 * keys * 2.0 ** -24) + sink * gain * 2.0 ** -16 * s + keys * 2.0 ** -31
+    assert (np.linalg.norm(to_f64(out) - gain[..., None] * (v @ dense(theta)), axis=-1) <= tol * np.linalg.norm(v)).all()
+    assert (np.abs(to_f64(lse) - np.log(np.exp(s) + keys - 1)) <= 2.0 ** -16 * s + 2.0 ** -20 + keys * 2.0 ** -24).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (128, 8), (64, 4), (64, 8)])
+@pytest.mark.parametrize("prefix_length", [0, 3000])
+def test_many_rows_of_large_and_uneven_scores(n, bits, prefix_length):
+    """Scores that rise and fall by hundreds along the keys, in the tiles of 256 rows."""
+    page, lengths, news = 16, [600, 333, 70], [70, 40, 66]
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 0, 131, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, 2, n, page, bits, 132)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = (torch.tensor([1.0, 20.0, 60.0, 0.0, 5.0, 10.0]).view(1, 6, 1) * queries(int(starts[-1]), 6, n, 133, 1.0).float()).to(torch.bfloat16)
+    some = dict(prefix=i32(prefix), prefix_length=prefix_length) if prefix_length else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
+    assert p.device_status() == 0
+    check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
