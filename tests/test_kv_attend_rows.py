@@ -218,3 +218,43 @@ def test_many_rows_of_large_and_uneven_scores(n, bits, prefix_length):
     out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
     assert p.device_status() == 0
     check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
+
+
+# ---- 9 to 48 rows to a key head: exact codes, two tiles of 16 and more ------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (128, 8), (64, 4), (64, 8)])
+@pytest.mark.parametrize("news,group", [([4, 3, 1, 0, 4], 8), ([1, 1, 1], 16), ([3, 2, 1], 16), ([12, 5, 9, 1], 4), ([6, 5, 4, 3, 2, 1], 5)])
+@pytest.mark.parametrize("prefix_length", [0, 90])
+def test_nine_to_48_rows(n, bits, news, group, prefix_length):
+    """Up to 48 rows that share a key head keep keys and values exact: roundings are those of the probabilities alone."""
+    page, hkv = 32, 2
+    lengths = [m + x for m, x in zip(news, [1200, 3, 64, 0, 500, 31])]
+    assert max(news) * group <= 48
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 0, 141, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 142)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = queries(int(starts[-1]), hkv * group, n, 143)
+    some = dict(prefix=i32(prefix), prefix_length=prefix_length) if prefix_length else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
+    assert p.device_status() == 0
+    # a prefix of so few keys goes to the kernel for few rows, however many rows there are
+    check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length, rounded=False))
+
+
+# ---- runs of many units, sequences on both sides of 48 rows, every row looked at -----------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,bits", [(128, 4), (64, 8), (128, 8), (64, 4)])
+@pytest.mark.parametrize("news,lengths,prefix_length,hkv,group", [([1] * 7, [9, 0, 70, 1, 33, 5, 200], 16384, 8, 7), ([40, 3, 60], [40, 90, 2000], 9000, 4, 2), ([100], [9000], 0, 4, 2),
+                                                                  ([1, 150, 1, 24, 25, 0, 1], [3000, 4000, 1, 700, 25, 9, 77], 0, 4, 2)])
+def test_long_runs_row_by_row(n, bits, news, lengths, prefix_length, hkv, group):
+    page = 64
+    p, theta = make_plan(n)
+    table, prefix, pages = tables(lengths, page, 2, 151, -(-prefix_length // page))
+    cache, (k, v) = make_cache(pages, hkv, n, page, bits, 152)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = queries(int(starts[-1]), hkv * group, n, 153)
+    some = dict(prefix=i32(prefix), prefix_length=prefix_length) if prefix_length else {}
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
+    assert p.device_status() == 0
+    check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
