@@ -52,7 +52,7 @@ typedef enum {
     BFQ_ERR_WORKSPACE = -7,      /* angles not set yet, or plan workspace too small */
     BFQ_ERR_CUDA = -8,           /* a CUDA runtime call failed; see bfq_last_cuda_error */
     BFQ_ERR_DEVICE_TIMEOUT = -9, /* a bounded device-side wait gave up (reported by bfq_device_status) */
-    BFQ_ERR_TOO_LARGE = -10,     /* bfq_backward_noalloc: n exceeds BFQ_NOALLOC_MAX_N; bfq_kv_attend: more row tiles than it numbers */
+    BFQ_ERR_TOO_LARGE = -10,     /* bfq_backward_noalloc: n exceeds BFQ_NOALLOC_MAX_N; bfq_kv_attend: more work than it numbers */
     BFQ_ERR_INDEX = -11          /* a slot, position, page or length on the device outside its range (reported by bfq_device_status) */
 } bfq_status;
 
@@ -426,7 +426,10 @@ int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots,
  * writes no such scale), other rows are not.  A page, length, start or number of tokens outside its range is reported by bfq_device_status
  * (BFQ_ERR_INDEX) and the outputs of that call mean nothing; memory outside the arrays is not touched.  workspace: device,
  * 256-byte aligned, the caller's until the call's work on `stream` is done, at least bfq_kv_attend_workspace bytes (0 on
- * bad arguments; does not look at the data pointers' contents), BFQ_ERR_WORKSPACE otherwise.  Allocates nothing.
+ * bad arguments; does not look at the data pointers' contents), BFQ_ERR_WORKSPACE otherwise.  Allocates nothing.  BFQ_ERR_TOO_LARGE:
+ * counted are the row tiles that the tokens can have, in sequences in any order (8 to 256 rows each, and one more for every sequence), for each of the cache's
+ * heads: 2^27 of them, or 2^30 units of 64 (few rows: 128) keys in them where every sequence has as many keys as its row of block_table has
+ * places; or 2^30 tiles where every sequence has max_new tokens.
  */
 typedef struct {
     bfq_heads q, out;

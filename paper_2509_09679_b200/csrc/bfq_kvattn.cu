@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(128) k_join(const AttendParams p, int each) {
             const int pair = tile.place * p.cache.heads + h;
             if (tile.keys == 0) return;
             if (!waited) grid_dep_wait(), waited = true;
-            const int2 found = load_plain(part.pairs + pair);
+            const int2 found = ctas_of(part, pair);
             const int64_t first = static_cast<int64_t>(found.x) + pair;
             constexpr int kAtOnce = 4;  // results on their way
             float v[kAtOnce][kE];
@@ -624,16 +624,19 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     Part& front = p->prefix_tall ? p->tall : p->few;
     const int64_t tiles_prefix = in->prefix_length > 0 ? (rows + front.rows - 1) / front.rows : 0, tiles_few = (rows_few + p->few.rows - 1) / p->few.rows,
                   tiles_seq = (p->seq_tall ? (rows_seq + kTallRows - 1) / kTallRows : 0) + tiles_few;
-    if ((tiles_prefix + tiles_seq * in->batch) * cache->heads >= int64_t(1) << 27) return BFQ_ERR_TOO_LARGE;
-    // units are numbered in 32 bits, those of 64 keys at most
-    if (double(tiles_prefix) * (double(in->prefix_length) / kTallUnit + 1) * cache->heads +
-            double(tiles_seq) * in->batch * (double(int64_t(in->table_width) << p->cache.page_shift) / kTallUnit + 1) * cache->heads >= double(1 << 30))
-        return BFQ_ERR_TOO_LARGE;
     front.tiles_prefix = int(tiles_prefix), p->few.tiles_seq = int(tiles_few), p->tall.tiles_seq = int(tiles_seq - tiles_few);
+    int64_t pairs = 0;
     for (Part* part : {&p->few, &p->tall}) {
         part->rows_shift = part->rows == 8 ? 3 : (part->rows == 16 ? 4 : 8);
+        if (part->tiles_prefix + int64_t(in->batch) * part->tiles_seq >= int64_t(1) << 30) return BFQ_ERR_TOO_LARGE;
         part->by_tokens = in->q_starts != nullptr && part->tiles_seq > 0 && p->places_by_tokens(*part) < p->entries(*part);
+        const int64_t places = p->places(*part);  // as many as tiles, or more
+        auto units = [&](int64_t keys) { return (keys + (1 << part->unit_shift) - 1) >> part->unit_shift; };
+        const int64_t most = part->tiles_prefix * units(in->prefix_length) + (places - part->tiles_prefix) * units(int64_t(in->table_width) << p->cache.page_shift);
+        if (most > ((1 << 30) - 1) / cache->heads) return BFQ_ERR_TOO_LARGE;
+        part->most = int(most), pairs += places * cache->heads;
     }
+    if (pairs >= int64_t(1) << 27) return BFQ_ERR_TOO_LARGE;
     static_assert(kTallRows == 1 << 8, "shift");
     p->scale_log2 = in->scale * 1.4426950408889634f;
     p->tw = plan->tw, p->status = plan->status_word;
@@ -650,9 +653,8 @@ namespace {
 cudaError_t ctas_of_both(const bfq_plan* plan, const kv::AttendParams& p, int* few, int* tall) {
     *few = *tall = 0;
     auto least = [&](const kv::Part& part, int ctas) {
-        auto units = [&](int64_t keys) { return (keys + (1 << part.unit_shift) - 1) >> part.unit_shift; };
-        const int64_t most = (part.tiles_prefix * units(p.prefix_length) + int64_t(p.batch) * part.tiles_seq * units(int64_t(p.table_width) << p.cache.page_shift)) * p.cache.heads;
-        return most < ctas ? (most > 1 ? int(most) : 1) : ctas;
+        const int most = part.most * p.cache.heads;
+        return most < ctas ? (most > 1 ? most : 1) : ctas;
     };
     cudaError_t e = cudaSuccess;
     if (p.entries(p.few) > 0) e = kv::attend(plan, p, few), *few = least(p.few, *few);
@@ -683,7 +685,7 @@ extern "C" int bfq_kv_attend(bfq_plan* plan, const bfq_kv_cache* cache, const bf
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return BFQ_ERR_ALIGN;
         kv::lay_out(&p, plan->n, few, tall, static_cast<uint8_t*>(workspace));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
-        p.beside_tall = tall > 0;
+        p.beside_tall = tall > 0, p.few.ctas = few, p.tall.ctas = tall;
         if (tall > 0) e = kv::tall_launch(plan, p, tall, st);
         if (e == cudaSuccess && few > 0) e = kv::attend(plan, p, nullptr, few, st);
         if (e == cudaSuccess && p.join_tall) e = kv::join_tall_launch(plan, p, st);

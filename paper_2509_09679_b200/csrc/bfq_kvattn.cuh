@@ -7,6 +7,9 @@
 // entry (CTA + pair) of the workspace, which no other CTA writes: the CTA after it starts at this pair or a later one.  Pairs have their numbers there
 // from the places of their tiles: row tiles counted for each sequence alike, or, where most sequences have far fewer tokens than the most that
 // one may have, by the tokens in front of them, (first row of the sequence) / rows + sequence + tile, which rises from tile to tile too.
+// What is numbered in 32 bits is bounded by the tokens, not by what every sequence might have: the host refuses a call whose tokens in any order could
+// have more.  Starts that fall can have more all the same (they are reported, and their outputs mean nothing): sums stop at that bound, what
+// lies behind it is not done, and what the joins read of such a pair's place is brought into range.
 //
 // Two kernels do this: one for few rows (tiles of 8 or 16 rows), one for many (256 rows); each has its own Part of the work.  A call gives the
 // prefix's tiles to one of them, and each sequence goes by its own rows, seen on the device: a batch may hold chunks of prompts beside single tokens.
@@ -27,6 +30,8 @@ struct Part {
     int tiles_prefix, tiles_seq;  // row tiles of the prefix, and of each sequence
     int seq_from, seq_to;         // rows of the sequences that are this part's
     int by_tokens;                // how tiles are placed in the workspace
+    int most;                     // units of a key head, at most
+    int ctas;                     // of the launch
     int2* pairs;                  // [pairs] first CTA, CTAs
     float2* sums;                 // [entries][rows] m, l
     float* parts;                 // [entries][rows][D]
@@ -53,8 +58,8 @@ struct AttendParams {
     int beside_tall;            // the kernel for few rows follows the one for many
     int* status;
     __host__ __device__ int entries(const Part& part) const { return part.tiles_prefix + batch * part.tiles_seq; }
-    int64_t places_by_tokens(const Part& part) const { return part.tiles_prefix + (tokens * group >> part.rows_shift) + batch; }
-    int64_t places(const Part& part) const { return part.by_tokens ? places_by_tokens(part) : entries(part); }
+    __host__ __device__ int64_t places_by_tokens(const Part& part) const { return part.tiles_prefix + (tokens * group >> part.rows_shift) + batch; }
+    __host__ __device__ int64_t places(const Part& part) const { return part.by_tokens ? places_by_tokens(part) : entries(part); }
 };
 
 __device__ __forceinline__ int first_token(const AttendParams& p, int b) {
@@ -112,6 +117,26 @@ __device__ __forceinline__ Tile tile_of(const AttendParams& p, const Part& part,
     return t;
 }
 
+// The entry whose tile has a place behind the prefix's; -1: none has.
+__device__ __forceinline__ int entry_at(const AttendParams& p, const Part& part, int place) {
+    if (!part.by_tokens) return place;
+    auto first_place = [&](int b) { return part.tiles_prefix + (first_token(p, b) * p.group >> part.rows_shift) + b; };
+    int lo = 0, hi = p.batch;  // the last sequence whose places begin at or before this one
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first_place(mid) <= place) lo = mid;
+        else hi = mid;
+    }
+    const int rt = place - first_place(lo);
+    return rt >= 0 && rt < part.tiles_seq ? part.tiles_prefix + lo * part.tiles_seq + rt : -1;
+}
+// What a pair's place holds: its first CTA and how many have a part of it.
+__device__ __forceinline__ int2 ctas_of(const Part& part, int pair) {
+    const int2 v = load_plain(part.pairs + pair);
+    const int first = min(max(v.x, 0), part.ctas - 1);
+    return make_int2(first, min(max(v.y, 0), part.ctas - first));
+}
+
 // the entry to look at after e: a sequence's tiles without rows are its last ones
 __device__ __forceinline__ int after(const Part& part, int e, const Tile& t) {
     if (t.rows > 0 || e < part.tiles_prefix) return e + 1;
@@ -142,7 +167,7 @@ struct Walk {
     __device__ __forceinline__ int pair(const AttendParams& p) const { return tile.place * p.cache.heads + head; }
 };
 
-// A CTA's run of units, found by all its threads together from the lengths.  All numbers are below 2^31: the host has seen to that.
+// A CTA's run of units, found by all its threads together from the lengths.  Units of a head are at most part.most, which times the heads is below 2^30.
 struct Run {
     int from;   // the first one's number
     int per;    // units of every CTA but the last
@@ -157,35 +182,36 @@ __device__ __forceinline__ Run find_run(const AttendParams& p, const Part& part,
     int mine = 0;
     for (int e = tid * each; e < entries && e < (tid + 1) * each;) {
         const Tile t = tile_of(p, part, e);
-        mine += units_of(t), e = after(part, e, t);
+        mine = min(mine + units_of(t), part.most), e = after(part, e, t);
     }
     int before = mine, total = 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(0xFFFFFFFFu, before, o);
-        if (lane >= o) before += v;
+        if (lane >= o) before = min(before + v, part.most);
     }
     if (lane == 31) scan[warp] = before;
+    before = __shfl_up_sync(0xFFFFFFFFu, before, 1);
+    if (lane == 0) before = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += scan[w];
-        total += scan[w];
+        if (w == warp) before = min(before + total, part.most);
+        total = min(total + scan[w], part.most);
     }
-    before -= mine;
     total *= heads;
     Run run;
     run.per = total > 0 ? (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x) : 1;
     run.from = run.per * static_cast<int>(blockIdx.x);
     run.count = run.from < total ? (run.per < total - run.from ? run.per : total - run.from) : 0;
     if (run.count == 0) return run;
-    if (run.from >= before * heads && run.from < (before + mine) * heads) {  // one thread: the entry that holds `from` is one of its own
+    if (run.from >= before * heads && run.from - before * heads < mine * heads) {  // one thread: the entry that holds `from` is one of its own
         int e = tid * each;
         if (each > 1)
             for (;;) {
                 const Tile t = tile_of(p, part, e);
                 const int u = units_of(t);
-                if (run.from < (before + u) * heads) break;
+                if (run.from - before * heads < u * heads) break;
                 before += u, e = after(part, e, t);
             }
         scan[kWarps] = e, scan[kWarps + 1] = run.from - before * heads;

@@ -18,7 +18,7 @@ struct JoinSmem {
 };
 
 template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall(const AttendParams p) {
+__global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall(const AttendParams p, int chunks) {  // 32 rows of a place and a head each
     using S = JoinSmem<D>;
     extern __shared__ __align__(16) uint8_t smem[];
     grid_dep_wait();
@@ -26,16 +26,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps, D == 128 ? 3 : 5) k_join_tall
     const uint32_t table = smem_u32(smem), rows_at = table + S::kWarps + (threadIdx.x >> 5) * S::kWarp;
     const Part& part = p.tall;
     const bool scaled = RowTurn<D>::build(reinterpret_cast<float*>(smem), reinterpret_cast<float*>(smem + S::kProducts), p.tw);
-    const int chunks = part.tiles_seq * p.batch * heads * (kTallRows / 32);
     int of = -1;
     Tile tile{};
     for (int c = blockIdx.x * kJoinWarps + (threadIdx.x >> 5); c < chunks; c += gridDim.x * kJoinWarps) {
-        const int numbered = c / (kTallRows / 32), entry = numbered / heads, head = numbered - entry * heads, r = c % (kTallRows / 32) * 32 + lane;
-        if (entry != of) tile = tile_of(p, part, entry), of = entry;
+        const int numbered = c / (kTallRows / 32), place = numbered / heads, head = numbered - place * heads, r = c % (kTallRows / 32) * 32 + lane;
+        if (place != of) {
+            const int entry = entry_at(p, part, place);
+            tile = tile_of(p, part, max(entry, 0)), of = place;
+            if (entry < 0) tile.rows = 0;
+        }
         if (r - lane >= tile.rows) continue;
         const bool there = r < tile.rows;
         const int pair = tile.place * heads + head;
-        const int2 ctas = tile.keys > 0 ? load_plain(part.pairs + pair) : make_int2(0, 0);
+        const int2 ctas = tile.keys > 0 ? ctas_of(part, pair) : make_int2(0, 0);
         const int64_t first = (static_cast<int64_t>(ctas.x) + pair) * kTallRows + r;
         u64 x[D / 2];
 #pragma unroll
@@ -85,8 +88,8 @@ static cudaError_t launch(const bfq_plan* plan, const AttendParams& p, cudaStrea
         if (e != cudaSuccess) return e;
         occ = n > 0 ? n : 1;
     }
-    const int64_t chunks = int64_t(p.tall.tiles_seq) * p.batch * p.cache.heads * (kTallRows / 32), want = (chunks + kJoinWarps - 1) / kJoinWarps, most = int64_t(plan->sm_count) * occ;
-    return launch_overlapped(k_join_tall<D>, dim3(unsigned(want < most ? want : most)), dim3(32 * kJoinWarps), JoinSmem<D>::kBytes, st, p);
+    const int64_t chunks = p.places(p.tall) * p.cache.heads * (kTallRows / 32), want = (chunks + kJoinWarps - 1) / kJoinWarps, most = int64_t(plan->sm_count) * occ;
+    return launch_overlapped(k_join_tall<D>, dim3(unsigned(want < most ? want : most)), dim3(32 * kJoinWarps), JoinSmem<D>::kBytes, st, p, int(chunks));
 }
 cudaError_t join_tall_launch(const bfq_plan* plan, const AttendParams& p, cudaStream_t st) { return plan->n == 64 ? launch<64>(plan, p, st) : launch<128>(plan, p, st); }
 

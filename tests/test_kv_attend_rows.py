@@ -17,7 +17,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2509_09679_b200 import KVCache, synth
+from paper_2509_09679_b200 import KVCache, binding, synth
 from parity import to_f64
 from test_kv_cache import DEV, dense, i32, make_cache, make_plan, tables
 
@@ -258,3 +258,97 @@ def test_long_runs_row_by_row(n, bits, news, lengths, prefix_length, hkv, group)
     out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=max(news), want_lse=True, **some)
     assert p.device_status() == 0
     check_rows(out, lse, expected(to_f64(q), theta, k, v, table, lengths, starts, page, n ** -0.5, prefix, prefix_length))
+
+
+# ---- what a call has, not what it might have ------------------------------------------------------------------------------------------
+@gpu
+def test_a_large_batch_told_of_long_chunks():
+    """256 sequences, one chunk of 8192 tokens and 255 single ones, block tables for 131072 keys: work is counted by the tokens that there are."""
+    n, page, hkv, group, batch, width = 128, 256, 8, 8, 256, 512
+    p, theta = make_plan(n)
+    news = [1] * 100 + [8192] + [1] * 155
+    lengths = [(977 * b) % 3000 + 1 for b in range(batch)]
+    lengths[100], lengths[3] = 9000, 20000
+    pages = 90
+    cache, (k, v) = make_cache(pages, hkv, n, page, 4, 171)
+    rng = np.random.default_rng(172)
+    table = np.stack([rng.permutation(np.resize(np.arange(pages), width)) for _ in range(batch)])  # sequences share pages
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = queries(int(starts[-1]), hkv * group, n, 173)
+    out, lse = p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=8192, want_lse=True)
+    assert p.device_status() == 0 and torch.equal(out, p.attend_kv(cache, q.to(DEV), i32(table), i32(lengths), q_starts=i32(starts), max_new=8192))
+    rows = np.unique(np.concatenate([starts[:-1:17], [3, 99, 100, 101, 131, 132, 4000, 8100, 8291, 8292, starts[-1] - 1]]))
+    for t, b in zip(rows, np.searchsorted(starts, rows, side="right") - 1):
+        own = lengths[b] - int(starts[b + 1] - 1 - t)
+        check_rows(out[t:t + 1], lse[t:t + 1], expected(to_f64(q[t:t + 1]), theta, k, v, table[b:b + 1], [own], [0, 1], page, n ** -0.5))
+
+
+@gpu
+@pytest.mark.parametrize("n,group", [(64, 8), (128, 2)])
+def test_a_captured_call_told_of_long_chunks(n, group):
+    """One captured call, replayed on batches that have single tokens, chunks and empty sequences in every order; results in the places of the tokens."""
+    page, hkv, batch, tokens, width = 16, 4, 70, 2000, 2048
+    p, theta = make_plan(n)
+    pages = 300
+    cache, (k, v) = make_cache(pages, hkv, n, page, 8, 181)
+    rng = np.random.default_rng(182)
+    table = np.stack([rng.permutation(np.resize(np.arange(pages), width)) for _ in range(batch)])
+    q = queries(tokens, hkv * group, n, 183)
+    dev, t, lens, at = q.to(DEV), i32(table), i32([0] * batch), i32([0] * (batch + 1))
+    wide = torch.zeros((tokens, hkv * group, n), dtype=torch.bfloat16, device=DEV)
+    call = lambda: p.attend_kv(cache, dev, t, lens, q_starts=at, max_new=tokens, out=wide)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for news in ([1] * batch, [0] * 30 + [1500] + [1] * 38 + [400], [2000] + [0] * (batch - 1), [0] * (batch - 1) + [2000], [1] * 35 + [30] * 35, [(7 * b) % 50 for b in range(batch)], [0] * batch):
+        lengths = [m + (31 * b) % 200 if b % 3 else m for b, m in enumerate(news)]
+        starts = np.concatenate([[0], np.cumsum(news)])
+        lens.copy_(i32(lengths)), at.copy_(i32(starts)), wide.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        used = int(starts[-1])
+        assert p.device_status() == 0 and (wide[used:] == 7).all()
+        rows = np.unique(np.linspace(0, used - 1, 40).astype(int)) if used else []
+        for at_row, b in zip(rows, np.searchsorted(starts, rows, side="right") - 1):
+            own = lengths[b] - int(starts[b + 1] - 1 - at_row)
+            check_rows(wide[at_row:at_row + 1], None, expected(to_f64(q[at_row:at_row + 1]), theta, k, v, table[b:b + 1], [own], [0, 1], page, n ** -0.5))
+
+
+@gpu
+def test_starts_that_fall_in_a_large_batch_are_reported():
+    """Sequences that, with starts that fall again and again, have far more tokens together than the call."""
+    n, page, hkv, batch, tokens, width = 64, 16, 8, 300, 4000, 4096
+    p, _ = make_plan(n)
+    cache, _ = make_cache(64, hkv, n, page, 4, 191)
+    q = queries(tokens, hkv * 8, n, 192).to(DEV)
+    table, lens = i32(np.arange(batch * width).reshape(batch, width) % 64), i32([page * width] * batch)
+    for bad in ([0, tokens] * (batch // 2) + [0], [tokens, 0] * (batch // 2) + [tokens], [0] + [tokens, 1] * (batch // 2), list(range(batch, -1, -1))):
+        p.attend_kv(cache, q, table, lens, q_starts=i32(bad), max_new=tokens)
+        assert p.device_status() == -11
+    news = [1] * batch
+    starts = np.concatenate([[0], np.cumsum(news)])
+    few = i32([100] * batch)
+    good = [p.attend_kv(cache, q, table, few, q_starts=i32(starts), max_new=m) for m in (1, tokens)]
+    assert p.device_status() == 0 and (good[0][:batch].double() - good[1][:batch].double()).abs().max() <= 2.0 ** -6 * good[0][:batch].double().abs().max()
+
+
+@gpu
+def test_work_beyond_the_numbering_is_refused():
+    """More units than 2^30: tokens and batch times the places of a row of the block table; or more tiles of what every sequence might have."""
+    n, page = 64, 16
+    p, _ = make_plan(n)
+    cache, _ = make_cache(4, 8, n, page, 4, 201)
+    L, c = binding.lib(), p._cache(cache)
+    small, lens = i32([[0]]), i32([0])
+
+    def size(tokens, batch, max_new, width):
+        q = torch.zeros((1, 64, n), dtype=torch.bfloat16, device=DEV).expand(tokens, 64, n)
+        h = p._head_rows(q, None, None, torch.bfloat16, "q")
+        a = binding._CQueries(h, h, None, tokens, batch, small.data_ptr(), width, width, lens.data_ptr(), lens.data_ptr(), max_new, None, 0, 0, 1.0)
+        return L.bfq_kv_attend_workspace(p._h, c, binding.ctypes.byref(a)), L.bfq_kv_attend(p._h, c, binding.ctypes.byref(a), None, 0, None)
+
+    assert size(8447, 256, 8192, 8192)[0] > 0 and size(8447, 256, 8192, 8192)[1] == -7  # no workspace given
+    assert size(40000, 1 << 16, 40000, 8192)[1] == -10 and size(40000, 1 << 20, 40000, 1)[1] == -10
+    assert size(8447, 256, 8192, 1 << 25)[1] == -10
