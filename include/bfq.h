@@ -397,7 +397,9 @@ typedef struct {
  * slots: int64 [tokens]; a negative slot: the token's keys and values go nowhere (padding).  The other slots must differ from one another:
  * of two tokens with one slot, parts of either may stay.  q and q_out may both be NULL, and q_out may be q in place where q is bf16.
  * k, v and q are of type xt.  Calls with many rows run other kernels than calls with few and round differently: rows are off by at most 2^-20 of
- * their norm before they are rounded or quantized.  A slot or position outside its range is reported by bfq_device_status (BFQ_ERR_INDEX): that slot is not
+ * their norm before they are rounded or quantized.  A row that has one infinite element when it comes to Q is all infinities, of the signs of a
+ * column of Q: as a key or value the scale 65504 and the codes at both ends; with several it is infinities and NaN in some places.  A row with a NaN is all NaN,
+ * and zero in the cache; a norm makes one of an infinity.  A slot or position outside its range is reported by bfq_device_status (BFQ_ERR_INDEX): that slot is not
  * written, that position counts as 0.  Allocates nothing.
  */
 int bfq_kv_append(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots, int64_t tokens, bfq_dtype xt, const bfq_heads* k, const bfq_heads* v,

@@ -66,6 +66,13 @@ __device__ __forceinline__ float largest(const u64 (&x)[D / 2]) {  // NaN elemen
     }
     return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
+// An infinity as the largest number, so that its two terms are not NaN: with its row's factor infinite afterwards, a row with one becomes
+// infinities of Q's signs, as the stages one by one make of it.
+__device__ __forceinline__ uint32_t finite_pair(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
 // pairs (i, i + R / 2), R known to the compiler so that the row stays in registers
 template <int D, int R>
 __device__ __forceinline__ void turn_halves(u64 (&x)[D / 2], const float* table) {
@@ -314,8 +321,9 @@ __global__ void __launch_bounds__(kRowsThreads, AppendSmem<D, F32>::kCtas) k_app
                 if (p.interleaved) turn_neighbours<D>(p.rope_dims, x, angles);
                 else turn_halves_of<D>(p.rope_dims, x, angles);
             }
-            const RowPower power(largest<D>(x));
-            down = power.down * (1.f / 1024.f);
+            const float top = largest<D>(x);
+            const RowPower power(top);
+            down = top == INFINITY ? INFINITY : power.down * (1.f / 1024.f);
             const u64 up2 = pack2(power.up, power.up);
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -325,10 +333,10 @@ __global__ void __launch_bounds__(kRowsThreads, AppendSmem<D, F32>::kCtas) k_app
                     const u64 y = mul2(x[16 * c + i], up2);
                     float a, b;
                     unpack2(y, a, b);
-                    h[i] = half_pair(a, b);
+                    h[i] = finite_pair(a, b);
                     const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
                     unpack2(sub2(y, pack2(back.x, back.y)), a, b);
-                    l[i] = half_pair(a, b);
+                    l[i] = finite_pair(a, b);
                 }
                 tmem_st16(mine + 16 * c, h);
                 tmem_st16(mine + D / 2 + 16 * c, l);
