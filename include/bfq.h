@@ -416,8 +416,8 @@ int bfq_kv_read(bfq_plan* plan, const bfq_kv_cache* cache, const int64_t* slots,
  *   lse         fp32 [tokens][q heads], or NULL: log sum exp(scale q k), -infinity for a row without keys
  *   block_table int32 [batch][table_width], rows table_ld apart: a sequence's pages in order; lengths int32 [batch]: its cached keys, those
  *               of its own tokens in this call included (pages behind them are not looked at)
- *   q_starts    int32 [batch + 1], not decreasing: sequence b has tokens q_starts[b] .. q_starts[b + 1] - 1 of q, at most max_new of them, the
- *               last of which is key lengths[b] - 1; each sees the keys up to its own.  NULL: token b is sequence b's only one.
+ *   q_starts    int32 [batch + 1], not decreasing: sequence b has tokens q_starts[b] .. q_starts[b + 1] - 1 of q, at most max_new of them (a
+ *               caller's limit: it may be above the tokens), the last of which is key lengths[b] - 1; each sees the keys up to its own.  NULL: token b is sequence b's only one.
  *   prefix      pages of a prefix that all sequences share, int32 [prefix_pages], of which prefix_length keys are read, once for the
  *               whole batch; every token sees all of them.  lengths and block_table do not count them.  prefix_length 0: none.
  * Sums are fp32; those of products, on the tensor cores, lose up to 2^-24 of the running sum a key.  Rounded to fp16 are a row's probabilities, times

@@ -18,6 +18,8 @@
 // left operand; the probabilities, keys by queries, are turned by movmatrix into its right one.
 //
 // What bounds it: instructions, some two thirds of them codes to fp16 (9 for 8 codes of 4 bits, 10 for 8 of 8).
+#include <algorithm>
+
 #include "bfq_kvattn.cuh"
 #include "bfq_n4096.cuh"
 
@@ -607,10 +609,10 @@ static int set_up(const bfq_plan* plan, const bfq_kv_cache* cache, const bfq_kv_
     for (const void* at : {static_cast<const void*>(in->lengths), static_cast<const void*>(in->block_table), static_cast<const void*>(in->q_starts),
                            static_cast<const void*>(in->prefix), static_cast<const void*>(in->lse)})
         if ((reinterpret_cast<uintptr_t>(at) & 3u) != 0) return BFQ_ERR_ALIGN;
-    if (in->q_starts == nullptr ? in->tokens < in->batch : in->max_new < 1 || in->max_new > in->tokens) return BFQ_ERR_STRIDE;
+    if (in->q_starts == nullptr ? in->tokens < in->batch : in->max_new < 1) return BFQ_ERR_STRIDE;
     p->lse = in->lse, p->block_table = in->block_table, p->table_ld = in->table_ld, p->table_width = in->table_width, p->lengths = in->lengths;
     p->q_starts = in->q_starts, p->prefix = in->prefix, p->prefix_pages = in->prefix_pages, p->prefix_length = cache->pages > 0 ? int(in->prefix_length) : 0;
-    p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : in->max_new;
+    p->tokens = in->tokens, p->batch = in->batch, p->group = in->q.heads / cache->heads, p->max_new = in->q_starts == nullptr ? 1 : int(std::min<int64_t>(in->max_new, in->tokens));
     const int64_t rows = (in->q_starts == nullptr ? in->batch : in->tokens) * int64_t(p->group), rows_seq = int64_t(p->max_new) * p->group;
     p->seq_tall = use_tall(rows_seq), p->prefix_tall = prefix_use_tall(rows, p->seq_tall, in->prefix_length, cache->heads, plan->sm_count);
     p->join_tall = p->seq_tall && p->prefix_length == 0 && in->tokens * in->q.heads > kJoinTallRows;

@@ -352,3 +352,25 @@ def test_work_beyond_the_numbering_is_refused():
     assert size(8447, 256, 8192, 8192)[0] > 0 and size(8447, 256, 8192, 8192)[1] == -7  # no workspace given
     assert size(40000, 1 << 16, 40000, 8192)[1] == -10 and size(40000, 1 << 20, 40000, 1)[1] == -10
     assert size(8447, 256, 8192, 1 << 25)[1] == -10
+
+
+def c_queries(p, q, out, table, lengths, starts, max_new):
+    a = binding._CQueries(p._head_rows(q, None, None, torch.bfloat16, "q"), p._head_rows(out, None, None, torch.bfloat16, "out"), None, q.shape[0], lengths.shape[0],
+                          table.data_ptr(), table.shape[1], table.shape[1], lengths.data_ptr(), starts.data_ptr(), max_new, None, 0, 0, p.n ** -0.5)
+    return binding.ctypes.byref(a)
+
+
+@gpu
+def test_the_c_entry_takes_a_max_new_above_the_tokens():
+    """A caller's limit of new tokens for each sequence, whatever this call has."""
+    p, _ = make_plan(64)
+    cache, _ = make_cache(8, 2, 64, 16, 4, 161)
+    q, table, lengths, starts = queries(3, 4, 64, 162).to(DEV), i32([[0, 1, 2, 3], [4, 5, 6, 7]]), i32([50, 60]), i32([0, 2, 3])
+    want, out, L, c = p.attend_kv(cache, q, table, lengths, q_starts=starts, max_new=3), torch.zeros_like(q), binding.lib(), p._cache(cache)
+    for max_new in (4, 1000, 2 ** 31 - 1):
+        a = c_queries(p, q, out.zero_(), table, lengths, starts, max_new)
+        size = L.bfq_kv_attend_workspace(p._h, c, a)
+        room = torch.empty(size + 256, dtype=torch.uint8, device=DEV)
+        assert size and L.bfq_kv_attend(p._h, c, a, (room.data_ptr() + 255) // 256 * 256, size, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(out, want) and p.device_status() == 0
+    assert L.bfq_kv_attend_workspace(p._h, c, c_queries(p, q, out, table, lengths, starts, 0)) == 0
