@@ -874,7 +874,7 @@ const char* bfq_status_string(int status) {
         case BFQ_ERR_WORKSPACE: return "angles not set or workspace too small";
         case BFQ_ERR_CUDA: return "CUDA runtime error";
         case BFQ_ERR_DEVICE_TIMEOUT: return "bounded device-side wait gave up";
-        case BFQ_ERR_TOO_LARGE: return "row length exceeds the fixed scratch of the no-allocation entry point";
+        case BFQ_ERR_TOO_LARGE: return "more than the call has room for (row length of the no-allocation backward) or numbers (work of one attention call)";
         case BFQ_ERR_INDEX: return "index on the device out of range";
         default: return "unknown status";
     }

@@ -374,3 +374,8 @@ def test_the_c_entry_takes_a_max_new_above_the_tokens():
         assert size and L.bfq_kv_attend(p._h, c, a, (room.data_ptr() + 255) // 256 * 256, size, torch.cuda.current_stream().cuda_stream) == 0
         assert torch.equal(out, want) and p.device_status() == 0
     assert L.bfq_kv_attend_workspace(p._h, c, c_queries(p, q, out, table, lengths, starts, 0)) == 0
+
+
+def test_the_error_of_too_much_work_says_so():
+    text = binding.lib().bfq_status_string(-10).decode()
+    assert "attention" in text and "no-allocation" in text
