@@ -17,7 +17,8 @@
 // units of 4 (2) codes: the halves of a register are two keys' codes of the same element, which is what the second product needs of its
 // left operand; the probabilities, keys by queries, are turned by movmatrix into its right one.
 //
-// What bounds it: instructions, some two thirds of them codes to fp16 (9 for 8 codes of 4 bits, 10 for 8 of 8).
+// What bounds it: long contexts of 8-bit codes, memory (0.85 of the copy's rate).  4-bit codes, instructions and their latencies together: of 720 for 32
+// keys 272 turn codes into fp16 (9 for 8 codes of 4 bits, 10 for 8 of 8); the schedulers issue in 0.59 of their cycles, ALU 49 %.
 #include <algorithm>
 
 #include "bfq_kvattn.cuh"
@@ -557,6 +558,8 @@ static cudaError_t attend(const bfq_plan* plan, const AttendParams& p, int* ctas
 // Tiles of 256 rows where there are rows enough to pay for them.  The kernel for few rows against the one for many, us (4-bit cache, n = 128, 8 key
 // heads): 16 sequences of 4096 keys, 32 rows each 63 / 88, 48 rows 91 / 91, 64 rows 114 / 95, 256 rows 422 / 137; 64 of 2048 keys, 48 rows
 // 193 / 221, 64 rows 251 / 226.  One sequence of 2048 keys alone fills no more than the start of either: 64 rows 14 / 18, 256 rows 27 / 23.
+// Other forms, 16 sequences of 4096 keys that come from memory (as above: 48 rows 102 / 121, 64 rows 127 / 123): n = 128 at 8 bits, 48 rows 107 / 145, 64 rows
+// 135 / 147, 96 rows 188 / 152; n = 64 at 4 bits, 48 rows 86 / 94, 64 rows 107 / 96, at 8 bits 92 / 96 and 115 / 98.
 static bool use_tall(int64_t rows) { return rows > kFewMost; }
 // A prefix too, but where the sequences do not need that kernel's launch beside theirs only from five units of 16 rows and 128 keys to an SM on:
 // 8192 keys, 32 rows 28 / 30, 64 rows 48 / 31; 1024 keys, 64 rows 17 / 23, 128 rows (3.5 units) 23 / 25, 256 rows (7) 38 / 27.
@@ -564,8 +567,9 @@ static bool prefix_use_tall(int64_t rows, bool seq_tall, int64_t keys, int heads
     return use_tall(rows) && (seq_tall || ((rows + 15) / 16) * ((keys + kFewUnit - 1) / kFewUnit) * heads > 5 * sm_count);
 }
 // A row to a thread in the join where the rows fill the chip so; else a row to a warp, whose lanes have the results' weights at once.  Whole calls
-// with k_join_tall against k_join, us (as above): 16 sequences, 8192 rows of results 101 / 95, 16384 rows 118 / 114 (n = 64: 87 / 91), 32768 rows
-// 137 / 152; one sequence, 512 rows 46 / 18.
+// with k_join_tall against k_join, us: one sequence, 512 rows 46 / 18; 16 sequences of 2048 keys from memory, 8192, 16384 and 32768 rows of results:
+// n = 128 at 4 bits 84 / 82, 90 / 90, 98 / 117, at 8 bits 98 / 94, 102 / 104, 113 / 129; n = 64 at 4 bits 66 / 64, 66 / 72, 78 / 96, at 8 bits 68 / 66, 70 / 74,
+// 78 / 98.
 constexpr int64_t kJoinTallRows = 16384;
 
 // The workspace: for each of the two kernels pairs, sums and parts.  Lays them out from `at` on (null: only counts); returns the bytes.

@@ -520,9 +520,15 @@ static cudaError_t launch_rows(const bfq_plan* plan, Kernel kern, bool* ready, i
     const int64_t want = (rows + 128 * kGroups - 1) / (128 * kGroups), most = int64_t(plan->sm_count) * S::kCtas;
     return launch_overlapped(kern, dim3(unsigned(want < most ? want : most)), dim3(kRowsThreads), S::kBytes, st, p);
 }
-// Measured either side (us; bf16, 32 + 2 x 8 heads appended with norms and positions / read, few : many): n = 128, 6144 rows 6.7 : 12.1 / 6.2 : 7.6,
-// 12288 13.8 : 12.3 / 7.2 : 7.6, 24576 20.8 : 12.5 / 9.5 : 7.9, 65280 37.7 : 21.8 / 16.0 : 11.7; n = 64, 6144 4.2 : 7.3 / 3.4 : 4.7,
-// 12288 5.3 : 7.4 / 4.5 : 4.6, 24576 11.0 : 7.4 / 5.4 : 4.8, 65280 19.5 : 10.4 / 8.5 : 6.9.
+// One line for appending and reading, either width and type.  Measured either side (us, few : many; 32 + 2 x 8 heads with norms and positions):
+//     rows                  6144         9216         12288        16368        24576
+//     append, n = 64, bf16  4.7 : 7.9    7.2 : 8.1    6.0 : 8.1    8.8 : 8.0    11.6 : 8.1
+//                     fp32  4.9 : 8.6    7.1 : 8.5    6.0 : 8.6    9.1 : 8.5    11.7 : 8.5
+//            n = 128, bf16  7.2 : 12.7  11.9 : 12.6  14.4 : 12.9  16.7 : 13.1  21.4 : 13.2
+//                     fp32  7.2 : 13.8  12.3 : 14.1  14.7 : 13.8  16.4 : 14.2  22.1 : 14.2
+//     read, n = 64          4.0 : 5.0    4.5 : 5.0    5.1 : 5.0    5.5 : 5.4     6.1 : 5.5
+//           n = 128         6.7 : 8.1    7.0 : 8.1    7.7 : 8.2    8.6 : 8.1    10.1 : 8.5
+// Appending at n = 128 would cross at some 10000 rows: up to 3.6 us are lost there between them and the line.
 static bool few_rows(int64_t rows) { return rows < 16384; }
 
 template <int D, bool F32, int BITS>
