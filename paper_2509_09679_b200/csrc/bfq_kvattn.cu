@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     const bool a_box = lane * box < kKeys;
     constexpr int64_t kNone = -(int64_t(1) << 32);
     int64_t page = kNone;  // of the lane's box; kNone: it has no keys
-    int sent = 0;          // units
+    int sent = 0;          // units; above count: a wait has given up
     auto look = [&]() {
         const int key = ahead.unit * kFewUnit + own;
         page = sent < count && a_box && key < ahead.tile.keys ? load_plain(ahead.tile.pages + (key >> p.cache.page_shift)) : kNone;
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
     for (int i = 0; i < count; ++i) {
         const int key0 = now.unit * kFewUnit + kKeys * warp;
         const uint32_t stage = stage_at(slot), scales = scales_at(slot);
-        wait_for(full(slot), phase, &dead, p.status);
+        const bool stuck = sent <= count && !wait_for(full(slot), phase, &dead, p.status);
         if (key0 < now.tile.keys) {
             // ---- scores of 32 keys: rows g and g + 8 of product j are keys 16 j + g and 16 j + 8 + g of the warp's
             float s[NB][2][4];
@@ -392,7 +392,15 @@ __global__ void __launch_bounds__(kAttendThreads, NB == 2 ? 2 : (D * BITS == 102
                     }
             }
         }
-        __syncwarp();
+        if (__any_sync(0xFFFFFFFFu, stuck)) {
+            // no copies go to a slot whose last ones have not come; those in flight, of up to kCount units, are waited for
+            uint32_t parity = phase;
+            for (int k = 0, x = slot; k < S::kCount && i + k < sent; ++k) {
+                drain(full(x), parity);
+                if (++x == S::kCount) x = 0, parity ^= 1;
+            }
+            sent = count + 1;
+        }
         fetch(slot);
         if (++slot == S::kCount) slot = 0, phase ^= 1;
         if (now.unit + 1 == now.units || i + 1 == count) {

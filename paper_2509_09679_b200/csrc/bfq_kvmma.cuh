@@ -65,20 +65,26 @@ struct RowPower {
     }
 };
 
-// Waits for a phase, with a limit.  Once one wait has given up all others of the CTA return at once (what they wait for may never come): the
-// kernel ends with meaningless outputs and the status word says so.
+// Waits for a phase, with a limit; false: gave up.  Once one wait has given up all others of the CTA return at once (what they wait for may never
+// come): the kernel ends with meaningless outputs and the status word says so, after it has drained what it has in flight.
 constexpr long long kWaitCycles = 1ll << 31;  // about a second
-__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
-    if (mbar_try_wait(bar, parity)) return;
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+    if (mbar_try_wait(bar, parity)) return true;
     const long long since = clock64();
     while (!mbar_try_wait(bar, parity)) {
-        if (*dead) return;
+        if (*dead) return false;
         if (clock64() - since > kWaitCycles) {
             *dead = 1;
             atomicExch(status, 3);
-            return;
+            return false;
         }
     }
+    return true;
+}
+// After a wait has given up: copies or products in flight still read and write the CTA's memory, which must not end before them.  A limit of its own.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+    const long long since = clock64();
+    while (!mbar_try_wait(bar, parity) && clock64() - since <= kWaitCycles) {}
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 

@@ -218,6 +218,13 @@ __device__ __forceinline__ void multiply(uint32_t columns, uint32_t matrix, uint
     phase ^= 1;
     tmem_fence_after();
 }
+// Before the CTA ends: products in flight after a wait has given up.  done: a barrier of the group's own.
+__device__ __forceinline__ void products_done(uint32_t done, volatile int* dead) {
+    if ((threadIdx.x >> 5 & 3) == 0 && __any_sync(0xFFFFFFFFu, *dead)) {
+        commit_to(elect_one(), done);
+        drain(done, 0);
+    }
+}
 // the result's row, times f
 template <int D>
 __device__ __forceinline__ void result_row(uint32_t at, float f, u64 (&x)[D / 2]) {
@@ -270,7 +277,7 @@ __global__ void __launch_bounds__(kRowsThreads, AppendSmem<D, F32>::kCtas) k_app
     auto angles_of = [&](int position) { return p.rope + (position >= 0 && position < p.rope_rows ? position : 0) * int64_t(p.rope_dims); };
     fetch(find(tiles.at));
     if (threadIdx.x == 0) {
-        for (int g = 0; g < kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);
+        for (int g = 0; g < 2 * kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);  // of a product, of all after a wait has given up
         mbar_init_fence();
         dead = 0;
     }
@@ -400,6 +407,7 @@ __global__ void __launch_bounds__(kRowsThreads, AppendSmem<D, F32>::kCtas) k_app
         if (F32) fetch(next);
     }
     copies_done();
+    products_done(bar + 8 * kGroups, &dead);
     tmem_fence_before();
     __syncthreads();
     if (warp == 0) tensor_memory_free<4 * D>(tmem_at);
@@ -445,7 +453,7 @@ __global__ void __launch_bounds__(kRowsThreads, ReadSmem<D, F32, BITS>::kCtas) k
     Row now = find(tiles.at);
     fetch(now);
     if (threadIdx.x == 0) {
-        for (int g = 0; g < kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);
+        for (int g = 0; g < 2 * kGroups; ++g) mbar_init(base + S::kBars + 8 * g, 1);  // of a product, of all after a wait has given up
         mbar_init_fence();
         dead = 0;
     }
@@ -501,6 +509,7 @@ __global__ void __launch_bounds__(kRowsThreads, ReadSmem<D, F32, BITS>::kCtas) k
         now = next;
     }
     copies_done();
+    products_done(bar + 8 * kGroups, &dead);
     tmem_fence_before();
     __syncthreads();
     if (warp == 0) tensor_memory_free<4 * D>(tmem_at);

@@ -40,8 +40,9 @@ struct TallSmem {
     static constexpr uint32_t kBars = kFactors + kStageCount * 16;
     static constexpr uint32_t kBytes = kBars + 24 * 8 + 1024;  // and what rounding the base up to 1024 takes
 };
-// per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products of a unit done, of a pair
-enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kOFull = 20, kBarCount = 22 };
+// per stage: operands there, free; per tile and buffer: scores there, probabilities there; per tile: queries there, products of a unit done, of a pair; all
+// products done (after a wait has given up)
+enum Bar { kKvFull = 0, kKvEmpty = 4, kSFull = 8, kPFull = 12, kQFull = 16, kDone = 18, kOFull = 20, kAllDone = 22, kBarCount = 23 };
 
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendParams p) {
@@ -69,6 +70,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             mbar_init(bar(kSFull + s), 1), mbar_init(bar(kPFull + s), 128);
         }
         for (int t = 0; t < 2; ++t) mbar_init(bar(kQFull + t), 128), mbar_init(bar(kDone + t), 1), mbar_init(bar(kOFull + t), 1);
+        mbar_init(bar(kAllDone), 1);
         mbar_init_fence();
         dead = 0;
     }
@@ -453,6 +455,10 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
             }
             for (int i = count > kStageCount ? count - kStageCount : 0; i < count; ++i)  // the last arrivals have come
                 wait_all(bar(kKvEmpty + (i & 3)), (i >> 2) & 1, &dead, p.status);
+            if (__any_sync(0xFFFFFFFFu, dead)) {
+                commit_to(lead, bar(kAllDone));
+                drain(bar(kAllDone), 0);
+            }
         }
         __syncwarp();
     }
