@@ -68,12 +68,12 @@ struct RowPower {
 // Waits for a phase, with a limit; false: gave up.  Once one wait has given up all others of the CTA return at once (what they wait for may never
 // come): the kernel ends with meaningless outputs and the status word says so, after it has drained what it has in flight.
 constexpr long long kWaitCycles = 1ll << 31;  // about a second
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* dead, int* status, long long cycles = kWaitCycles) {
     if (mbar_try_wait(bar, parity)) return true;
     const long long since = clock64();
     while (!mbar_try_wait(bar, parity)) {
         if (*dead) return false;
-        if (clock64() - since > kWaitCycles) {
+        if (clock64() - since > cycles) {
             *dead = 1;
             atomicExch(status, 3);
             return false;

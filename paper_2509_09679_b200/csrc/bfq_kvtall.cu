@@ -203,10 +203,12 @@ __global__ void __launch_bounds__(kTallThreads, 1) k_attend_tall(const AttendPar
                 const int key0 = walk.unit * kTallUnit, buffer = i & 1;
                 const bool edge = key0 + kTallUnit > least;  // some row of the warp ends in this unit, or has ended
                 const uint32_t s_at = scores(tile, buffer) + lanes;
-                // the factors and the scores, usually both there: one latency
+                // the factors and the scores, usually both there: one latency.  The warps of tile 1 pass over pairs that have no rows for it, and
+                // may be here while all of the run before is still to be done: a wait is given 2^14 cycles for each unit of it (2350 are usual)
+                const long long cycles = kWaitCycles + (static_cast<long long>(i) << 14);
                 const bool kv_there = mbar_try_wait(bar(kKvFull + (i & 3)), (i >> 2) & 1), s_there = mbar_try_wait(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1);
-                if (!kv_there) wait_for(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status);
-                if (!s_there) wait_for(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1, &dead, p.status);
+                if (!kv_there) wait_for(bar(kKvFull + (i & 3)), (i >> 2) & 1, &dead, p.status, cycles);
+                if (!s_there) wait_for(bar(kSFull + 2 * tile + buffer), s_phase >> buffer & 1, &dead, p.status, cycles);
                 s_phase ^= 1u << buffer;
                 tmem_fence_after();
                 uint32_t v[2][32];

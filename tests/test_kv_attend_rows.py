@@ -379,3 +379,30 @@ def test_the_c_entry_takes_a_max_new_above_the_tokens():
 def test_the_error_of_too_much_work_says_so():
     text = binding.lib().bfq_status_string(-10).decode()
     assert "attention" in text and "no-allocation" in text
+
+
+# ---- a run of more than a second ------------------------------------------------------------------------------------------------------
+@gpu
+def test_a_tile_that_waits_for_a_long_run():
+    """Sequences of one tile of 128 rows, keys of which take a CTA some two seconds, and at the end of its run one with two tiles: the second tile's
+    warps have waited all that time.  All sequences are the same million keys and the same queries, so that one alone gives every result."""
+    n, page, bits, hkv, group, keys = 64, 256, 4, 8, 64, 1 << 20
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    each = 20  # sequences to a CTA: 8 x 16384 units each, some 1600 cycles a unit
+    p, _ = make_plan(n)
+    pages = 64
+    cache, _ = make_cache(pages, hkv, n, page, bits, 211)
+    news = ([1] * (each - 1) + [3]) * sms
+    starts = torch.from_numpy(np.concatenate([[0], np.cumsum(news)])).to(torch.int32).to(DEV)
+    table = (torch.arange(keys // page, dtype=torch.int32, device=DEV) % pages).repeat(len(news), 1)
+    one = queries(3, hkv * group, n, 212).to(DEV)
+    q = torch.cat([one[:1].expand(each - 1, -1, -1), one]).repeat(sms, 1, 1)
+    lengths = torch.full((len(news),), keys, dtype=torch.int32, device=DEV)
+    out = p.attend_kv(cache, q, table, lengths, q_starts=starts, max_new=3)
+    assert p.device_status() == 0
+    alone = [p.attend_kv(cache, x, table[:1], lengths[:1], q_starts=i32([0, len(x)]), max_new=3) for x in (one[:1], one)]
+    assert p.device_status() == 0
+    got = out.view(sms, each + 2, hkv * group, n)
+    for rows, ref in ((got[:, :each - 1], alone[0]), (got[:, each - 1:], alone[1])):
+        # other splits of the keys: a rounding to bf16 each, and sums that lose up to 2^-24 a key
+        assert ((rows.double() - ref.double()).norm(dim=-1) <= (2.0 ** -7 + 2 * keys * 2.0 ** -24) * ref.double().norm(dim=-1)).all()
